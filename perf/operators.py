@@ -7,8 +7,8 @@ norm_fwd      layer norm of rows of features, with the statistics that its
 norm_bwd      its backward pass: the gradients of the rows, and those of the
               weight and the bias, summed over the rows
 logprob_fwd   log probabilities of given tokens (or classes) under the softmax
-              of each row of logits, with its entropy and its k likeliest
-              alternatives
+              of each row of logits, with its entropy, its k likeliest
+              alternatives and the statistics that the backward pass takes
 logprob_bwd   the gradient of these log probabilities and entropies in the logits
 clip          the global norm of a list of gradients and their clipping to it
 
@@ -147,8 +147,8 @@ def work(case):
         return {"bytes": 3 * n * b + 3 * w + 8 * rows, "flops": 15 * n}
     n = rows * case["vocab"]
     if op == "logprob_fwd":
-        return {"bytes": n * b + rows * (8 + 12 + 12 * case["top"]), "flops": 6 * n}
-    return {"bytes": 2 * n * b + rows * (16 + (8 if case["entropy"] else 0)), "flops": 8 * n}
+        return {"bytes": n * b + rows * (8 + 20 + 12 * case["top"]), "flops": 6 * n}
+    return {"bytes": 2 * n * b + rows * (20 + (8 if case["entropy"] else 0)), "flops": 8 * n}
 
 
 # ----------------------------------------------------------------- inputs
@@ -205,10 +205,12 @@ def _inputs(case, seed):
     d = {"logits": z, "targets": given}
     if case["op"] == "logprob_bwd":
         d["dlogp"] = -_uniform(g, rows) / rows  # a weighted mean of the losses
-        s = z.float() * case["scale"]
-        d["lse"] = torch.logsumexp(s, 1)
+        f = z.float()
+        peak = f.max(1)[0]
+        s = (f - peak[:, None]) * case["scale"]
+        d["stats"] = torch.stack([peak, torch.logsumexp(s, 1)], 1)
         if case["entropy"]:
-            s -= d["lse"][:, None]
+            s -= d["stats"][:, 1:]
             d["entropy"] = -torch.where(s == -math.inf, torch.zeros_like(s), s * s.exp()).sum(1)
             d["dentropy"] = -0.01 * _uniform(g, rows) / rows
     return d
@@ -266,12 +268,12 @@ def _run_own(state):
         return {"dx": dx, "dw": dw, "db": db}
     if op == "logprob_fwd":
         r = m.logprob_fwd(d["logits"], d["targets"], top=case["top"], scale=case["scale"])
-        res = {"logp": r.logp, "lse": r.lse, "entropy": r.entropy}
+        res = {"logp": r.logp, "lse": r.lse, "entropy": r.entropy, "stats": r.stats}
         if case["top"]:
             res.update(top_logp=r.top_logp, top_index=r.top_index)
         return res
     if op == "logprob_bwd":
-        return {"dlogits": m.logprob_bwd(d["logits"], d["lse"], d["targets"], d["dlogp"],
+        return {"dlogits": m.logprob_bwd(d["logits"], d["stats"], d["targets"], d["dlogp"],
                                          d.get("entropy"), d.get("dentropy"),
                                          scale=case["scale"], **out)}
     norm = m.grad_clip(d["grads"], case["max_norm"], out=out["clipped"], norm=out["norm"],
@@ -322,22 +324,22 @@ def _run_plain(state):
     at = t.clamp(min=0)[:, None]
     if op == "logprob_fwd":
         z = d["logits"].float()
-        s = z * case["scale"]
-        s = s - s.max(1, keepdim=True)[0]
+        peak = z.max(1)[0]
+        s = (z - peak[:, None]) * case["scale"]
         e = torch.exp(s)
         total = e.sum(1)
-        shift = (z.max(1)[0] * case["scale"])
-        lse = shift + torch.log(total)
+        lse = peak * case["scale"] + torch.log(total)
         logp = torch.where(given, s.gather(1, at)[:, 0] - torch.log(total), torch.zeros_like(lse))
         weighted = torch.where(e > 0, e * s, torch.zeros_like(s)).sum(1)
-        out = {"logp": logp, "lse": lse, "entropy": torch.log(total) - weighted / total}
+        out = {"logp": logp, "lse": lse, "entropy": torch.log(total) - weighted / total,
+               "stats": torch.stack([peak, torch.log(total)], 1)}
         if case["top"]:
             # Ties go to the lowest index (+ 0.0: the two zeros are equal).
             index = torch.sort(z + 0.0, dim=1, descending=True, stable=True)[1][:, :case["top"]]
             out["top_logp"] = s.gather(1, index) - torch.log(total)[:, None]
             out["top_index"] = index
         return out
-    s = d["logits"].float() * case["scale"] - d["lse"][:, None]
+    s = (d["logits"].float() - d["stats"][:, :1]) * case["scale"] - d["stats"][:, 1:]
     p = torch.exp(s)
     dlogp = torch.where(given, d["dlogp"], torch.zeros_like(d["dlogp"]))
     dz = -p * dlogp[:, None]
@@ -400,6 +402,8 @@ def _exact_rows(case, d, r):
     if op == "logprob_fwd":
         out = {"logp": torch.where(one > 0, lp, torch.zeros_like(lp)).sum(1),
                "lse": torch.logsumexp(z, 1), "entropy": -plogp.sum(1)}
+        peak = d["logits"][r].max(1)[0].double()
+        out["stats"] = torch.stack([peak, out["lse"] - peak * case["scale"]], 1)
         if case["top"]:
             order = torch.sort(d["logits"][r].double() + 0.0, dim=1, descending=True, stable=True)
             index = order.indices[:, :case["top"]]
