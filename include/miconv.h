@@ -73,8 +73,11 @@ typedef enum miconv_status {
     MICONV_ERR_PASS = -8,      /* unknown pass id */
     MICONV_ERR_PLAN = -9,      /* plan index outside [0, conv_plan_count()) */
     MICONV_ERR_MODE = -10,     /* pooling mode other than MICONV_POOL_MAX / _AVG */
-    MICONV_ERR_SCRATCH = -11   /* conv_bwd_weight_noalloc: the plan's workspace exceeds
+    MICONV_ERR_SCRATCH = -11,  /* conv_bwd_weight_noalloc: the plan's workspace exceeds
                                   MICONV_NOALLOC_SCRATCH_BYTES */
+    MICONV_ERR_TYPE = -12,     /* mitrain.h: unknown element type, or types that do not
+                                  go together */
+    MICONV_ERR_VALUE = -13     /* mitrain.h: a number outside the operator's range */
 } miconv_status;
 
 /* Pass ids for conv_workspace_size and the plan calls. */

@@ -5,6 +5,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 if __package__ in (None, ""):
     sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
@@ -13,8 +15,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIBRARY = os.path.join(PKG, "libmiconv.so")
-SOURCES = ["api.hip", "conv_kernels.hip", "wino_kernels.hip",
-           "pool_kernels.hip"]
+SOURCES = ["api.hip", "conv_kernels.hip", "wino_kernels.hip", "pool_kernels.hip",
+           "train_api.hip", "norm_kernels.hip", "logprob_kernels.hip", "clip_kernels.hip"]
 PEAK_LIBRARY = os.path.join(PKG, "libmipeak.so")
 PEAK_SOURCES = ["peaks.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -28,9 +30,8 @@ FLAGS = [
 ]
 
 
-def _compile(sources, out, verbose):
-    tmp = out + ".tmp"
-    cmd = [HIPCC] + FLAGS + [os.path.join(CSRC, s) for s in sources] + ["-o", tmp]
+def _hipcc(args, verbose):
+    cmd = [HIPCC] + args
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -41,6 +42,18 @@ def _compile(sources, out, verbose):
         raise RuntimeError(f"hipcc failed ({res.returncode}):\n{text}")
     if text.strip() and verbose:
         print(text, file=sys.stderr)
+
+
+def _compile(sources, out, verbose):
+    """Each source to an object (several at a time), the objects to out.tmp."""
+    tmp = out + ".tmp"
+    flags = [f for f in FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as obj_dir, ThreadPoolExecutor(4) as pool:
+        objs = [os.path.join(obj_dir, s + ".o") for s in sources]
+        list(pool.map(lambda so: _hipcc(
+            flags + ["-c", os.path.join(CSRC, so[0]), "-o", so[1]], verbose),
+            zip(sources, objs)))
+        _hipcc(["--offload-arch=gfx950", "-fPIC", "-shared"] + objs + ["-o", tmp], verbose)
     return tmp
 
 

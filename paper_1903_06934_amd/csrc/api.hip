@@ -149,6 +149,8 @@ int check_buffers(const Range *r, int n, const bool *required, const void *ws, s
     return MICONV_OK;
 }
 
+}  // namespace
+
 // Compute units of the current device (its multiProcessorCount, read once
 // per device), or 256, the MI355X's, when no device can be queried (the
 // host-only plan and workspace queries still work then).
@@ -172,9 +174,6 @@ int num_cus()
     return n;
 }
 
-int target_workgroups() { return 4 * num_cus(); }
-int tap_target_workgroups() { return 16 * num_cus(); }
-
 int check_device()
 {
     static std::atomic<int> cache[64];  // 0 unknown, 1 gfx950, 2 other
@@ -194,6 +193,13 @@ int check_device()
         cache[dev].store(ok ? 1 : 2, std::memory_order_relaxed);
     return ok ? MICONV_OK : MICONV_ERR_DEVICE;
 }
+
+int launch_status(hipError_t e) { return e == hipSuccess ? MICONV_OK : MICONV_ERR_LAUNCH; }
+
+namespace {
+
+int target_workgroups() { return 4 * num_cus(); }
+int tap_target_workgroups() { return 16 * num_cus(); }
 
 // ------------------------------------------------------------ kernel choice
 int gemm_tiles(int M, int Ncol, int bm, int bn)
@@ -1659,7 +1665,6 @@ WgradPlan wgrad_current(const Geom &g)
 }
 
 // ------------------------------------------------------------ execution
-int launch_status(hipError_t e) { return e == hipSuccess ? MICONV_OK : MICONV_ERR_LAUNCH; }
 
 // Caller-owned timing events of conv_set_timing_events, per calling thread.
 struct TimingEvents {
@@ -2723,6 +2728,8 @@ const char *conv_error_string(int status)
     case MICONV_ERR_MODE: return "unknown pooling mode";
     case MICONV_ERR_SCRATCH:
         return "the plan needs more workspace than the library's fixed device scratch holds";
+    case MICONV_ERR_TYPE: return "unknown element type, or types that do not go together";
+    case MICONV_ERR_VALUE: return "a number outside the operator's range";
     default: return "unknown status";
     }
 }

@@ -24,6 +24,12 @@ __host__ __device__ inline uint32_t fast_div(uint32_t n, FastDiv f)
 
 FastDiv make_fastdiv(uint32_t d);
 
+// Of the current device (api.hip): compute units, MICONV_OK or
+// MICONV_ERR_DEVICE; the status of a launch.
+int num_cus();
+int check_device();
+int launch_status(hipError_t e);
+
 // ---------------------------------------------------------------------------
 // Implicit GEMM whose columns are pixels of an image-like output and whose
 // B operand gathers from an image-like source.  Used for the forward pass

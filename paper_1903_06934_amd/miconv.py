@@ -1,4 +1,5 @@
-"""ctypes binding of libmiconv.so (include/miconv.h).
+"""ctypes binding of libmiconv.so (include/miconv.h; mitrain.py binds the
+operators of include/mitrain.h).
 
 Argument marshalling only: every pass runs in the library's HIP kernels.
 Tensors are torch tensors used as device memory (float32, contiguous, on the
@@ -19,6 +20,7 @@ STATUS = {
     -3: "MICONV_ERR_WORKSPACE", -4: "MICONV_ERR_ALIAS", -5: "MICONV_ERR_ALIGN",
     -6: "MICONV_ERR_DEVICE", -7: "MICONV_ERR_LAUNCH", -8: "MICONV_ERR_PASS",
     -9: "MICONV_ERR_PLAN", -10: "MICONV_ERR_MODE", -11: "MICONV_ERR_SCRATCH",
+    -12: "MICONV_ERR_TYPE", -13: "MICONV_ERR_VALUE",
 }
 POOL_MODES = {"max": 0, "avg": 1}
 PASS_FWD, PASS_BWD_DATA, PASS_BWD_WEIGHT = 0, 1, 2
@@ -27,6 +29,8 @@ _lib = None
 _I = ctypes.c_int
 _P = ctypes.c_void_p
 _Z = ctypes.c_size_t
+_L = ctypes.c_longlong
+_F = ctypes.c_float
 
 
 class MiconvError(RuntimeError):
@@ -86,6 +90,23 @@ def lib():
     L.pool_fwd.restype = _I
     L.pool_bwd.argtypes = [_I] * 9 + [_P, _P, _P, _P]
     L.pool_bwd.restype = _I
+    rows = [_I, _L, _L]  # element type, rows, columns
+    L.layernorm_fwd_workspace_size.argtypes = rows
+    L.layernorm_bwd_workspace_size.argtypes = rows
+    L.layernorm_fwd.argtypes = [_I] + rows + [_P, _L, _P, _P, _F, _P, _L, _P, _P, _P, _Z, _P]
+    L.layernorm_bwd.argtypes = [_I] + rows + [_P, _L, _P, _L, _P, _P, _P, _P, _L, _P, _P, _P, _Z,
+                                              _P]
+    L.logprob_fwd_workspace_size.argtypes = rows + [_I]
+    L.logprob_fwd.argtypes = rows + [_P, _L, _P, _F, _I] + [_P] * 7 + [_Z, _P]
+    L.logprob_bwd.argtypes = rows + [_P, _L, _P, _F, _P, _P, _P, _P, _P, _L, _P]
+    L.grad_workspace_size.argtypes = [_I, _P, _P]
+    L.grad_norm.argtypes = [_I] + [_P] * 5 + [_Z, _P]
+    L.grad_clip.argtypes = [_I, _P, _P, _P, _F, _P, _P, _P, _Z, _P]
+    for name in ("layernorm_fwd", "layernorm_bwd", "logprob_fwd", "logprob_bwd", "grad_norm",
+                 "grad_clip"):
+        getattr(L, name).restype = _I
+    for name in ("layernorm_fwd", "layernorm_bwd", "logprob_fwd", "grad"):
+        getattr(L, name + "_workspace_size").restype = _Z
     _lib = L
     return L
 
