@@ -2,6 +2,7 @@
 // a row is read once and held in registers between its statistics and its
 // result.
 #include <algorithm>
+#include <initializer_list>
 
 #include "internal.h"
 #include "rows.h"
@@ -11,77 +12,122 @@ namespace miconv {
 
 namespace {
 
-// ------------------------------------------------------------ rows in registers
-// A group of tpr threads (a power of two: up to a wave, or the whole
-// workgroup) holds a row: thread t the vectors t, t + tpr, ..., NV of them.
-// The variance is taken about the mean, from the registers.
-template <class T, class TW, int NV>
-__global__ __launch_bounds__(1024) void norm_fwd_rows(NormFwdArgs a, int tpr)
+// The N weights at column c of a row of cols (`none` without weights).
+template <int N, class TW>
+__device__ __forceinline__ void load_weights(const TW *w, long long c, long long cols, float none,
+                                             float *f)
 {
-    constexpr int N = Pack<T>::N;
-    __shared__ float red[2][16];
-    const T *x = (const T *)a.x.p;
-    T *y = (T *)a.y.p;
-    const TW *w = (const TW *)a.w, *b = (const TW *)a.b;
-    const int cols = (int)a.cols;
-    const int t = threadIdx.x & (tpr - 1);
-    const long long row = (long long)blockIdx.x * (blockDim.x / tpr) + threadIdx.x / tpr;
-    if (row >= a.rows)  // whole groups; a workgroup of one group has one row
+#pragma unroll
+    for (int j = 0; j < N; j++)
+        f[j] = none;
+    if (!w || c >= cols)
         return;
-    const T *xr = x + row * a.x.ld;
-    typename Pack<T>::V raw[NV];
+    if (c + N <= cols) {
+        constexpr int K = Pack<TW>::N < N ? Pack<TW>::N : N;
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const int c = (t + i * tpr) * N;
-        raw[i] = typename Pack<T>::V{};
-        if (c < cols)
-            raw[i] = load_pack<T>(xr + c, cols - c, (T)0.f);
-    }
-    const float n = (float)cols;
-    float s = 0.f;
+        for (int i = 0; i < N; i += K) {
+            typedef TW V __attribute__((ext_vector_type(K), aligned(sizeof(TW))));
+            const V v = *(const V *)(w + c + i);
 #pragma unroll
-    for (int i = 0; i < NV; i++)
+            for (int j = 0; j < K; j++)
+                f[i + j] = (float)v[j];
+        }
+    } else {
 #pragma unroll
         for (int j = 0; j < N; j++)
-            s += (float)raw[i][j];
-    const float mean = group_reduce(s, tpr, red[0], Add()) / n;
-    float q = 0.f;
+            if (c + j < cols)
+                f[j] = (float)w[c + j];
+    }
+}
+
+// ------------------------------------------------------------ rows in registers
+// A group of tpr threads (a power of two up to a wave, or a workgroup of some
+// waves) holds a row: thread t the vectors t, t + tpr, ..., NV of them.
+// The variance is taken about the mean, from the registers.  Groups take row
+// after row; HOLD: with their weights and biases in registers.
+template <class T, class TW, int NV, bool HOLD, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, bool stream)
+{
+    constexpr int N = Pack<T>::N;
+    __shared__ float red[2][2][16];
+    const TW *w = (const TW *)a.w, *b = (const TW *)a.b;
+    const int cols = (int)a.cols;
+    const int t = tpr > 64 ? threadIdx.x : threadIdx.x & (tpr - 1);
+    const int groups = blockDim.x / tpr;
+    const float n = (float)cols;
+    float wv[HOLD ? NV : 1][N], bv[HOLD ? NV : 1][N];
+    if constexpr (HOLD)
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const int left = cols - (t + i * tpr) * N;
-#pragma unroll
-        for (int j = 0; j < N; j++) {
-            const float d = (float)raw[i][j] - mean;
-            q += j < left ? d * d : 0.f;
+        for (int i = 0; i < NV; i++) {
+            load_weights<N>(w, (t + i * tpr) * N, cols, 1.f, wv[i]);
+            load_weights<N>(b, (t + i * tpr) * N, cols, 0.f, bv[i]);
         }
-    }
-    const float var = group_reduce(q, tpr, red[1], Add()) / n;
-    const float rstd = 1.f / sqrtf(var + a.eps);
-    if (t == 0) {
-        if (a.mean)
-            a.mean[row] = mean;
-        if (a.rstd)
-            a.rstd[row] = rstd;
-    }
-    T *yr = y + row * a.y.ld;
+    int turn = 0;
+    for (long long row = (long long)blockIdx.x * groups + threadIdx.x / tpr; row < a.rows;
+         row += (long long)gridDim.x * groups) {
+        const T *xr = (const T *)a.x.p + row * a.x.ld;
+        typename Pack<T>::V raw[NV];
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const int c = (t + i * tpr) * N;
-        if (c >= cols)
-            continue;
-        typename Pack<T>::V v;
-#pragma unroll
-        for (int j = 0; j < N; j++) {
-            float f = ((float)raw[i][j] - mean) * rstd;
-            if (c + j < cols) {
-                if (w)
-                    f *= (float)w[c + j];
-                if (b)
-                    f += (float)b[c + j];
+        for (int i = 0; i < NV; i++) {
+            const int c = (t + i * tpr) * N;
+            raw[i] = typename Pack<T>::V{};
+            if (c < cols) {
+                if (stream)
+                    raw[i] = load_pack<T, true>(xr + c, cols - c, (T)0.f);
+                else
+                    raw[i] = load_pack<T>(xr + c, cols - c, (T)0.f);
             }
-            v[j] = (T)f;
         }
-        store_pack<T>(yr + c, cols - c, v);
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; i++)
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                s += (float)raw[i][j];
+        const float mean = group_reduce(s, tpr, red[turn][0], Add()) / n;
+        float q = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const int left = cols - (t + i * tpr) * N;
+            if (left >= N) {
+#pragma unroll
+                for (int j = 0; j < N; j++) {
+                    const float d = (float)raw[i][j] - mean;
+                    q += d * d;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; j++) {
+                    const float d = (float)raw[i][j] - mean;
+                    q += j < left ? d * d : 0.f;
+                }
+            }
+        }
+        const float var = group_reduce(q, tpr, red[turn][1], Add()) / n;
+        turn ^= 1;
+        const float rstd = 1.f / sqrtf(var + a.eps);
+        if (t == 0) {
+            if (a.mean)
+                a.mean[row] = mean;
+            if (a.rstd)
+                a.rstd[row] = rstd;
+        }
+        T *yr = (T *)a.y.p + row * a.y.ld;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const int c = (t + i * tpr) * N, h = HOLD ? i : 0;
+            if (c >= cols)
+                continue;
+            if constexpr (!HOLD) {
+                load_weights<N>(w, c, cols, 1.f, wv[0]);
+                load_weights<N>(b, c, cols, 0.f, bv[0]);
+            }
+            typename Pack<T>::V v;
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                v[j] = (T)(((float)raw[i][j] - mean) * rstd * wv[h][j] + bv[h][j]);
+            store_pack<T>(yr + c, cols - c, v);
+        }
     }
 }
 
@@ -113,7 +159,9 @@ __device__ __forceinline__ Moments wave_merge(Moments m)
     return m;
 }
 
-// Rows cut into `splits` pieces of `piece` elements (a multiple of a pack):
+constexpr int kPieces = 64;
+
+// Rows cut into `splits` (at most kPieces) pieces of `piece` elements (a multiple of a pack):
 // the moments of each piece to ws[row][split].
 template <class T>
 __global__ __launch_bounds__(256) void norm_fwd_pieces(NormFwdArgs a, long long piece, int splits)
@@ -153,8 +201,8 @@ __global__ __launch_bounds__(256) void norm_fwd_pieces(NormFwdArgs a, long long 
     }
 }
 
-// The pieces' results: every workgroup merges its row's moments (in the order
-// of the pieces) and normalises one piece.
+// The pieces' results: every wave merges its row's moments (at most kPieces) and
+// normalises its part of one piece.
 template <class T, class TW>
 __global__ __launch_bounds__(256) void norm_fwd_apply(NormFwdArgs a, long long piece, int splits)
 {
@@ -162,9 +210,11 @@ __global__ __launch_bounds__(256) void norm_fwd_apply(NormFwdArgs a, long long p
     const long long row = blockIdx.x / splits;
     const int split = (int)(blockIdx.x - row * splits);
     const Moments *parts = (const Moments *)a.ws + row * splits;
-    Moments m = parts[0];
-    for (int i = 1; i < splits; i++)
-        m = merge(m, parts[i]);
+    const int lane = threadIdx.x & 63;
+    Moments m{0.f, 0.f, 0.f};
+    if (lane < splits)
+        m = parts[lane];
+    m = wave_merge(m);
     const float mean = m.mean, rstd = 1.f / sqrtf(m.m2 / (float)a.cols + a.eps);
     if (split == 0 && threadIdx.x == 0) {
         if (a.mean)
@@ -180,80 +230,111 @@ __global__ __launch_bounds__(256) void norm_fwd_apply(NormFwdArgs a, long long p
     for (long long c = first + threadIdx.x * N; c < end; c += 256 * N) {
         const int left = (int)min((long long)N, end - c);
         const auto raw = load_pack<T>(xr + c, left, (T)0.f);
+        float wv[N], bv[N];
+        load_weights<N>(w, c, a.cols, 1.f, wv);
+        load_weights<N>(b, c, a.cols, 0.f, bv);
         typename Pack<T>::V v;
 #pragma unroll
-        for (int j = 0; j < N; j++) {
-            float f = ((float)raw[j] - mean) * rstd;
-            if (j < left) {
-                if (w)
-                    f *= (float)w[c + j];
-                if (b)
-                    f += (float)b[c + j];
-            }
-            v[j] = (T)f;
-        }
+        for (int j = 0; j < N; j++)
+            v[j] = (T)(((float)raw[j] - mean) * rstd * wv[j] + bv[j]);
         store_pack<T>(yr + c, left, v);
     }
 }
 
 // -------------------------------------------------------------------- backward
-// Rows in registers as forward; a thread's columns are the same for all its
-// rows, so it sums its columns' share of dw and db in registers over the
-// rows g, g + groups, ... of its group g.  The groups of a workgroup meet in
-// LDS, the workgroups in parts[workgroup][2][cols].
-template <class T, class TW, int NV>
-__global__ __launch_bounds__(1024) void norm_bwd_rows(NormBwdArgs a, int tpr)
+// Rows in registers as forward, the next one's loads in flight while a row is
+// worked on; a thread's columns are the same for all its rows, so it sums its
+// columns' share of dw and db in registers over the rows of its group.  The
+// groups of a workgroup meet in LDS, the workgroups in
+// parts[workgroup][2][cols], or, if there is one only, it writes dw and db.
+// Elements past the row's end are zeros in dy.
+template <class T, class TW, int NV, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, bool stream)
 {
     constexpr int N = Pack<T>::N;
     extern __shared__ float lds[];
     __shared__ float red[2][2][16];
     const int cols = (int)a.cols;
-    const int t = threadIdx.x & (tpr - 1), group = threadIdx.x / tpr;
-    const int groups = blockDim.x / tpr;
-    const TW *w = (const TW *)a.w;
+    const int t = tpr > 64 ? threadIdx.x : threadIdx.x & (tpr - 1);
+    const int groups = blockDim.x / tpr, group = tpr > 64 ? 0 : threadIdx.x / tpr;
     const float inv_n = 1.f / (float)cols;
     float wv[NV][N], sw[NV][N], sb[NV][N];
 #pragma unroll
-    for (int i = 0; i < NV; i++)
+    for (int i = 0; i < NV; i++) {
+        load_weights<N>((const TW *)a.w, (t + i * tpr) * N, cols, 1.f, wv[i]);
 #pragma unroll
-        for (int j = 0; j < N; j++) {
-            const int c = (t + i * tpr) * N + j;
-            wv[i][j] = c < cols ? (w ? (float)w[c] : 1.f) : 0.f;
+        for (int j = 0; j < N; j++)
             sw[i][j] = sb[i][j] = 0.f;
-        }
-    int turn = 0;
-    for (long long row = (long long)blockIdx.x * groups + group; row < a.rows;
-         row += (long long)gridDim.x * groups) {
+    }
+    typename Pack<T>::V rx[NV], rd[NV], nx[NV], nd[NV];
+    float mean = 0.f, rstd = 0.f, nmean = 0.f, nrstd = 0.f;
+    const auto load = [&](long long row) {
+        if (row >= a.rows)
+            return;
         const T *xr = (const T *)a.x.p + row * a.x.ld;
         const T *dyr = (const T *)a.dy.p + row * a.dy.ld;
-        typename Pack<T>::V rx[NV], rd[NV];
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const int c = (t + i * tpr) * N;
-            rx[i] = rd[i] = typename Pack<T>::V{};
+            nx[i] = nd[i] = typename Pack<T>::V{};
             if (c < cols) {
-                rx[i] = load_pack<T>(xr + c, cols - c, (T)0.f);
-                rd[i] = load_pack<T>(dyr + c, cols - c, (T)0.f);
+                if (stream) {
+                    nx[i] = load_pack<T, true>(xr + c, cols - c, (T)0.f);
+                    nd[i] = load_pack<T, true>(dyr + c, cols - c, (T)0.f);
+                } else {
+                    nx[i] = load_pack<T>(xr + c, cols - c, (T)0.f);
+                    nd[i] = load_pack<T>(dyr + c, cols - c, (T)0.f);
+                }
             }
         }
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        nmean = a.mean[row];
+        nrstd = a.rstd[row];
+    };
+    const long long step = (long long)gridDim.x * groups;
+    long long row = (long long)blockIdx.x * groups + group;
+    load(row);
+    int turn = 0;
+    for (; row < a.rows; row += step) {  // one row for the workgroup where it meets at the barrier
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            rx[i] = nx[i];
+            rd[i] = nd[i];
+        }
+        mean = nmean;
+        rstd = nrstd;
+        load(row + step);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; i++)
 #pragma unroll
             for (int j = 0; j < N; j++) {
                 const float d = (float)rd[i][j], u = ((float)rx[i][j] - mean) * rstd;
+                const float g = d * wv[i][j];
                 sw[i][j] += d * u;
                 sb[i][j] += d;
-                s1 += d * wv[i][j];
-                s2 += d * wv[i][j] * u;
+                s1 += g;
+                s2 += g * u;
             }
         if (!a.dx.p)
             continue;
-        s1 = group_reduce(s1, tpr, red[turn][0], Add()) * inv_n;
-        s2 = group_reduce(s2, tpr, red[turn][1], Add()) * inv_n;
-        turn ^= 1;
+        s1 = wave_reduce(s1, tpr, Add());
+        s2 = wave_reduce(s2, tpr, Add());
+        if (tpr > 64) {
+            if ((threadIdx.x & 63) == 0) {
+                red[turn][0][threadIdx.x >> 6] = s1;
+                red[turn][1][threadIdx.x >> 6] = s2;
+            }
+            __syncthreads();
+            s1 = red[turn][0][0];
+            s2 = red[turn][1][0];
+            for (int v = 1; v < tpr >> 6; v++) {
+                s1 += red[turn][0][v];
+                s2 += red[turn][1][v];
+            }
+            turn ^= 1;
+        }
         T *dxr = (T *)a.dx.p + row * a.dx.ld;
+        const float c1 = s1 * inv_n, c2 = s2 * inv_n;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const int c = (t + i * tpr) * N;
@@ -263,7 +344,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_rows(NormBwdArgs a, int tpr)
 #pragma unroll
             for (int j = 0; j < N; j++) {
                 const float d = (float)rd[i][j], u = ((float)rx[i][j] - mean) * rstd;
-                v[j] = (T)(rstd * (d * wv[i][j] - s1 - u * s2));
+                v[j] = (T)(rstd * (d * wv[i][j] - c1 - u * c2));
             }
             store_pack<T>(dxr + c, cols - c, v);
         }
@@ -271,52 +352,79 @@ __global__ __launch_bounds__(1024) void norm_bwd_rows(NormBwdArgs a, int tpr)
     if (!a.dw && !a.db)
         return;
     float *part = a.ws + (size_t)blockIdx.x * 2 * cols;
+    const auto put = [&](int k, int c, float v) {
+        TW *out = (TW *)(k ? a.db : a.dw);
+        if (gridDim.x > 1)
+            part[(size_t)k * cols + c] = v;
+        else if (out)
+            out[c] = (TW)v;
+    };
 #pragma unroll
     for (int k = 0; k < 2; k++) {
-        __syncthreads();
+        if (groups > 1)
+            __syncthreads();
 #pragma unroll
         for (int i = 0; i < NV; i++)
 #pragma unroll
-            for (int j = 0; j < N; j++)
-                lds[(group * tpr * NV + t + i * tpr) * N + j] = k ? sb[i][j] : sw[i][j];
+            for (int j = 0; j < N; j++) {
+                const int c = (t + i * tpr) * N + j;
+                const float v = k ? sb[i][j] : sw[i][j];
+                if (groups > 1)
+                    lds[group * tpr * NV * N + c] = v;
+                else if (c < cols)
+                    put(k, c, v);
+            }
+        if (groups == 1)
+            continue;
         __syncthreads();
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
-            float s = lds[c];
+            float v = lds[c];
             for (int g = 1; g < groups; g++)
-                s += lds[g * tpr * NV * N + c];
-            part[(size_t)k * cols + c] = s;
+                v += lds[g * tpr * NV * N + c];
+            put(k, c, v);
         }
     }
 }
 
-// parts[n][2][cols] summed into dw and db: 64 columns a workgroup, each wave
-// every fourth part.
+// parts[n][2][cols] summed into dw and db: 32 columns a workgroup, its
+// half-waves every 32nd part, eight loads in flight.
 template <class TW>
-__global__ __launch_bounds__(256) void norm_bwd_sum(const float *parts, int n, long long cols,
-                                                    TW *dw, TW *db)
+__global__ __launch_bounds__(1024) void norm_bwd_sum(const float *parts, int n, long long cols,
+                                                     TW *dw, TW *db)
 {
-    __shared__ float lds[4][64];
+    __shared__ float lds[32][33];
     const int k = blockIdx.y;
     TW *out = k ? db : dw;
     if (!out)
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long c = (long long)blockIdx.x * 64 + lane;
+    const int lane = threadIdx.x & 31, half = threadIdx.x >> 5;
+    const long long c = (long long)blockIdx.x * 32 + lane;
+    const float *in = parts + (size_t)k * cols + c;
     float s = 0.f;
     if (c < cols)
-        for (int p = wave; p < n; p += 4)
-            s += parts[((size_t)p * 2 + k) * cols + c];
-    lds[wave][lane] = s;
+        for (int p = half; p < n; p += 256) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                v[i] = p + 32 * i < n ? in[(size_t)(p + 32 * i) * 2 * cols] : 0.f;
+            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
+    lds[half][lane] = s;
     __syncthreads();
-    if (wave == 0 && c < cols)
-        out[c] = (TW)(lds[0][lane] + lds[1][lane] + (lds[2][lane] + lds[3][lane]));
+    // Half-wave h of the transposed block: the 32 sums of column h.
+    s = lds[lane][half];
+    s = wave_reduce(s, 32, Add());
+    const long long col = (long long)blockIdx.x * 32 + half;
+    if (lane == 0 && col < cols)
+        out[col] = (TW)s;
 }
 
-// Long rows: sums of g and g u of each piece to sums[row][split][2].
+// Long rows: sums of g and g u of each piece to sums[row][split][2], four packs
+// of x and dy in flight a thread.
 template <class T, class TW>
 __global__ __launch_bounds__(256) void norm_bwd_pieces(NormBwdArgs a, long long piece, int splits)
 {
-    constexpr int N = Pack<T>::N;
+    constexpr int N = Pack<T>::N, F = 4;
     __shared__ float red[2][4];
     const long long row = blockIdx.x / splits;
     const int split = (int)(blockIdx.x - row * splits);
@@ -327,16 +435,28 @@ __global__ __launch_bounds__(256) void norm_bwd_pieces(NormBwdArgs a, long long 
     const TW *w = (const TW *)a.w;
     const float mean = a.mean[row], rstd = a.rstd[row];
     float s1 = 0.f, s2 = 0.f;
-    for (long long c = first + threadIdx.x * N; c < end; c += 256 * N) {
-        const int left = (int)min((long long)N, end - c);
-        const auto rx = load_pack<T>(xr + c, left, (T)0.f);
-        const auto rd = load_pack<T>(dyr + c, left, (T)0.f);
+    for (long long c0 = first + threadIdx.x * N; c0 < end; c0 += F * 256 * N) {
+        typename Pack<T>::V rx[F], rd[F];
+        float wv[F][N];
 #pragma unroll
-        for (int j = 0; j < N; j++) {
-            const float g = j < left ? (w ? (float)rd[j] * (float)w[c + j] : (float)rd[j]) : 0.f;
-            s1 += g;
-            s2 += j < left ? g * (((float)rx[j] - mean) * rstd) : 0.f;
+        for (int i = 0; i < F; i++) {
+            const long long c = c0 + i * 256 * N;
+            rx[i] = rd[i] = typename Pack<T>::V{};
+            if (c < end) {
+                rx[i] = load_pack<T>(xr + c, a.cols - c, (T)0.f);
+                rd[i] = load_pack<T>(dyr + c, a.cols - c, (T)0.f);
+            }
+            load_weights<N>(w, c, end, 1.f, wv[i]);
         }
+#pragma unroll
+        for (int i = 0; i < F; i++)
+#pragma unroll
+            for (int j = 0; j < N; j++) {
+                const bool in = c0 + i * 256 * N + j < end;
+                const float g = in ? (float)rd[i][j] * wv[i][j] : 0.f;
+                s1 += g;
+                s2 += in ? g * (((float)rx[i][j] - mean) * rstd) : 0.f;
+            }
     }
     s1 = group_reduce(s1, 256, red[0], Add());
     s2 = group_reduce(s2, 256, red[1], Add());
@@ -347,53 +467,89 @@ __global__ __launch_bounds__(256) void norm_bwd_pieces(NormBwdArgs a, long long 
     }
 }
 
-// Long rows: a workgroup owns 64 packs of columns, its waves rows of the
-// chunk of rows blockIdx.y: dx, and the columns' shares of dw and db, to
-// parts[chunk][2][cols].
+// Long rows: a workgroup owns 64 packs of columns and the chunk of rows
+// blockIdx.y, of which its eight waves take every eighth: dx, and the columns'
+// shares of dw and db, to parts[chunk][2][cols], or to dw and db if there is
+// one chunk only.  The rows' sums are joined in LDS, kJoin rows at a time.
+constexpr int kJoin = 64;
+
 template <class T, class TW>
-__global__ __launch_bounds__(256) void norm_bwd_cols(NormBwdArgs a, int splits, long long chunk,
+__global__ __launch_bounds__(512) void norm_bwd_cols(NormBwdArgs a, int splits, long long chunk,
                                                      float *parts)
 {
-    constexpr int N = Pack<T>::N;
-    __shared__ float lds[4][2][64 * N];
+    constexpr int N = Pack<T>::N, F = 2;
+    __shared__ float lds[8][2][64 * N];
+    __shared__ float join[kJoin][2];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long c = ((long long)blockIdx.x * 64 + lane) * N;
     const long long end = min((long long)(blockIdx.y + 1) * chunk, a.rows);
     const int left = (int)max(0LL, min((long long)N, a.cols - c));
-    const TW *w = (const TW *)a.w;
     const float inv_n = 1.f / (float)a.cols;
     float wv[N], sw[N], sb[N];
+    load_weights<N>((const TW *)a.w, c, a.cols, 1.f, wv);
 #pragma unroll
-    for (int j = 0; j < N; j++) {
-        wv[j] = j < left ? (w ? (float)w[c + j] : 1.f) : 0.f;
+    for (int j = 0; j < N; j++)
         sw[j] = sb[j] = 0.f;
-    }
-    for (long long row = blockIdx.y * chunk + wave; row < end; row += 4) {
-        const float mean = a.mean[row], rstd = a.rstd[row];
-        float s1 = 0.f, s2 = 0.f;
+    for (long long base = blockIdx.y * chunk; base < end; base += kJoin) {
+        const int here = (int)min((long long)kJoin, end - base);
         if (a.dx.p) {
-            const float *sums = a.ws + (size_t)row * splits * 2;
-            for (int i = 0; i < splits; i++) {
-                s1 += sums[2 * i];
-                s2 += sums[2 * i + 1];
+            // Eight threads a row.
+            const int r = threadIdx.x >> 3, part = threadIdx.x & 7;
+            float s1 = 0.f, s2 = 0.f;
+            if (r < here) {
+                const float2 *sums = (const float2 *)a.ws + (size_t)(base + r) * splits;
+                for (int i = part; i < splits; i += 8) {
+                    const float2 v = sums[i];
+                    s1 += v.x;
+                    s2 += v.y;
+                }
             }
-            s1 *= inv_n;
-            s2 *= inv_n;
+            s1 = wave_reduce(s1, 8, Add());
+            s2 = wave_reduce(s2, 8, Add());
+            __syncthreads();
+            if (part == 0) {
+                join[r][0] = s1 * inv_n;
+                join[r][1] = s2 * inv_n;
+            }
+            __syncthreads();
         }
         if (!left)
             continue;
-        const auto rx = load_pack<T>((const T *)a.x.p + row * a.x.ld + c, left, (T)0.f);
-        const auto rd = load_pack<T>((const T *)a.dy.p + row * a.dy.ld + c, left, (T)0.f);
-        typename Pack<T>::V v;
+        for (int r0 = wave; r0 < here; r0 += 8 * F) {
+            typename Pack<T>::V rx[F], rd[F];
+            float mean[F], rstd[F];
 #pragma unroll
-        for (int j = 0; j < N; j++) {
-            const float d = (float)rd[j], u = ((float)rx[j] - mean) * rstd;
-            sw[j] += d * u;
-            sb[j] += d;
-            v[j] = (T)(rstd * (d * wv[j] - s1 - u * s2));
+            for (int i = 0; i < F; i++) {
+                const int r = r0 + 8 * i;
+                rx[i] = rd[i] = typename Pack<T>::V{};
+                mean[i] = rstd[i] = 0.f;
+                if (r < here) {
+                    const long long row = base + r;
+                    mean[i] = a.mean[row];
+                    rstd[i] = a.rstd[row];
+                    rx[i] = load_pack<T>((const T *)a.x.p + row * a.x.ld + c, left, (T)0.f);
+                    rd[i] = load_pack<T>((const T *)a.dy.p + row * a.dy.ld + c, left, (T)0.f);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < F; i++) {
+                const int r = r0 + 8 * i;
+                if (r >= here)
+                    continue;
+                const float s1 = a.dx.p ? join[r][0] : 0.f, s2 = a.dx.p ? join[r][1] : 0.f;
+                typename Pack<T>::V v;
+#pragma unroll
+                for (int j = 0; j < N; j++) {
+                    const float d = (float)rd[i][j];
+                    const float u = ((float)rx[i][j] - mean[i]) * rstd[i];
+                    sw[j] += d * u;
+                    sb[j] += d;
+                    v[j] = (T)(rstd[i] * (d * wv[j] - s1 - u * s2));
+                }
+                if (a.dx.p)
+                    store_pack<T>((T *)a.dx.p + (base + r) * a.dx.ld + c, left, v);
+            }
         }
-        if (a.dx.p)
-            store_pack<T>((T *)a.dx.p + row * a.dx.ld + c, left, v);
     }
     if (!a.dw && !a.db)
         return;
@@ -404,52 +560,117 @@ __global__ __launch_bounds__(256) void norm_bwd_cols(NormBwdArgs a, int splits, 
     }
     __syncthreads();
     float *part = parts + (size_t)blockIdx.y * 2 * a.cols;
-    for (int i = threadIdx.x; i < 2 * 64 * N; i += 256) {
+    for (int i = threadIdx.x; i < 2 * 64 * N; i += 512) {
         const int k = i / (64 * N), j = i - k * 64 * N;
         const long long col = (long long)blockIdx.x * 64 * N + j;
-        if (col < a.cols)
-            part[(size_t)k * a.cols + col] =
-                lds[0][k][j] + lds[1][k][j] + (lds[2][k][j] + lds[3][k][j]);
+        if (col >= a.cols)
+            continue;
+        float s = lds[0][k][j];
+#pragma unroll
+        for (int v = 1; v < 8; v++)
+            s += lds[v][k][j];
+        TW *out = (TW *)(k ? a.db : a.dw);
+        if (gridDim.y > 1)
+            part[(size_t)k * a.cols + col] = s;
+        else if (out)
+            out[col] = (TW)s;
     }
 }
 
 // ----------------------------------------------------------------- launch rules
-int elem_size(int xtype) { return xtype == 0 ? 4 : 2; }
+int pack_of(int xtype) { return xtype == 0 ? 4 : 8; }
 
 size_t up16(size_t v) { return (v + 15) / 16 * 16; }
 
-// Threads a row and packs a thread of the register kernels; nv = 0: the row
-// is too long for them.
+// A thread's elements of a row, at most: kValues with weights (and, backward,
+// their gradients) in registers beside them; forward rows too long for that
+// twice as many without.
+constexpr int kValues = 16;
+
+// Threads a row, packs a thread and threads a workgroup of the register
+// kernels; nv = 0: the row is too long for them.
 struct RowPlan {
     int tpr, nv, block;
 };
 
-RowPlan row_plan(int xtype, long long cols, int max_values)
+RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
 {
-    const int n = 16 / elem_size(xtype);
+    const int n = pack_of(xtype);
     const long long packs = (cols + n - 1) / n;
-    int tpr = 1;
-    while (tpr < 1024 && packs > tpr)
-        tpr *= 2;
-    // Up to a wave, one pack a thread; then more packs a thread before more
-    // threads, as a row inside a wave needs no barrier.
-    int nv = 1;
-    while (tpr > 64 && nv * 2 * n <= max_values) {
-        tpr /= 2;
-        nv *= 2;
+    if (forward && cols > 16384 && rows <= 64)
+        return RowPlan{0, 0, 0};
+    if (!forward && (cols > 8192 || (cols >= 4096 && rows <= (n == 4 ? cols / 128 : 1024))))
+        return RowPlan{0, 0, 0};
+    if (packs <= 64) {
+        int tpr = 1;
+        while (packs > tpr)
+            tpr *= 2;
+        return RowPlan{tpr, 1, 256};
     }
-    if (tpr > 1024 || (long long)tpr * nv < packs) {
-        tpr = 1024;
-        nv = 1;
-        while (nv * n < max_values && (long long)tpr * nv < packs)
-            nv *= 2;
-        if ((long long)tpr * nv < packs)
+    // As few idle places as can be; then more packs a thread before more
+    // threads, as a row inside a wave needs no barrier.  Few rows are spread
+    // over more threads.
+    const auto waves = [&](int nv) { return (packs + 64 * nv - 1) / (64 * nv); };
+    const auto idle = [&](int nv) {
+        const long long w = waves(nv);
+        return w * nv + (!forward && (w == 2 || w == 3));  // small workgroups: many sums to join
+    };
+    const int most = forward ? 16 : 8;  // waves of a workgroup
+    int best = 0;
+    for (int nv = 1; nv * n <= kValues; nv++) {
+        if (waves(nv) > most)
+            continue;
+        if (!best || (idle(nv) <= idle(best) && (!forward || rows * waves(nv) > 8LL * num_cus())))
+            best = nv;
+    }
+    if (!best) {
+        best = 2 * kValues / n;
+        if (!forward || waves(best) > most)
             return RowPlan{0, 0, 0};
     }
-    return RowPlan{tpr, nv, tpr > 64 ? tpr : 256};
+    const int tpr = 64 * (int)waves(best);
+    return RowPlan{tpr, best, tpr > 64 ? tpr : 256};
 }
 
-constexpr int kFwdValues = 32, kBwdValues = 16;  // a thread's elements of a row, at most
+// Workgroups of the register kernels.  Forward: 1536 threads a CU (16384 rows
+// of 4096 bf16: 51.6 us; with 1024, 2048 and 4096 threads 52.9, 57.8 and 53.5).
+int fwd_blocks(const RowPlan &p, long long rows)
+{
+    const long long groups = std::max(1, p.block / p.tpr);
+    return (int)std::min((rows + groups - 1) / groups, 1536LL / p.block * num_cus());
+}
+
+// Backward: each workgroup adds 2 x cols partial sums to write and to read
+// again, so 512 threads a CU (16384 x 4096 bf16: 83.7 us; with 768 and 1024
+// 92.5 and 102.4); 1024 where a thread holds one pack, too little in flight,
+// and takes at least five rows (31000 x 1700 bf16: 101 us instead of 149;
+// 3000 x 1500, three rows: 26.6 instead of 22.6).  A single workgroup, which
+// needs no sum after it, takes up to two rows a group (7 x 1024 bf16: 8.6 us
+// instead of 9.8).
+int bwd_blocks(const RowPlan &p, long long rows)
+{
+    const long long groups = std::max(1, p.block / p.tpr);
+    if (rows <= 2 * groups)
+        return 1;
+    const auto blocks = [&](int threads) {
+        return (long long)std::max(1, threads / p.block) * num_cus();
+    };
+    const bool more = p.nv == 1 && rows >= 5 * groups * blocks(1024);
+    return (int)std::min((rows + groups - 1) / groups, blocks(more ? 1024 : 512));
+}
+
+// Loads that leave nothing in the caches, for inputs larger than the last-level
+// one holds beside the rest (from 100 MB on: 16384 x 4096 bf16 49.2 us instead
+// of 51.4 forward, 83.5 instead of 86.7 backward; 9000 x 4096 26.7 with them 29.6),
+// of whole cache lines (31000 x 1700 bf16, lines shared by rows: 48.9 with them,
+// 45.6 without).
+bool streams(long long rows, long long cols, size_t elem, std::initializer_list<Rows> in)
+{
+    bool lines = rows * cols * (long long)elem > 100LL << 20;
+    for (const Rows &r : in)
+        lines = lines && (uintptr_t)r.p % 128 == 0 && r.ld * elem % 128 == 0;
+    return lines;
+}
 
 // Pieces of long rows: as many as give every CU four workgroups, of at least
 // 4096 elements, at most 64 a row.
@@ -458,106 +679,109 @@ struct PiecePlan {
     int splits;
 };
 
-PiecePlan piece_plan(long long rows, long long cols)
+PiecePlan piece_plan(long long rows, long long cols, bool forward)
 {
-    const long long want = std::max(1LL, 4LL * num_cus() / std::max(1LL, rows));
-    const long long most = std::min(64LL, std::max(1LL, cols / 4096));
+    const long long per_cu = forward ? 8 : 4, least = forward ? 2048 : 4096;
+    const long long want = std::max(1LL, per_cu * num_cus() / std::max(1LL, rows));
+    const long long most = std::min((long long)kPieces, std::max(1LL, cols / least));
     const long long splits = std::min(want, most);
     const long long piece = ((cols + splits - 1) / splits + 2047) / 2048 * 2048;
     return PiecePlan{piece, (int)((cols + piece - 1) / piece)};
 }
 
-int bwd_blocks(const RowPlan &p, long long rows)
-{
-    const long long groups = p.block / p.tpr;
-    return (int)std::min((rows + groups - 1) / groups, 2LL * num_cus());
-}
-
-// Chunks of rows of norm_bwd_cols.
+// Chunks of rows of norm_bwd_cols: one for up to 64 rows, which then needs no
+// sum over the chunks; else as many as give every CU two workgroups.
 int row_chunks(int xtype, long long rows, long long cols)
 {
-    const int n = 16 / elem_size(xtype);
+    const int n = pack_of(xtype);
     const long long tiles = (cols + 64 * n - 1) / (64 * n);
-    const long long want = std::max(1LL, 4LL * num_cus() / tiles);
-    return (int)std::max(1LL, std::min(want, (rows + 15) / 16));
+    const long long want = std::max(1LL, 2LL * num_cus() / tiles);
+    return (int)std::max(1LL, std::min(want, rows / 64));
+}
+
+template <class T, class TW, int NV, bool HOLD>
+void fwd_rows(const NormFwdArgs &a, const RowPlan &p, hipStream_t stream)
+{
+    const int n = fwd_blocks(p, a.rows);
+    const bool through = streams(a.rows, a.cols, sizeof(T), {a.x});
+    if (p.block <= 256)
+        norm_fwd_rows<T, TW, NV, HOLD, 256><<<n, p.block, 0, stream>>>(a, p.tpr, through);
+    else
+        norm_fwd_rows<T, TW, NV, HOLD, 1024><<<n, p.block, 0, stream>>>(a, p.tpr, through);
 }
 
 template <class T, class TW>
 hipError_t fwd(int xtype, const NormFwdArgs &a, hipStream_t stream)
 {
-    const RowPlan p = row_plan(xtype, a.cols, kFwdValues);
-    if (p.nv) {
-        const long long groups = p.block / p.tpr, most = kMaxBlocks * groups;
-        for (long long first = 0; first < a.rows; first += most) {
-            NormFwdArgs c = a;  // the rows of this launch
-            c.rows = std::min(most, a.rows - first);
-            c.x.p = (const T *)a.x.p + first * a.x.ld;
-            c.y.p = (const T *)a.y.p + first * a.y.ld;
-            c.mean = a.mean ? a.mean + first : nullptr;
-            c.rstd = a.rstd ? a.rstd + first : nullptr;
-            const dim3 grid((unsigned)((c.rows + groups - 1) / groups));
-            switch (p.nv) {
-            case 1: norm_fwd_rows<T, TW, 1><<<grid, p.block, 0, stream>>>(c, p.tpr); break;
-            case 2: norm_fwd_rows<T, TW, 2><<<grid, p.block, 0, stream>>>(c, p.tpr); break;
-            case 4: norm_fwd_rows<T, TW, 4><<<grid, p.block, 0, stream>>>(c, p.tpr); break;
-            default:
-                norm_fwd_rows<T, TW, kFwdValues / Pack<T>::N>
-                    <<<grid, p.block, 0, stream>>>(c, p.tpr);
-                break;
-            }
-        }
-        return hipGetLastError();
-    }
+    constexpr int N = Pack<T>::N;
     if (!a.rows)
         return hipSuccess;
+    const RowPlan p = row_plan(xtype, a.rows, a.cols, true);
+    if (p.nv == 1)
+        fwd_rows<T, TW, 1, true>(a, p, stream);
+    else if (p.nv == 2)
+        fwd_rows<T, TW, 2, true>(a, p, stream);
+    else if (p.nv == 3 && N == 4)
+        fwd_rows<T, TW, N == 4 ? 3 : 1, true>(a, p, stream);
+    else if (p.nv == 4 && N == 4)
+        fwd_rows<T, TW, kValues / N, true>(a, p, stream);
+    else if (p.nv)
+        fwd_rows<T, TW, 2 * kValues / N, false>(a, p, stream);
+    if (p.nv)
+        return hipGetLastError();
     // rows * cols is below 2^37 and a row above 2^15: below 2^23 workgroups.
-    const PiecePlan s = piece_plan(a.rows, a.cols);
+    const PiecePlan s = piece_plan(a.rows, a.cols, true);
     const dim3 grid((unsigned)(a.rows * s.splits));
     norm_fwd_pieces<T><<<grid, 256, 0, stream>>>(a, s.piece, s.splits);
     norm_fwd_apply<T, TW><<<grid, 256, 0, stream>>>(a, s.piece, s.splits);
     return hipGetLastError();
 }
 
+template <class T, class TW, int NV>
+void bwd_rows(const NormBwdArgs &a, const RowPlan &p, int n, hipStream_t stream)
+{
+    const size_t lds =
+        p.block > p.tpr ? (size_t)p.block * NV * Pack<T>::N * sizeof(float) : 0;
+    const bool through = streams(a.rows, a.cols, sizeof(T), {a.x, a.dy});
+    if (p.block <= 256)
+        norm_bwd_rows<T, TW, NV, 256><<<n, p.block, lds, stream>>>(a, p.tpr, through);
+    else
+        norm_bwd_rows<T, TW, NV, 512><<<n, p.block, lds, stream>>>(a, p.tpr, through);
+}
+
 template <class T, class TW>
 hipError_t bwd(int xtype, const NormBwdArgs &a, hipStream_t stream)
 {
-    const RowPlan p = row_plan(xtype, a.cols, kBwdValues);
-    const bool params = a.dw || a.db;
-    const float *parts;
-    int n;
-    if (p.nv) {
-        constexpr int N = Pack<T>::N;
+    constexpr int N = Pack<T>::N;
+    const RowPlan p = row_plan(xtype, a.rows, a.cols, false);
+    const float *parts = a.ws;
+    int n = 0;
+    if (a.rows && p.nv) {
         n = bwd_blocks(p, a.rows);
-        parts = a.ws;
-        if (n) {
-            const size_t lds = params ? (size_t)p.block * p.nv * N * sizeof(float) : 0;
-            switch (p.nv) {
-            case 1: norm_bwd_rows<T, TW, 1><<<n, p.block, lds, stream>>>(a, p.tpr); break;
-            case 2: norm_bwd_rows<T, TW, 2><<<n, p.block, lds, stream>>>(a, p.tpr); break;
-            default:
-                norm_bwd_rows<T, TW, 16 / N><<<n, p.block, lds, stream>>>(a, p.tpr);
-                break;
-            }
-        }
-    } else {
-        const PiecePlan s = piece_plan(a.rows, a.cols);
-        n = a.rows ? row_chunks(xtype, a.rows, a.cols) : 0;
-        const size_t sums = up16((size_t)a.rows * s.splits * 2 * sizeof(float));
-        float *out = (float *)((char *)a.ws + sums);
+        if (p.nv == 1)
+            bwd_rows<T, TW, 1>(a, p, n, stream);
+        else if (p.nv == 2)
+            bwd_rows<T, TW, 2>(a, p, n, stream);
+        else if (p.nv == 3)
+            bwd_rows<T, TW, N == 4 ? 3 : 1>(a, p, n, stream);
+        else
+            bwd_rows<T, TW, kValues / N>(a, p, n, stream);
+    } else if (a.rows) {
+        const PiecePlan s = piece_plan(a.rows, a.cols, false);
+        n = row_chunks(xtype, a.rows, a.cols);
+        float *out = (float *)((char *)a.ws +
+                               up16((size_t)a.rows * s.splits * 2 * sizeof(float)));
         parts = out;
-        if (a.rows && a.dx.p)
+        if (a.dx.p)
             norm_bwd_pieces<T, TW><<<(unsigned)(a.rows * s.splits), 256, 0, stream>>>(
                 a, s.piece, s.splits);
-        if (a.rows) {
-            const long long cols_wg = 64 * Pack<T>::N;
-            const dim3 grid((unsigned)((a.cols + cols_wg - 1) / cols_wg), n);
-            const long long chunk = (a.rows + n - 1) / n;
-            norm_bwd_cols<T, TW><<<grid, 256, 0, stream>>>(a, s.splits, chunk, out);
-        }
+        const dim3 grid((unsigned)((a.cols + 64 * N - 1) / (64 * N)), n);
+        norm_bwd_cols<T, TW><<<grid, 512, 0, stream>>>(a, s.splits, (a.rows + n - 1) / n, out);
     }
-    if (params) {
-        const dim3 grid((unsigned)((a.cols + 63) / 64), 2);
-        norm_bwd_sum<TW><<<grid, 256, 0, stream>>>(parts, n, a.cols, (TW *)a.dw, (TW *)a.db);
+    // One workgroup (or chunk) has written them itself; without rows they are 0.
+    if (n != 1 && (a.dw || a.db)) {
+        const dim3 grid((unsigned)((a.cols + 31) / 32), 2);
+        norm_bwd_sum<TW><<<grid, 1024, 0, stream>>>(parts, n, a.cols, (TW *)a.dw, (TW *)a.db);
     }
     return hipGetLastError();
 }
@@ -566,18 +790,19 @@ hipError_t bwd(int xtype, const NormBwdArgs &a, hipStream_t stream)
 
 size_t norm_fwd_ws(int xtype, long long rows, long long cols)
 {
-    if (row_plan(xtype, cols, kFwdValues).nv)
+    if (row_plan(xtype, rows, cols, true).nv)
         return 0;
-    return (size_t)rows * piece_plan(rows, cols).splits * sizeof(Moments);
+    return (size_t)rows * piece_plan(rows, cols, true).splits * sizeof(Moments);
 }
 
 size_t norm_bwd_ws(int xtype, long long rows, long long cols)
 {
-    const RowPlan p = row_plan(xtype, cols, kBwdValues);
+    const RowPlan p = row_plan(xtype, rows, cols, false);
+    const size_t part = 2 * (size_t)cols * sizeof(float);
     if (p.nv)
-        return (size_t)bwd_blocks(p, rows) * 2 * cols * sizeof(float);
-    return up16((size_t)rows * piece_plan(rows, cols).splits * 2 * sizeof(float)) +
-           (size_t)row_chunks(xtype, rows, cols) * 2 * cols * sizeof(float);
+        return bwd_blocks(p, rows) * part;
+    return up16((size_t)rows * piece_plan(rows, cols, false).splits * 2 * sizeof(float)) +
+           row_chunks(xtype, rows, cols) * part;
 }
 
 hipError_t launch_norm_fwd(int xtype, bool w32, const NormFwdArgs &a, hipStream_t stream)

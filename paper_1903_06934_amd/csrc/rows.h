@@ -22,12 +22,13 @@ struct Pack {
 
 // The N elements at p of which the first `left` (>= 1) are in the row; the
 // others are `fill`.
-template <class T>
+template <class T, bool STREAM = false>
 __device__ __forceinline__ typename Pack<T>::V load_pack(const T *p, long long left, T fill)
 {
     typename Pack<T>::V v;
     if (left >= Pack<T>::N) {
-        v = *(const typename Pack<T>::At *)p;
+        const auto *at = (const typename Pack<T>::At *)p;
+        v = STREAM ? __builtin_nontemporal_load(at) : *at;
     } else {
 #pragma unroll
         for (int i = 0; i < Pack<T>::N; i++)
@@ -40,7 +41,7 @@ template <class T>
 __device__ __forceinline__ void store_pack(T *p, long long left, typename Pack<T>::V v)
 {
     if (left >= Pack<T>::N) {
-        *(typename Pack<T>::At *)p = v;
+        __builtin_nontemporal_store(v, (typename Pack<T>::At *)p);
     } else {
 #pragma unroll
         for (int i = 0; i < Pack<T>::N; i++)
@@ -50,7 +51,7 @@ __device__ __forceinline__ void store_pack(T *p, long long left, typename Pack<T
 }
 
 // Sum (or maximum) over the `width` threads of a group, in a fixed order; every
-// thread of the group gets it.  width is a power of two: up to 64 lanes of a
+// thread of the group gets it.  width is a power of two up to the 64 lanes of a
 // wave, or the whole workgroup, whose waves then meet in `lds` (one value a
 // wave; the caller takes another part of it for the next reduction, so that one
 // barrier is enough).
@@ -61,11 +62,37 @@ struct Max {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 
+// Within a wave without LDS: lanes of 4, 8 and 16 exchange by DPP (quad_perm,
+// row_half_mirror, row_mirror: after each step its two partners hold their
+// halves' results), rows of 16 and halves of 32 by swaps.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v)
+{
+    return __int_as_float(
+        __builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
 template <class Op>
 __device__ __forceinline__ float wave_reduce(float v, int width, Op op)
 {
-    for (int o = 1; o < width && o < 64; o <<= 1)
-        v = op(v, __shfl_xor(v, o));
+    if (width > 1)
+        v = op(v, dpp<0xb1>(v));
+    if (width > 2)
+        v = op(v, dpp<0x4e>(v));
+    if (width > 4)
+        v = op(v, dpp<0x141>(v));
+    if (width > 8)
+        v = op(v, dpp<0x140>(v));
+    if (width > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v),
+                                                        false, false);
+        v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (width > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v),
+                                                        false, false);
+        v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
     return v;
 }
 

@@ -105,6 +105,29 @@ def test_layernorm(cols, xt, wt):
     assert only[1] is None and torch.equal(only[0], dx)
 
 
+@pytest.mark.parametrize("xt", [F32, BF16])
+@pytest.mark.parametrize("rows", [9, 130, 1030])
+def test_layernorm_row_lengths(rows, xt):
+    """Many row lengths: every share of a row among threads and packs."""
+    import paper_1903_06934_amd as m
+    g = gen(rows, 9)
+    lengths = torch.randint(1, 9000, (24,), generator=g).tolist() + [4500, 6500, 8192, 8193]
+    for cols in lengths if rows < 1000 else lengths[:4] + [5000, 3000, 1700]:
+        x, dy = randn(g, rows, cols).to(xt), randn(g, rows, cols).to(xt)
+        w = randn(g, cols).to(xt)
+        y, mean, rstd = m.layernorm_fwd(x.cuda(), w.cuda())
+        ry, rmean, rrstd, size, msize = ref.layernorm_fwd(x, w)
+        k = norm_terms(cols) * U
+        assert_close(mean, rmean, k * msize, f"mean {cols}")
+        assert_close(y, ry, 2 * k * size + half_ulp(ry, xt) * 1.01, f"y {cols}")
+        dx, dw, db = m.layernorm_bwd(dy.cuda(), x.cuda(), mean, rstd, w.cuda())
+        want = ref.layernorm_bwd(dy, x, mean.cpu(), rstd.cpu(), w)
+        assert_close(dx, want[0][0], k * want[0][1] + half_ulp(want[0][0], xt) * 1.01,
+                     f"dx {cols}")
+        for got, (val, mag), name in ((dw, want[1], "dw"), (db, want[2], "db")):
+            assert_close(got, val, 300 * U * mag + half_ulp(val, xt) * 1.01, f"{name} {cols}")
+
+
 @pytest.mark.parametrize("rows", [0, 1, 2, 255, 4097])
 @pytest.mark.parametrize("cols,xt", [(48, BF16), (513, F32), (3000, BF16), (40000, F32)])
 def test_layernorm_rows(rows, cols, xt):
