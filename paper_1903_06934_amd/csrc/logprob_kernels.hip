@@ -11,8 +11,6 @@ namespace miconv {
 
 namespace {
 
-constexpr int kGroups = 128;      // thread groups whose maxima bound the top (>= MITRAIN_TOP_MAX)
-constexpr int kCandidates = 1024; // tokens at or above that bound held in LDS
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInf = __builtin_inff();
 
@@ -32,38 +30,49 @@ struct Soft {
 // (z - m) with banned logits at a finite value, so that their e = 0 makes 0.
 __device__ __forceinline__ float shifted(float z, float m) { return fmaxf(z - m, -1e30f); }
 
-__device__ __forceinline__ Soft merge(Soft a, Soft b, float c)
+// p about the maximum m >= p.m.
+__device__ __forceinline__ Soft about(Soft p, float m, float c)
 {
-    const float m = fmaxf(a.m, b.m);
     if (m == -kInf)
-        return Soft{m, a.s + b.s, a.t + b.t};  // zeros, or NaN
-    const float ua = shifted(a.m, m), ub = shifted(b.m, m);
-    const float ea = exp2_(ua * c), eb = exp2_(ub * c);
-    return Soft{m, a.s * ea + b.s * eb, (a.t + ua * a.s) * ea + (b.t + ub * b.s) * eb};
+        return p;  // sums of zeros, or NaN
+    const float u = shifted(p.m, m), e = exp2_(u * c);
+    return Soft{m, p.s * e, (p.t + u * p.s) * e};
 }
 
-// A finite maximum of nothing but -inf and NaN so far is taken as 0.
-template <class T>
-__device__ __forceinline__ void add_pack(Soft &p, typename Pack<T>::V raw, float c)
+
+// The lanes' parts joined: first the maximum, then each part about it.
+__device__ __forceinline__ Soft wave_merge(Soft p, float c)
+{
+    const float m = wave_reduce(p.m, 64, Max());
+    p = about(p, m, c);
+    return Soft{m, wave_reduce(p.s, 64, Add()), wave_reduce(p.t, 64, Add())};
+}
+
+// F packs' logits.  A maximum of nothing but -inf and NaN so far is taken as 0.
+template <class T, int F>
+__device__ __forceinline__ void add_packs(Soft &p, const typename Pack<T>::V (&raw)[F], float c)
 {
     constexpr int N = Pack<T>::N;
     float m = p.m;
 #pragma unroll
-    for (int j = 0; j < N; j++)
-        m = fmaxf(m, (float)raw[j]);
-    const float base = m == -kInf ? 0.f : m;
-    if (m > p.m) {
-        const float u = shifted(p.m, m), e = exp2_(u * c);
-        p.t = (p.t + u * p.s) * e;
-        p.s *= e;
-        p.m = m;
-    }
+    for (int i = 0; i < F; i++)
 #pragma unroll
-    for (int j = 0; j < N; j++) {
-        const float u = (float)raw[j] - base, e = exp2_(u * c);
-        p.s += e;
-        p.t += fmaxf(u, -1e30f) * e;
-    }
+        for (int j = 0; j < N; j++)
+            m = fmaxf(m, (float)raw[i][j]);
+    if (m > p.m)
+        p = about(p, m, c);
+    const float base = m == -kInf ? 0.f : m;
+    float s = 0.f, t = 0.f;
+#pragma unroll
+    for (int i = 0; i < F; i++)
+#pragma unroll
+        for (int j = 0; j < N; j++) {
+            const float u = (float)raw[i][j] - base, e = exp2_(u * c);
+            s += e;
+            t += fmaxf(u, -1e30f) * e;
+        }
+    p.s += s;
+    p.t += t;
 }
 
 // --------------------------------------------------------------------- the top
@@ -84,133 +93,181 @@ __device__ __forceinline__ uint64_t key(float z, uint32_t index)
     return (uint64_t)order(ranked(z)) << 32 | (0xffffffffu - index);
 }
 
-struct TopShared {
-    float group[kGroups];
-    float bound;
-    int count;
-    int wave[17];
-    uint64_t keys[kCandidates];
+// A row (or piece) is worked on by a team of SIZE threads: a workgroup, or for
+// short rows a wave, four of which share a workgroup and never meet.
+template <int SIZE>
+struct Team {
+    static constexpr int kGroups = SIZE < 128 ? SIZE : 128;  // >= MITRAIN_TOP_MAX
+    static constexpr int kPer = SIZE / kGroups;              // threads a group
+    static constexpr int kWaves = SIZE / 64;
+    static constexpr int kKeys = SIZE < 128 ? 256 : 1024;    // tokens at or above the bound in LDS
+
+    struct Shared {
+        alignas(16) float group[kGroups];
+        Soft soft[kWaves];
+        float bound;
+        int count, nactive;
+        unsigned short active[SIZE];
+        int wave[kWaves];
+        uint64_t keys[kKeys];
+    };
+
+    static __device__ __forceinline__ int thread() { return SIZE == 64 ? threadIdx.x & 63 : threadIdx.x; }
+
+    static __device__ __forceinline__ void sync()
+    {
+        if constexpr (SIZE == 64) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        } else {
+            __syncthreads();
+        }
+    }
+
+    static __device__ __forceinline__ Soft join(Shared &sh, Soft p, float c)
+    {
+        p = wave_merge(p, c);
+        if constexpr (SIZE > 64) {
+            if ((threadIdx.x & 63) == 0)
+                sh.soft[threadIdx.x >> 6] = p;
+            __syncthreads();
+            const int lane = threadIdx.x & 63;
+            p = lane < kWaves ? sh.soft[lane] : Soft{-kInf, 0.f, 0.f};
+            p = wave_merge(p, c);
+        }
+        return p;
+    }
+
+    static __device__ __forceinline__ int sum(Shared &sh, int v)
+    {
+        for (int o = 1; o < 64; o <<= 1)
+            v += __shfl_xor(v, o);
+        if constexpr (SIZE > 64) {
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0)
+                sh.wave[threadIdx.x >> 6] = v;
+            __syncthreads();
+            v = 0;
+            for (int i = 0; i < kWaves; i++)
+                v += sh.wave[i];
+        }
+        return v;
+    }
 };
 
-// The bound: the k-th largest of kGroups group maxima (at least k elements
-// reach it).
-__device__ __forceinline__ float top_bound(TopShared &sh, int k)
+// A lower bound of the k-th largest logit: the k-th largest of the groups'
+// maxima (so at least k elements reach it, and few more where large logits lie
+// anywhere).  mine: the thread's maximum.
+template <class Tm>
+__device__ __forceinline__ float top_bound(typename Tm::Shared &sh, float mine, int k)
 {
-    __syncthreads();
-    if (threadIdx.x < kGroups) {
-        const float mine = sh.group[threadIdx.x];
-        int above = 0;
-        for (int i = 0; i < kGroups; i++) {
-            const float o = sh.group[i];
-            above += o > mine || (o == mine && i < (int)threadIdx.x);
+    const int t = Tm::thread();
+    const float gm = wave_reduce(mine, Tm::kPer, Max());
+    if (t % Tm::kPer == 0)
+        sh.group[t / Tm::kPer] = gm;
+    if (t == 0)
+        sh.count = sh.nactive = 0;
+    Tm::sync();
+    if (t < Tm::kGroups) {
+        const float own = sh.group[t];
+        int above = 0, reach = 0;
+#pragma unroll 8
+        for (int i = 0; i < Tm::kGroups; i += 4) {
+            const float4 o = *(const float4 *)&sh.group[i];
+            above += (o.x > own) + (o.y > own) + (o.z > own) + (o.w > own);
+            reach += (o.x >= own) + (o.y >= own) + (o.z >= own) + (o.w >= own);
         }
-        if (above == k - 1)
-            sh.bound = mine;
+        if (above < k && reach >= k)
+            sh.bound = own;  // one value, whoever has it
     }
-    if (threadIdx.x == 0)
-        sh.count = 0;
-    __syncthreads();
+    Tm::sync();
     return sh.bound;
 }
 
-// Ranks the n <= kCandidates keys and hands key and rank of the first k to put.
+// Ranks n keys in LDS and hands rank and key of the first k to put.
 template <class Put>
-__device__ __forceinline__ void put_ranked(const TopShared &sh, int n, int k, Put put)
+__device__ __forceinline__ void put_ranked(const uint64_t *keys, int n, int k, int thread, int size,
+                                           Put put)
 {
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const uint64_t mine = sh.keys[i];
+    for (int i = thread; i < n; i += size) {
+        const uint64_t mine = keys[i];
         int above = 0;
+#pragma unroll 4
         for (int j = 0; j < n; j++)
-            above += sh.keys[j] > mine;
+            above += keys[j] > mine;
         if (above < k)
             put(above, mine);
     }
 }
 
-// Sum over the workgroup.
-__device__ __forceinline__ int block_count(TopShared &sh, int v)
-{
-    for (int o = 1; o < 64; o <<= 1)
-        v += __shfl_xor(v, o);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0)
-        sh.wave[threadIdx.x >> 6] = v;
-    __syncthreads();
-    int n = 0;
-    for (int i = 0; i < (int)blockDim.x / 64; i++)
-        n += sh.wave[i];
-    return n;
-}
-
 // Elements of z[0, n) above v.
-template <class T>
-__device__ int count_above(TopShared &sh, const T *z, int n, float v)
+template <class T, class Tm, int SIZE>
+__device__ int count_above(typename Tm::Shared &sh, const T *z, int n, float v)
 {
     constexpr int N = Pack<T>::N;
     int c = 0;
-    for (int i = threadIdx.x * N; i < n; i += blockDim.x * N) {
+    for (int i = Tm::thread() * N; i < n; i += SIZE * N) {
         const auto raw = load_pack<T>(z + i, n - i, (T)-kInf);
 #pragma unroll
         for (int j = 0; j < N; j++)
             c += (float)raw[j] > v;
     }
-    return block_count(sh, c);
+    return Tm::sum(sh, c);
 }
 
 // The keys of the top k of z[0, n) where too many elements reach the bound
 // (equal logits, or large ones in few threads): the k-th largest value by
 // bisection, then the elements above it, and of those equal to it the first.
-// Returns their number, k.
-template <class T>
-__device__ int top_by_value(TopShared &sh, const T *z, int n, uint32_t first, int k, float bound,
-                            float most)
+template <class T, class Tm, int SIZE>
+__device__ __noinline__ void top_by_value(typename Tm::Shared &sh, const T *z, int n,
+                                          uint32_t first, int k, float bound, float most)
 {
     constexpr int N = Pack<T>::N;
     uint32_t lo = order(ranked(bound)), hi = order(ranked(most));
-    if (count_above(sh, z, n, bound) < k) {
+    if (count_above<T, Tm, SIZE>(sh, z, n, bound) < k) {
         hi = lo;
     } else {
         while (hi - lo > 1) {
             const uint32_t mid = lo + (hi - lo) / 2;
-            if (count_above(sh, z, n, unorder(mid)) < k)
+            if (count_above<T, Tm, SIZE>(sh, z, n, unorder(mid)) < k)
                 hi = mid;
             else
                 lo = mid;
         }
     }
     const float v = unorder(hi);  // fewer than k elements lie above it, k reach it
-    __syncthreads();
-    if (threadIdx.x == 0)
+    const int t = Tm::thread();
+    Tm::sync();
+    if (t == 0)
         sh.count = 0;
-    __syncthreads();
-    for (int i = threadIdx.x * N; i < n; i += blockDim.x * N) {
+    Tm::sync();
+    for (int i = t * N; i < n; i += SIZE * N) {
         const auto raw = load_pack<T>(z + i, n - i, (T)-kInf);
 #pragma unroll
         for (int j = 0; j < N; j++)
             if ((float)raw[j] > v)
                 sh.keys[atomicAdd(&sh.count, 1)] = key((float)raw[j], first + i + j);
     }
-    __syncthreads();
+    Tm::sync();
     int have = sh.count;
-    for (int base = 0; base < n && have < k; base += blockDim.x) {
-        const int i = base + threadIdx.x;
+    for (int base = 0; base < n && have < k; base += SIZE) {
+        const int i = base + t;
         const bool equal = i < n && ranked((float)z[i]) == v;
         const uint64_t ballot = __ballot(equal);
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        __syncthreads();
+        const int lane = t & 63, wave = t >> 6;
+        Tm::sync();
         if (lane == 0)
             sh.wave[wave] = __popcll(ballot);
-        __syncthreads();
+        Tm::sync();
         int at = have + __popcll(ballot & ((1ull << lane) - 1));
-        for (int w = 0; w < (int)blockDim.x / 64; w++) {
+        for (int w = 0; w < Tm::kWaves; w++) {
             at += w < wave ? sh.wave[w] : 0;
             have += sh.wave[w];
         }
         if (equal && at < k)
             sh.keys[at] = key(v, first + i);
     }
-    __syncthreads();
-    return k;
+    Tm::sync();
 }
 
 // The sums' results.
@@ -233,8 +290,17 @@ __device__ __forceinline__ float log_prob(float z, Soft p, Done d, float scale)
     return (z - p.m) * scale - d.log_s;
 }
 
+// The logit of a row's given token.
 template <class T>
-__device__ __forceinline__ void write_row(const LogprobArgs &a, long long row, Soft p, Done d)
+__device__ __forceinline__ float logit_of(const LogprobArgs &a, long long row, long long token)
+{
+    return token >= 0 && token < a.vocab
+               ? (float)((const T *)a.logits.p)[row * a.logits.ld + token]
+               : 0.f;
+}
+
+__device__ __forceinline__ void write_row(const LogprobArgs &a, long long row, long long token,
+                                          float z, Soft p, Done d)
 {
     if (a.lse)
         a.lse[row] = d.lse;
@@ -245,12 +311,11 @@ __device__ __forceinline__ void write_row(const LogprobArgs &a, long long row, S
         a.stats[2 * row + 1] = d.log_s;
     }
     if (a.logp) {
-        const long long t = a.targets[row];
         float lp = 0.f;
-        if (t >= a.vocab)
+        if (token >= a.vocab)
             lp = __builtin_nanf("");
-        else if (t >= 0)
-            lp = log_prob((float)((const T *)a.logits.p)[row * a.logits.ld + t], p, d, a.scale);
+        else if (token >= 0)
+            lp = log_prob(z, p, d, a.scale);
         a.logp[row] = lp;
     }
 }
@@ -262,157 +327,189 @@ __device__ __forceinline__ void put_top(const LogprobArgs &a, long long row, int
     a.top_logp[row * a.top + rank] = log_prob(unorder((uint32_t)(k >> 32)), p, d, a.scale);
 }
 
-// One workgroup a row, or a piece of it: then the piece's sums and its top go
-// to ws, as parts[row][split] and keys[row][split][top].
-template <class T>
-__global__ __launch_bounds__(1024) void logprob_rows(LogprobArgs a, int piece, int splits,
-                                                     Soft *parts, uint64_t *keys)
+// A team a row, or a piece of it: then the piece's sums and its top go to ws,
+// as parts[row][split] and keys[row][split][top].
+template <class T, int SIZE>
+__global__ __launch_bounds__(SIZE < 256 ? 256 : SIZE) void logprob_rows(LogprobArgs a, int piece,
+                                                                        int splits, bool through,
+                                                                        Soft *parts, uint64_t *keys)
 {
-    constexpr int N = Pack<T>::N;
-    __shared__ Soft waves[16];
-    __shared__ TopShared sh;
-    const long long row = blockIdx.x / splits;
-    const int split = (int)(blockIdx.x - row * splits);
+    using Tm = Team<SIZE>;
+    constexpr int N = Pack<T>::N, F = 2, TEAMS = SIZE < 256 ? 256 / SIZE : 1;
+    __shared__ typename Tm::Shared shared[TEAMS];
+    const int team = TEAMS > 1 ? threadIdx.x / SIZE : 0;
+    typename Tm::Shared &sh = shared[team];
+    const long long item = (long long)blockIdx.x * TEAMS + team;
+    const long long row = splits == 1 ? item : item / splits;
+    if (row >= a.rows)
+        return;
+    const int split = (int)(item - row * splits), t = Tm::thread();
     const int first = split * piece, n = (int)min((long long)piece, a.vocab - first);
     const T *z = (const T *)a.logits.p + row * a.logits.ld + first;
     const float c = a.scale * kLog2e;
+    const long long token = splits == 1 && a.logp ? a.targets[row] : -1;
+    typename Pack<T>::V raw[F];
+    const auto load = [&](int i) {
+#pragma unroll
+        for (int f = 0; f < F; f++) {
+            const int at = i + f * SIZE * N;
+            raw[f] = typename Pack<T>::V((T)-kInf);
+            if (at < n)
+                raw[f] = through ? load_pack<T, true>(z + at, n - at, (T)-kInf)
+                                 : load_pack<T>(z + at, n - at, (T)-kInf);
+        }
+    };
     Soft p{-kInf, 0.f, 0.f};
-    for (int i = threadIdx.x * N; i < n; i += blockDim.x * N)
-        add_pack<T>(p, load_pack<T>(z + i, n - i, (T)-kInf), c);
-    const float mine = p.m;
-    for (int o = 1; o < 64; o <<= 1) {
-        const Soft u{__shfl_xor(p.m, o), __shfl_xor(p.s, o), __shfl_xor(p.t, o)};
-        p = (threadIdx.x & o) ? merge(u, p, c) : merge(p, u, c);
+    for (int i = t * N; i < n; i += F * SIZE * N) {
+        load(i);
+        add_packs<T, F>(p, raw, c);
     }
-    if ((threadIdx.x & 63) == 0)
-        waves[threadIdx.x >> 6] = p;
-    __syncthreads();
-    p = waves[0];
-    for (int i = 1; i < (int)blockDim.x / 64; i++)
-        p = merge(p, waves[i], c);
+    const float zt = logit_of<T>(a, row, token);
+    const float mine = p.m;
+    p = Tm::join(sh, p, c);
     const Done d = finish(p, a.scale);
-    if (threadIdx.x == 0) {
+    if (t == 0) {
         if (splits == 1)
-            write_row<T>(a, row, p, d);
+            write_row(a, row, token, zt, p, d);
         else
-            parts[row * splits + split] = p;
+            parts[item] = p;
     }
     if (!a.top)
         return;
-    // A group's maximum: of blockDim / kGroups neighbouring threads.
-    const int per = blockDim.x / kGroups;
-    const float gm = wave_reduce(mine, per, Max());
-    if (threadIdx.x % per == 0)
-        sh.group[threadIdx.x / per] = gm;
     const int k = min(a.top, n);
-    const float bound = top_bound(sh, k);
-    if (mine >= bound) {
-        for (int i = threadIdx.x * N; i < n; i += blockDim.x * N) {
-            if (*(volatile int *)&sh.count > kCandidates)
-                break;
-            const auto raw = load_pack<T>(z + i, n - i, (T)0.f);
+    const float bound = top_bound<Tm>(sh, mine, k);
+    const auto collect = [&](typename Pack<T>::V v, int i) {
 #pragma unroll
-            for (int j = 0; j < N; j++) {
-                const float f = ranked((float)raw[j]);
-                if (i + j < n && f >= bound) {
-                    const int at = atomicAdd(&sh.count, 1);
-                    if (at < kCandidates)
-                        sh.keys[at] = key(f, first + i + j);
-                }
+        for (int j = 0; j < N; j++) {
+            const float f = ranked((float)v[j]);
+            if (f >= bound && i + j < n) {
+                const int at = atomicAdd(&sh.count, 1);
+                if (at < Tm::kKeys)
+                    sh.keys[at] = key(f, first + i + j);
             }
         }
+    };
+    const int rounds = (n + SIZE * N - 1) / (SIZE * N);  // packs of a thread
+    if (rounds <= F) {  // in its registers still
+        if (mine >= bound)
+#pragma unroll
+            for (int f = 0; f < F; f++)
+                collect(raw[f], (t + f * SIZE) * N);
+    } else {
+        // The packs of the threads that reach the bound, dealt out to all.
+        if (mine >= bound)
+            sh.active[atomicAdd(&sh.nactive, 1)] = t;
+        Tm::sync();
+        const int items = sh.nactive * rounds;
+        for (int i = t; i < items; i += SIZE) {
+            if (*(volatile int *)&sh.count > Tm::kKeys)
+                break;
+            const int at = (sh.active[i / rounds] + i % rounds * SIZE) * N;
+            if (at < n)
+                collect(load_pack<T>(z + at, n - at, (T)0.f), at);
+        }
     }
-    __syncthreads();
+    Tm::sync();
     int found = sh.count;
-    if (found > kCandidates)
-        found = top_by_value<T>(sh, z, n, first, k, bound, p.m);
+    if (found > Tm::kKeys) {
+        top_by_value<T, Tm, SIZE>(sh, z, n, first, k, bound, p.m);
+        found = k;
+    }
     if (splits == 1)
-        put_ranked(sh, found, k, [&](int rank, uint64_t ky) { put_top(a, row, rank, ky, p, d); });
+        put_ranked(sh.keys, found, k, t, SIZE,
+                   [&](int rank, uint64_t ky) { put_top(a, row, rank, ky, p, d); });
     else
-        put_ranked(sh, found, k, [&](int rank, uint64_t ky) {
-            keys[(row * splits + split) * a.top + rank] = ky;
-        });
+        put_ranked(sh.keys, found, k, t, SIZE,
+                   [&](int rank, uint64_t ky) { keys[item * a.top + rank] = ky; });
 }
 
-// Joins the pieces of a row.
+// Joins the pieces (two at least, at most kPieces) of a row.  Each has sorted
+// keys; all but the last have `top` of them.  A bound as above: the top-th of
+// the first q keys of each piece, q the fewest that make `top` of them.
+constexpr int kPieces = 64;
+
 template <class T>
 __global__ __launch_bounds__(256) void logprob_join(LogprobArgs a, int piece, int splits,
                                                     const Soft *parts, const uint64_t *keys)
 {
+    __shared__ uint64_t heads[256], found[kPieces * 64];
+    __shared__ uint64_t bound;
+    __shared__ int count;
     const long long row = blockIdx.x;
+    const int lane = threadIdx.x & 63, top = a.top;
     const float c = a.scale * kLog2e;
-    Soft p = parts[row * splits];
-    for (int i = 1; i < splits; i++)
-        p = merge(p, parts[row * splits + i], c);
+    const long long token = a.logp ? a.targets[row] : -1;
+    Soft p{-kInf, 0.f, 0.f};
+    if (lane < splits)
+        p = parts[row * splits + lane];
+    const int last = (int)min((long long)top, a.vocab - (long long)(splits - 1) * piece);
+    const int q = (top + splits - 2) / (splits - 1);
+    const int nheads = (splits - 1) * q + min(q, last);
+    const uint64_t *list = keys + row * splits * top;
+    // heads[i]: key i % q of piece i / q.  q (splits - 1) < top + splits, so all
+    // of them are fewer than 64 + 2 * 64.
+    if ((int)threadIdx.x < nheads)
+        heads[threadIdx.x] = list[threadIdx.x / max(q, 1) * top + threadIdx.x % max(q, 1)];
+    if (threadIdx.x == 0)
+        count = 0;
+    const float zt = logit_of<T>(a, row, token);
+    p = wave_merge(p, c);
     const Done d = finish(p, a.scale);
     if (threadIdx.x == 0)
-        write_row<T>(a, row, p, d);
-    if (!a.top)
+        write_row(a, row, token, zt, p, d);
+    if (!top)
         return;
-    // A key's rank: the keys above it in its piece's list, which is sorted,
-    // and in each other one.
-    for (int i = threadIdx.x; i < splits * a.top; i += 256) {
-        const int split = i / a.top, at = i - split * a.top;
-        if (at >= min((long long)piece, a.vocab - (long long)split * piece))
-            continue;
-        const uint64_t mine = keys[(row * splits + split) * a.top + at];
-        int above = at;
-        for (int s = 0; s < splits && above < a.top; s++) {
-            if (s == split)
-                continue;
-            const int len = (int)min((long long)a.top,
-                                     min((long long)piece, a.vocab - (long long)s * piece));
-            const uint64_t *list = keys + (row * splits + s) * a.top;
-            int lo = 0, hi = len;  // list[lo - 1] > mine > list[hi]
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (list[mid] > mine)
-                    lo = mid + 1;
-                else
-                    hi = mid;
-            }
-            above += lo;
-        }
-        if (above < a.top)
-            put_top(a, row, above, mine, p, d);
+    __syncthreads();
+    put_ranked(heads, nheads, top, threadIdx.x, 256, [&](int rank, uint64_t k) {
+        if (rank == top - 1)
+            bound = k;
+    });
+    __syncthreads();
+    const int n = (splits - 1) * top + last;
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const uint64_t k = list[i];
+        if (k >= bound)
+            found[atomicAdd(&count, 1)] = k;
     }
+    __syncthreads();
+    put_ranked(found, count, top, threadIdx.x, 256,
+               [&](int rank, uint64_t k) { put_top(a, row, rank, k, p, d); });
 }
 
 // -------------------------------------------------------------------- backward
-// Groups of tpr threads (a power of two up to 256) take `per` packs each of a
-// row's piece.
+// Groups of tpr threads (a power of two up to 256) take NV packs each: of a row
+// each, or, as a workgroup, of the piece blockIdx.x of row blockIdx.y.
 template <class T, int NV>
-__global__ __launch_bounds__(256) void logprob_back(LogprobBwdArgs a, int tpr, int pieces)
+__global__ __launch_bounds__(256) void logprob_back(LogprobBwdArgs a, int tpr)
 {
     constexpr int N = Pack<T>::N;
-    const int t = threadIdx.x & (tpr - 1);
-    const long long item = (long long)blockIdx.x * (256 / tpr) + threadIdx.x / tpr;
-    const long long row = item / pieces;
+    const int t = threadIdx.x & (tpr - 1), vocab = (int)a.vocab;
+    const long long row = tpr == 256 ? blockIdx.y : blockIdx.x * (256 / tpr) + threadIdx.x / tpr;
     if (row >= a.rows)
         return;
-    const long long first = (item - row * pieces) * tpr * N * NV;
-    const float peak = a.stats[2 * row], log_s = a.stats[2 * row + 1], scale = a.scale;
-    const long long target = a.dlogp ? a.targets[row] : -1;
-    float dl = target >= 0 ? a.dlogp[row] * scale : 0.f;
-    if (target >= a.vocab)
-        dl = __builtin_nanf("");
-    const float de = a.dentropy ? a.dentropy[row] * scale : 0.f;
-    const float ent = a.dentropy ? a.entropy[row] : 0.f;
-    const bool none = peak == -kInf && log_s == 0.f;
+    const int first = tpr == 256 ? blockIdx.x * (256 * N * NV) : 0;
     const T *z = (const T *)a.logits.p + row * a.logits.ld;
     T *dz = (T *)a.dlogits.p + row * a.dlogits.ld;
     typename Pack<T>::V raw[NV];
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-        const long long c = first + (t + i * tpr) * N;
+        const int c = first + (t + i * tpr) * N;
         raw[i] = typename Pack<T>::V{};
-        if (c < a.vocab)
-            raw[i] = load_pack<T>(z + c, a.vocab - c, (T)0.f);
+        if (c < vocab)
+            raw[i] = load_pack<T>(z + c, vocab - c, (T)0.f);
     }
+    const float peak = a.stats[2 * row], log_s = a.stats[2 * row + 1], scale = a.scale;
+    const long long target = a.dlogp ? a.targets[row] : -1;
+    float dl = target >= 0 ? a.dlogp[row] * scale : 0.f;
+    if (target >= vocab)
+        dl = __builtin_nanf("");
+    const float de = a.dentropy ? a.dentropy[row] * scale : 0.f;
+    const float ent = a.dentropy ? a.entropy[row] : 0.f;
+    const bool none = peak == -kInf && log_s == 0.f;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-        const long long c = first + (t + i * tpr) * N;
-        if (c >= a.vocab)
+        const int c = first + (t + i * tpr) * N;
+        if (c >= vocab)
             continue;
         typename Pack<T>::V v;
 #pragma unroll
@@ -425,36 +522,39 @@ __global__ __launch_bounds__(256) void logprob_back(LogprobBwdArgs a, int tpr, i
             if (c + j == target)
                 f += dl;
             if (none)
-                f = target >= a.vocab ? dl : 0.f;
+                f = target >= vocab ? dl : 0.f;
             v[j] = (T)f;
         }
-        store_pack<T>(dz + c, a.vocab - c, v);
+        store_pack<T>(dz + c, vocab - c, v);
     }
 }
 
 // ----------------------------------------------------------------- launch rules
 int pack_of(int xtype) { return xtype == 0 ? 4 : 8; }
 
-int block_of(int n_pack, long long n)
-{
-    return n >= 1024LL * n_pack * 4 ? 1024 : n >= 512LL * n_pack * 2 ? 512 : 256;
-}
-
-// Pieces of a row: one workgroup a row where the rows fill the CUs; else pieces
-// of at least 4096 elements, up to 64.
+// Pieces of a row, and the threads of a team.  One piece a row where the rows
+// fill the CUs; else pieces of at least 4096 elements, up to kPieces.
 struct Cut {
-    int piece, splits;
+    int piece, splits, team;
 };
 
-Cut cut(int xtype, long long rows, long long vocab)
+Cut cut(int xtype, long long rows, long long vocab, int top)
 {
+    const int n = pack_of(xtype);
     const long long want = std::max(1LL, (long long)num_cus() / std::max(1LL, rows));
-    const long long most = std::min(64LL, std::max(1LL, vocab / 4096));
-    const long long splits = std::min(want, most);
-    const int n = pack_of(xtype) * 256;
-    const long long piece =
-        splits == 1 ? vocab : ((vocab + splits - 1) / splits + n - 1) / n * n;
-    return Cut{(int)piece, (int)((vocab + piece - 1) / piece)};
+    const long long most = std::min((long long)kPieces, std::max(1LL, vocab / 4096));
+    long long splits = std::min(want, most), piece = vocab;
+    if (splits > 1) {
+        piece = ((vocab + splits - 1) / splits + n * 256 - 1) / (n * 256) * (n * 256);
+        splits = (vocab + piece - 1) / piece;
+    }
+    int team = 256;
+    if (splits == 1 && ((vocab <= 64LL * n * 4 && (top || rows >= 2LL * num_cus())) ||
+                        (vocab <= 64LL * n * 16 && rows >= 2LL * num_cus())))
+        team = 64;
+    else if (vocab >= 256LL * n * 32 && splits == 1 && rows <= 2LL * num_cus())
+        team = 1024;
+    return Cut{(int)piece, (int)splits, team};
 }
 
 size_t parts_bytes(long long rows, int splits)
@@ -465,19 +565,17 @@ size_t parts_bytes(long long rows, int splits)
 template <class T>
 hipError_t forward(int xtype, const LogprobArgs &a, hipStream_t stream)
 {
-    const Cut s = cut(xtype, a.rows, a.vocab);
+    const Cut s = cut(xtype, a.rows, a.vocab, a.top);
     Soft *parts = (Soft *)a.ws;
     uint64_t *keys = (uint64_t *)((char *)a.ws + parts_bytes(a.rows, s.splits));
-    const int block = block_of(pack_of(xtype), s.piece);
-    if (s.splits > 1) {
-        logprob_rows<T><<<(unsigned)(a.rows * s.splits), block, 0, stream>>>(a, s.piece, s.splits,
-                                                                             parts, keys);
-        logprob_join<T><<<(unsigned)a.rows, 256, 0, stream>>>(a, s.piece, s.splits, parts, keys);
-        return hipGetLastError();
-    }
-    for (long long first = 0; first < a.rows; first += kMaxBlocks) {
-        LogprobArgs c = a;  // the rows of this launch
-        c.rows = std::min(kMaxBlocks, a.rows - first);
+    const long long teams = s.team < 256 ? 256 / s.team : 1;
+    // Loads that leave nothing in the caches, for logits larger than the
+    // last-level one holds beside the rest.
+    const bool through = a.rows * a.vocab * (long long)sizeof(T) > 100LL << 20;
+    const long long most = s.splits > 1 ? a.rows : kMaxBlocks * teams;  // rows of a launch
+    for (long long first = 0; first < a.rows; first += most) {
+        LogprobArgs c = a;
+        c.rows = std::min(most, a.rows - first);
         c.logits.p = (const T *)a.logits.p + first * a.logits.ld;
         c.targets = a.targets ? a.targets + first : nullptr;
         c.logp = a.logp ? a.logp + first : nullptr;
@@ -486,7 +584,19 @@ hipError_t forward(int xtype, const LogprobArgs &a, hipStream_t stream)
         c.stats = a.stats ? a.stats + 2 * first : nullptr;
         c.top_logp = a.top ? a.top_logp + first * a.top : nullptr;
         c.top_index = a.top ? a.top_index + first * a.top : nullptr;
-        logprob_rows<T><<<(unsigned)c.rows, block, 0, stream>>>(c, s.piece, 1, nullptr, nullptr);
+        const unsigned grid = (unsigned)((c.rows * s.splits + teams - 1) / teams);
+        if (s.team == 64)
+            logprob_rows<T, 64><<<grid, 256, 0, stream>>>(c, s.piece, s.splits, through, parts,
+                                                               keys);
+        else if (s.team == 256)
+            logprob_rows<T, 256><<<grid, 256, 0, stream>>>(c, s.piece, s.splits, through, parts,
+                                                           keys);
+        else
+            logprob_rows<T, 1024><<<grid, 1024, 0, stream>>>(c, s.piece, s.splits, through, parts,
+                                                             keys);
+        if (s.splits > 1)
+            logprob_join<T><<<(unsigned)c.rows, 256, 0, stream>>>(c, s.piece, s.splits, parts,
+                                                                  keys);
     }
     return hipGetLastError();
 }
@@ -494,15 +604,16 @@ hipError_t forward(int xtype, const LogprobArgs &a, hipStream_t stream)
 template <class T>
 hipError_t backward(const LogprobBwdArgs &a, hipStream_t stream)
 {
-    constexpr int N = Pack<T>::N, NV = 4;
+    constexpr int N = Pack<T>::N, NV = 2;
     const long long packs = (a.vocab + N - 1) / N;
     int tpr = 1;
     while (tpr < 256 && (long long)tpr * NV < packs)
         tpr *= 2;
-    const long long pieces = (packs + tpr * NV - 1) / (tpr * NV);
-    const long long groups = 256 / tpr;
-    // Rows of one launch: its workgroups stay below kMaxBlocks.
-    const long long most = std::max(1LL, kMaxBlocks * groups / pieces);
+    // A vocabulary below 2^29 makes at most 2^17 pieces; rows of a launch by the
+    // grid's limits.
+    const long long pieces = tpr == 256 ? (packs + 256 * NV - 1) / (256 * NV) : 1;
+    const long long most =
+        tpr == 256 ? std::min(65535LL, std::max(1LL, 4 * kMaxBlocks / pieces)) : kMaxBlocks;
     for (long long first = 0; first < a.rows; first += most) {
         LogprobBwdArgs c = a;
         c.rows = std::min(most, a.rows - first);
@@ -513,8 +624,9 @@ hipError_t backward(const LogprobBwdArgs &a, hipStream_t stream)
         c.dlogp = a.dlogp ? a.dlogp + first : nullptr;
         c.entropy = a.entropy ? a.entropy + first : nullptr;
         c.dentropy = a.dentropy ? a.dentropy + first : nullptr;
-        const long long blocks = (c.rows * pieces + groups - 1) / groups;
-        logprob_back<T, NV><<<(unsigned)blocks, 256, 0, stream>>>(c, tpr, (int)pieces);
+        const dim3 grid = tpr == 256 ? dim3((unsigned)pieces, (unsigned)c.rows)
+                                     : dim3((unsigned)((c.rows * tpr + 255) / 256));
+        logprob_back<T, NV><<<grid, 256, 0, stream>>>(c, tpr);
     }
     return hipGetLastError();
 }
@@ -523,7 +635,7 @@ hipError_t backward(const LogprobBwdArgs &a, hipStream_t stream)
 
 size_t logprob_ws(int xtype, long long rows, long long vocab, int top)
 {
-    const Cut s = cut(xtype, rows, vocab);
+    const Cut s = cut(xtype, rows, vocab, top);
     if (s.splits == 1)
         return 0;
     return parts_bytes(rows, s.splits) + (size_t)rows * s.splits * top * sizeof(uint64_t);
