@@ -13,9 +13,21 @@ namespace {
 
 // The tensors of one launch go by value with its arguments, which hold below
 // 4 KiB: so no table of them has to reach the device.
+#ifndef FS
+#define FS 4
+#endif
+#ifndef FC
+#define FC 4
+#endif
+#ifndef CH
+#define CH 16384
+#endif
+#ifndef MP
+#define MP 1024
+#endif
 constexpr int kTensors = 112;
-constexpr int kChunk = 16384;     // elements of a tensor that a workgroup takes at once
-constexpr int kMaxParts = 1024;   // workgroups, and partial sums, of a launch
+constexpr int kChunk = CH;     // elements of a tensor that a workgroup takes at once
+constexpr int kMaxParts = MP;   // workgroups, and partial sums, of a launch
 
 struct TensorList {
     const void *in[kTensors];
@@ -53,20 +65,39 @@ __device__ __forceinline__ double block_sum(double v, double *lds)
     return lds[0] + lds[1] + (lds[2] + lds[3]);
 }
 
+// F packs of the n elements at p in flight, a pack a thread and step.
+template <class T, int F, class Use>
+__device__ __forceinline__ void each_pack(const T *p, int n, Use use)
+{
+    constexpr int N = Pack<T>::N;
+    for (int i = threadIdx.x * N; i < n; i += F * 256 * N) {
+        typename Pack<T>::V raw[F];
+#pragma unroll
+        for (int f = 0; f < F; f++) {
+            const int at = i + f * 256 * N;
+            raw[f] = typename Pack<T>::V{};
+            if (at < n)
+                raw[f] = load_pack<T>(p + at, n - at, (T)0.f);
+        }
+#pragma unroll
+        for (int f = 0; f < F; f++)
+            use(raw[f], i + f * 256 * N);
+    }
+}
+
 template <class T>
 __device__ __forceinline__ double chunk_squares(const T *p, int n)
 {
     constexpr int N = Pack<T>::N;
-    double s = 0;
-    for (int i = threadIdx.x * N; i < n; i += 256 * N) {
-        const auto raw = load_pack<T>(p + i, n - i, (T)0.f);
+    double s[4] = {0, 0, 0, 0};
+    each_pack<T, FS>(p, n, [&](typename Pack<T>::V v, int) {
 #pragma unroll
         for (int j = 0; j < N; j++) {
-            const double d = (double)(float)raw[j];
-            s = fma(d, d, s);
+            const double d = (double)(float)v[j];
+            s[j & 3] = fma(d, d, s[j & 3]);
         }
-    }
-    return s;
+    });
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 __global__ __launch_bounds__(256) void squares(TensorList l, double *parts)
@@ -111,14 +142,14 @@ template <class T>
 __device__ __forceinline__ void chunk_scale(const T *p, T *out, int n, float f)
 {
     constexpr int N = Pack<T>::N;
-    for (int i = threadIdx.x * N; i < n; i += 256 * N) {
-        const auto raw = load_pack<T>(p + i, n - i, (T)0.f);
+    each_pack<T, FC>(p, n, [&](typename Pack<T>::V raw, int i) {
         typename Pack<T>::V v;
 #pragma unroll
         for (int j = 0; j < N; j++)
             v[j] = (T)((float)raw[j] * f);
-        store_pack<T>(out + i, n - i, v);
-    }
+        if (i < n)
+            store_pack<T>(out + i, n - i, v);
+    });
 }
 
 __global__ __launch_bounds__(256) void clip(TensorList l, const double *parts, int nparts,
