@@ -1,5 +1,6 @@
-"""Build libmiconv.so (the HIP kernels and the C ABI) and libmipeak.so (the
-benchmark's measured reference points) in-tree for gfx950."""
+"""Build libmiconv.so (the HIP kernels and the C ABI), _mitrain.so (the Python
+binding of include/mitrain.h) and libmipeak.so (the benchmark's measured
+reference points) in-tree for gfx950."""
 from __future__ import annotations
 
 import os
@@ -19,6 +20,7 @@ SOURCES = ["api.hip", "conv_kernels.hip", "wino_kernels.hip", "pool_kernels.hip"
            "train_api.hip", "norm_kernels.hip", "logprob_kernels.hip", "clip_kernels.hip"]
 PEAK_LIBRARY = os.path.join(PKG, "libmipeak.so")
 PEAK_SOURCES = ["peaks.hip"]
+BINDING = os.path.join(PKG, "_mitrain.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -31,7 +33,10 @@ FLAGS = [
 
 
 def _hipcc(args, verbose):
-    cmd = [HIPCC] + args
+    _run([HIPCC] + args, verbose)
+
+
+def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -39,7 +44,7 @@ def _hipcc(args, verbose):
     text = "\n".join(l for l in res.stdout.splitlines()
                      if "packed-fp32-ops' is not a recognized feature" not in l)
     if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{text}")
+        raise RuntimeError(f"{cmd[0]} failed ({res.returncode}):\n{text}")
     if text.strip() and verbose:
         print(text, file=sys.stderr)
 
@@ -57,6 +62,27 @@ def _compile(sources, out, verbose):
     return tmp
 
 
+def _binding(verbose):
+    """The binding is host code on torch's headers: no HIP compiler."""
+    import sysconfig
+
+    import torch
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    include = os.path.join(os.path.dirname(torch.__file__), "include")
+    tmp = BINDING + ".tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+           "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"),
+           "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"],
+           "-isystem", os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include"),
+           os.path.join(CSRC, "binding.cpp"), "-o", tmp,
+           "-L", lib, "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
+    _run(cmd, verbose)
+    return tmp
+
+
 def build(verbose: bool = False) -> str:
     tmp = _compile(SOURCES, LIBRARY, verbose)
     # The image GEMM's untracked filter loads are only correct if the
@@ -64,6 +90,7 @@ def build(verbose: bool = False) -> str:
     from paper_1903_06934_amd import isa_check
     isa_check.check(HIPCC, FLAGS, os.path.join(CSRC, "conv_kernels.hip"))
     os.replace(tmp, LIBRARY)
+    os.replace(_binding(verbose), BINDING)
     os.replace(_compile(PEAK_SOURCES, PEAK_LIBRARY, verbose), PEAK_LIBRARY)
     return LIBRARY
 

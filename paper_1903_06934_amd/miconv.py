@@ -1,4 +1,4 @@
-"""ctypes binding of libmiconv.so (include/miconv.h; mitrain.py binds the
+"""ctypes binding of libmiconv.so (include/miconv.h; mitrain.py has the
 operators of include/mitrain.h).
 
 Argument marshalling only: every pass runs in the library's HIP kernels.

@@ -239,13 +239,14 @@ def test_binding_refuses():
     with pytest.raises(ValueError):
         m.grad_norm([x])
     from paper_1903_06934_amd import mitrain
-    assert mitrain._rows(torch.zeros(4, 6, 8), "x") == (24, 8, 8)
-    assert mitrain._rows(torch.zeros(4, 6, 8)[:, :, :5], "x") == (24, 5, 8)
-    assert mitrain._rows(torch.zeros(4, 6, 8)[:, 0], "x") == (4, 8, 48)
-    assert mitrain._rows(torch.zeros(4, 1, 8)[:, :, 2:], "x") == (4, 6, 8)
-    assert mitrain._rows(torch.zeros(8), "x") == (1, 8, 8)
-    assert mitrain._rows(torch.zeros(0, 8), "x") == (0, 8, 8)
+    rows = mitrain._binding().rows
+    assert rows(torch.zeros(4, 6, 8)) == (24, 8, 8)
+    assert rows(torch.zeros(4, 6, 8)[:, :, :5]) == (24, 5, 8)
+    assert rows(torch.zeros(4, 6, 8)[:, 0]) == (4, 8, 48)
+    assert rows(torch.zeros(4, 1, 8)[:, :, 2:]) == (4, 6, 8)
+    assert rows(torch.zeros(8)) == (1, 8, 8)
+    assert rows(torch.zeros(0, 8)) == (0, 8, 8)
     for bad in (torch.zeros(4, 6, 8)[:, :3], torch.zeros(8, 4).t(), torch.zeros(1, 8).expand(3, 8),
                 torch.zeros(())):
         with pytest.raises(ValueError):
-            mitrain._rows(bad, "x")
+            rows(bad)
