@@ -118,7 +118,7 @@ int logprob_bwd(int xtype, long long rows, long long vocab, const void *logits, 
  *   norm = sqrt(sum over the tensors of the sum of g^2),
  *   out = g f  with  f = 1 where norm <= max_norm, else max_norm / norm.
  * grads and out are host arrays of n device pointers, count their elements
- * (>= 0, at most 2^48 in all), types their element types; the arrays are read
+ * (>= 0, at most 2^37 in all), types their element types; the arrays are read
  * before the calls return.  out[i] may be grads[i] (clipping in place); the
  * tensors of out overlap no other tensor, nor norm or ws (MICONV_ERR_ALIAS).
  * The squares are summed in 64 bits, so their sum neither overflows nor loses

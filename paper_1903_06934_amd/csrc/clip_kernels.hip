@@ -11,47 +11,60 @@ namespace miconv {
 
 namespace {
 
-// The tensors of one launch go by value with its arguments, which hold below
-// 4 KiB: so no table of them has to reach the device.
-#ifndef FS
-#define FS 4
-#endif
-#ifndef FC
-#define FC 4
-#endif
-#ifndef CH
-#define CH 16384
-#endif
-#ifndef MP
-#define MP 1024
-#endif
+// Few tensors go by value with a launch's arguments, which hold below 4 KiB, so
+// no table of them has to reach the device before; more of them are first
+// written to a table in the workspace, kTensors a launch.
 constexpr int kTensors = 112;
-constexpr int kChunk = CH;     // elements of a tensor that a workgroup takes at once
-constexpr int kMaxParts = MP;   // workgroups, and partial sums, of a launch
+constexpr int kMaxParts = 1024;  // workgroups, and partial sums
 
 struct TensorList {
-    const void *in[kTensors];
-    void *out[kTensors];
-    long long count[kTensors];
-    unsigned first[kTensors + 1];  // chunks before tensor i
-    unsigned char type[kTensors];
-    int n;
+    GradEntry e[kTensors];
 };
 
-static_assert(sizeof(TensorList) <= 3840, "kernel arguments");
+static_assert(sizeof(TensorList) <= 3584, "kernel arguments");
 
-// The tensor of chunk c.
-__device__ __forceinline__ int tensor_of(const TensorList &l, unsigned c)
+__global__ __launch_bounds__(kTensors) void write_table(TensorList l, int n, GradEntry *table)
 {
-    int lo = 0, hi = l.n;  // first[lo] <= c < first[hi]
+    if ((int)threadIdx.x < n)
+        table[threadIdx.x] = l.e[threadIdx.x];
+}
+
+// The last of n entries that begins at chunk c or before it.  In the table by
+// the lanes of a wave, 64 at a time; among the arguments (scalar loads) by
+// halves.
+__device__ __forceinline__ int entry_of(const GradEntry *e, int n, unsigned c, bool table)
+{
+    int lo = 0, hi = n;
+    if (table) {
+        const int lane = threadIdx.x & 63;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+            const bool before = at < hi && e[at].first <= c;
+            const int k = __popcll(__ballot(before)) - 1;
+            lo += k * step;
+            hi = min(hi, lo + step);
+        }
+        return __builtin_amdgcn_readfirstlane(lo);
+    }
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (l.first[mid] <= c)
+        if (e[mid].first <= c)
             lo = mid;
         else
             hi = mid;
     }
     return lo;
+}
+
+// A workgroup's chunks: those of its share of all of them.
+struct Share {
+    unsigned first, end;
+};
+
+__device__ __forceinline__ Share share_of(unsigned chunks)
+{
+    return Share{(unsigned)((unsigned long long)chunks * blockIdx.x / gridDim.x),
+                 (unsigned)((unsigned long long)chunks * (blockIdx.x + 1) / gridDim.x)};
 }
 
 // Sum over a workgroup of 256 threads, in a fixed order.
@@ -65,8 +78,10 @@ __device__ __forceinline__ double block_sum(double v, double *lds)
     return lds[0] + lds[1] + (lds[2] + lds[3]);
 }
 
-// F packs of the n elements at p in flight, a pack a thread and step.
-template <class T, int F, class Use>
+// F packs of the n elements at p in flight, a pack a thread and step.  LAST: the
+// last time that they are read (clipping 75 M gradients of which the caches
+// hold a part, 288 tensors: 82 us instead of 90).
+template <class T, int F, bool LAST, class Use>
 __device__ __forceinline__ void each_pack(const T *p, int n, Use use)
 {
     constexpr int N = Pack<T>::N;
@@ -77,7 +92,7 @@ __device__ __forceinline__ void each_pack(const T *p, int n, Use use)
             const int at = i + f * 256 * N;
             raw[f] = typename Pack<T>::V{};
             if (at < n)
-                raw[f] = load_pack<T>(p + at, n - at, (T)0.f);
+                raw[f] = load_pack<T, LAST>(p + at, n - at, (T)0.f);
         }
 #pragma unroll
         for (int f = 0; f < F; f++)
@@ -90,7 +105,7 @@ __device__ __forceinline__ double chunk_squares(const T *p, int n)
 {
     constexpr int N = Pack<T>::N;
     double s[4] = {0, 0, 0, 0};
-    each_pack<T, FS>(p, n, [&](typename Pack<T>::V v, int) {
+    each_pack<T, 4, false>(p, n, [&](typename Pack<T>::V v, int) {
 #pragma unroll
         for (int j = 0; j < N; j++) {
             const double d = (double)(float)v[j];
@@ -100,24 +115,41 @@ __device__ __forceinline__ double chunk_squares(const T *p, int n)
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-__global__ __launch_bounds__(256) void squares(TensorList l, double *parts)
+// The share's chunks in order.
+__device__ __forceinline__ void add_squares(const GradEntry *e, int n, unsigned chunks,
+                                            double *parts, bool table)
 {
     __shared__ double lds[4];
+    const Share w = share_of(chunks);
     double s = 0;
-    for (unsigned c = blockIdx.x; c < l.first[l.n]; c += gridDim.x) {
-        const int i = tensor_of(l, c);
-        const long long at = (long long)(c - l.first[i]) * kChunk;
-        const int n = (int)min((long long)kChunk, l.count[i] - at);
-        if (l.type[i] == 0)
-            s += chunk_squares((const float *)l.in[i] + at, n);
-        else if (l.type[i] == 1)
-            s += chunk_squares((const __bf16 *)l.in[i] + at, n);
+    int i = entry_of(e, n, w.first, table);
+    for (unsigned c = w.first; c < w.end; c++) {
+        while (i + 1 < n && e[i + 1].first <= c)
+            i++;
+        const long long at = (long long)(c - e[i].first) * kGradChunk;
+        const int k = (int)min((long long)kGradChunk, e[i].count - at);
+        if (e[i].type == 0)
+            s += chunk_squares((const float *)e[i].in + at, k);
+        else if (e[i].type == 1)
+            s += chunk_squares((const __bf16 *)e[i].in + at, k);
         else
-            s += chunk_squares((const _Float16 *)l.in[i] + at, n);
+            s += chunk_squares((const _Float16 *)e[i].in + at, k);
     }
     s = block_sum(s, lds);
     if (threadIdx.x == 0)
         parts[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(256) void squares_few(TensorList l, int n, unsigned chunks,
+                                                   double *parts)
+{
+    add_squares(l.e, n, chunks, parts, false);
+}
+
+__global__ __launch_bounds__(256) void squares_table(const GradEntry *table, int n,
+                                                     unsigned chunks, double *parts)
+{
+    add_squares(table, n, chunks, parts, true);
 }
 
 // The norm from the partial sums; every workgroup of 256 threads computes the
@@ -142,7 +174,7 @@ template <class T>
 __device__ __forceinline__ void chunk_scale(const T *p, T *out, int n, float f)
 {
     constexpr int N = Pack<T>::N;
-    each_pack<T, FC>(p, n, [&](typename Pack<T>::V raw, int i) {
+    each_pack<T, 4, true>(p, n, [&](typename Pack<T>::V raw, int i) {
         typename Pack<T>::V v;
 #pragma unroll
         for (int j = 0; j < N; j++)
@@ -152,96 +184,93 @@ __device__ __forceinline__ void chunk_scale(const T *p, T *out, int n, float f)
     });
 }
 
-__global__ __launch_bounds__(256) void clip(TensorList l, const double *parts, int nparts,
-                                            float max_norm, float *norm)
+// The share's chunks in reverse: a workgroup of the same index has read them, the
+// last ones most recently, and its caches hold them still.
+__device__ __forceinline__ void scale_share(const GradEntry *e, int n, unsigned chunks,
+                                            const double *parts, int nparts, float max_norm,
+                                            float *norm, bool table)
 {
     __shared__ double lds[4];
     const double v = norm_of(parts, nparts, lds);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0)
         *norm = (float)v;
     const float f = v <= (double)max_norm ? 1.f : (float)((double)max_norm / v);
-    // The chunks that the norm read last come first: the caches still hold them.
-    const unsigned chunks = l.first[l.n];
-    for (unsigned b = blockIdx.x; b < chunks; b += gridDim.x) {
-        const unsigned c = chunks - 1 - b;
-        const int i = tensor_of(l, c);
-        const long long at = (long long)(c - l.first[i]) * kChunk;
-        const int n = (int)min((long long)kChunk, l.count[i] - at);
-        if (f == 1.f && l.out[i] == l.in[i])
+    const Share w = share_of(chunks);
+    if (w.first == w.end)
+        return;
+    int i = entry_of(e, n, w.end - 1, table);
+    for (unsigned c = w.end; c-- > w.first;) {
+        while (e[i].first > c)
+            i--;
+        if (f == 1.f && e[i].out == e[i].in)
             continue;  // in place, nothing to clip: as it is
-        if (l.type[i] == 0)
-            chunk_scale((const float *)l.in[i] + at, (float *)l.out[i] + at, n, f);
-        else if (l.type[i] == 1)
-            chunk_scale((const __bf16 *)l.in[i] + at, (__bf16 *)l.out[i] + at, n, f);
+        const long long at = (long long)(c - e[i].first) * kGradChunk;
+        const int k = (int)min((long long)kGradChunk, e[i].count - at);
+        if (e[i].type == 0)
+            chunk_scale((const float *)e[i].in + at, (float *)e[i].out + at, k, f);
+        else if (e[i].type == 1)
+            chunk_scale((const __bf16 *)e[i].in + at, (__bf16 *)e[i].out + at, k, f);
         else
-            chunk_scale((const _Float16 *)l.in[i] + at, (_Float16 *)l.out[i] + at, n, f);
+            chunk_scale((const _Float16 *)e[i].in + at, (_Float16 *)e[i].out + at, k, f);
     }
 }
 
-// Fills l with the tensors from `from` on, at most kTensors and 2^31 chunks; the
-// first tensor not in it.  Empty ones are left out.
-int fill(TensorList &l, int from, int n, const void *const *grads, void *const *out,
-         const long long *count, const int *types)
+__global__ __launch_bounds__(256) void clip_few(TensorList l, int n, unsigned chunks,
+                                                const double *parts, int nparts, float max_norm,
+                                                float *norm)
 {
-    l.n = 0;
-    unsigned long long chunks = 0;
-    int i = from;
-    for (; i < n && l.n < kTensors; i++) {
-        if (!count[i])
-            continue;
-        const unsigned long long c = (unsigned long long)((count[i] + kChunk - 1) / kChunk);
-        l.in[l.n] = grads[i];
-        l.out[l.n] = out ? out[i] : nullptr;
-        l.count[l.n] = count[i];
-        l.type[l.n] = (unsigned char)types[i];
-        l.first[l.n++] = (unsigned)chunks;
-        chunks += c;
-    }
-    l.first[l.n] = (unsigned)chunks;
-    return i;
+    scale_share(l.e, n, chunks, parts, nparts, max_norm, norm, false);
 }
 
-int blocks_of(const TensorList &l)
+__global__ __launch_bounds__(256) void clip_table(const GradEntry *table, int n, unsigned chunks,
+                                                  const double *parts, int nparts, float max_norm,
+                                                  float *norm)
 {
-    return (int)std::min<unsigned>(l.first[l.n], kMaxParts);
+    scale_share(table, n, chunks, parts, nparts, max_norm, norm, true);
+}
+
+TensorList list_of(const GradEntry *e, int n)
+{
+    TensorList l;
+    std::copy(e, e + n, l.e);
+    return l;
 }
 
 }  // namespace
 
-size_t clip_ws(int n, const long long *count, const int *types)
+size_t clip_ws(int n)
 {
-    (void)types;
-    int some = 0;
-    for (int i = 0; i < n; i++)
-        some += count[i] > 0;
-    return (size_t)(some + kTensors - 1) / kTensors * kMaxParts * sizeof(double);
+    return kMaxParts * sizeof(double) + (n > kTensors ? (size_t)n * sizeof(GradEntry) : 0);
 }
 
-hipError_t launch_clip(int n, const void *const *grads, const long long *count, const int *types,
-                       float max_norm, void *const *out, float *norm, double *ws,
-                       hipStream_t stream)
+hipError_t launch_clip(const GradEntry *e, int n, unsigned chunks, float max_norm, bool scale,
+                       float *norm, void *ws, hipStream_t stream)
 {
-    TensorList l;
-    int nparts = 0;
-    for (int i = 0; i < n;) {
-        i = fill(l, i, n, grads, out, count, types);
-        if (!l.n)
-            break;
-        squares<<<blocks_of(l), 256, 0, stream>>>(l, ws + nparts);
-        nparts += blocks_of(l);
-    }
-    if (!out || !nparts) {
+    double *parts = (double *)ws;
+    GradEntry *table = (GradEntry *)(parts + kMaxParts);
+    const int blocks = (int)std::min<unsigned>(chunks, kMaxParts);
+    if (!n) {
         if (norm)
-            norm_only<<<1, 256, 0, stream>>>(ws, nparts, norm);
+            norm_only<<<1, 256, 0, stream>>>(parts, 0, norm);
         return hipGetLastError();
     }
-    for (int i = 0; i < n;) {
-        i = fill(l, i, n, grads, out, count, types);
-        if (!l.n)
-            break;
-        clip<<<blocks_of(l), 256, 0, stream>>>(l, ws, nparts, max_norm, norm);
-        norm = nullptr;
+    if (n <= kTensors) {
+        const TensorList l = list_of(e, n);
+        squares_few<<<blocks, 256, 0, stream>>>(l, n, chunks, parts);
+        if (scale)
+            clip_few<<<blocks, 256, 0, stream>>>(l, n, chunks, parts, blocks, max_norm, norm);
+    } else {
+        for (int i = 0; i < n; i += kTensors) {
+            const int k = std::min(kTensors, n - i);
+            write_table<<<1, kTensors, 0, stream>>>(list_of(e + i, k), k, table + i);
+        }
+        squares_table<<<blocks, 256, 0, stream>>>(table, n, chunks, parts);
+        if (scale)
+            clip_table<<<blocks, 256, 0, stream>>>(table, n, chunks, parts, blocks, max_norm,
+                                                   norm);
     }
+    if (!scale)
+        norm_only<<<1, 256, 0, stream>>>(parts, blocks, norm);
     return hipGetLastError();
 }
 

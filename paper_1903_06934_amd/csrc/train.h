@@ -63,10 +63,18 @@ hipError_t launch_logprob_fwd(int xtype, const LogprobArgs &a, hipStream_t strea
 hipError_t launch_logprob_bwd(int xtype, const LogprobBwdArgs &a, hipStream_t stream);
 
 // ------------------------------------------------------------------ clipping
-size_t clip_ws(int n, const long long *count, const int *types);
-// out null: the norm only.
-hipError_t launch_clip(int n, const void *const *grads, const long long *count, const int *types,
-                       float max_norm, void *const *out, float *norm, double *ws,
-                       hipStream_t stream);
+// A tensor with elements; first: the chunks of the tensors before it.
+constexpr int kGradChunk = 16384;  // elements that a workgroup takes at once
+struct GradEntry {
+    const void *in;
+    void *out;
+    long long count;
+    unsigned first;
+    int type;
+};
+size_t clip_ws(int n);
+// The norm of n tensors of some chunks, and if scale is set their clipping.
+hipError_t launch_clip(const GradEntry *e, int n, unsigned chunks, float max_norm, bool scale,
+                       float *norm, void *ws, hipStream_t stream);
 
 }  // namespace miconv

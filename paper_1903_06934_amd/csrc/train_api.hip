@@ -112,7 +112,7 @@ int check_list(int n, const void *const *grads, const long long *count, const in
         return MICONV_ERR_SHAPE;
     if (n && (!grads || !count || !types))
         return MICONV_ERR_NULL;
-    long long left = kMaxSpan;
+    long long left = kMaxAll;
     for (int i = 0; i < n; i++) {
         if (!known_type(types[i]))
             return MICONV_ERR_TYPE;
@@ -131,27 +131,60 @@ int check_list(int n, const void *const *grads, const long long *count, const in
 
 struct Span {
     uintptr_t first, end;
-    bool written;
 };
 
-// Whether a written span overlaps any other: in the order of their
-// beginnings, one that begins before the farthest end so far overlaps the span
-// that has it.
-bool any_overlap(std::vector<Span> &s)
+// Sorted by beginning (lists of tensors often are already).
+void sort_spans(std::vector<Span> &s)
 {
-    const auto before = [](const Span &a, const Span &b) {
-        return a.first != b.first ? a.first < b.first : a.end > b.end;
-    };
+    const auto before = [](const Span &a, const Span &b) { return a.first < b.first; };
     if (!std::is_sorted(s.begin(), s.end(), before))
         std::sort(s.begin(), s.end(), before);
-    uintptr_t read_end = 0, written_end = 0;
-    for (const Span &v : s) {
-        if (v.first < written_end || (v.written && v.first < read_end))
+}
+
+// Whether any two written spans overlap, or a written one and a read one.
+bool any_overlap(std::vector<Span> &written, std::vector<Span> &read)
+{
+    sort_spans(written);
+    sort_spans(read);
+    uintptr_t written_end = 0, read_end = 0;  // the farthest ends of the spans so far
+    size_t r = 0;
+    for (const Span &w : written) {
+        for (; r < read.size() && read[r].first < w.first; r++) {
+            if (read[r].first < written_end)
+                return true;
+            read_end = std::max(read_end, read[r].end);
+        }
+        if (w.first < written_end || w.first < read_end)
             return true;
-        uintptr_t &end = v.written ? written_end : read_end;
-        end = std::max(end, v.end);
+        written_end = w.end;
     }
-    return false;
+    return r < read.size() && read[r].first < written_end;
+}
+
+int some_tensors(int n, const long long *count)
+{
+    int some = 0;
+    for (int i = 0; i < n; i++)
+        some += count[i] > 0;
+    return some;
+}
+
+// The tensors with elements; false: more chunks than their numbers hold.
+bool entries(int n, const void *const *grads, const long long *count, const int *types,
+             void *const *out, std::vector<GradEntry> &e, unsigned *chunks)
+{
+    unsigned long long c = 0;
+    e.reserve(n);
+    for (int i = 0; i < n; i++) {
+        if (!count[i])
+            continue;
+        e.push_back(GradEntry{grads[i], out ? out[i] : nullptr, count[i], (unsigned)c, types[i]});
+        c += (unsigned long long)((count[i] + kGradChunk - 1) / kGradChunk);
+        if (c >> 31)
+            return false;
+    }
+    *chunks = (unsigned)c;
+    return true;
 }
 
 }  // namespace
@@ -301,7 +334,8 @@ size_t grad_workspace_size(int n, const long long *count, const int *types)
 {
     if (n <= 0 || !count || !types)
         return 0;
-    return clip_ws(n, count, types);
+    const int some = some_tensors(n, count);
+    return some ? clip_ws(some) : 0;
 }
 
 int grad_norm(int n, const void *const *grads, const long long *count, const int *types,
@@ -310,7 +344,7 @@ int grad_norm(int n, const void *const *grads, const long long *count, const int
     int st = check_list(n, grads, count, types);
     if (st != MICONV_OK)
         return st;
-    const size_t need = clip_ws(n, count, types);
+    const size_t need = grad_workspace_size(n, count, types);
     const Buffer out = flat(norm, 4, 4, true, true);
     if ((st = check(&out, 1, ws, ws_bytes, need)) != MICONV_OK)
         return st;
@@ -320,10 +354,18 @@ int grad_norm(int n, const void *const *grads, const long long *count, const int
         if (overlap(g, out) || overlap(g, w))
             return MICONV_ERR_ALIAS;
     }
-    if ((st = ready()) != MICONV_OK)
-        return st;
-    return launch_status(
-        launch_clip(n, grads, count, types, 0.f, nullptr, norm, (double *)ws, stream));
+    try {
+        std::vector<GradEntry> e;
+        unsigned chunks = 0;
+        if (!entries(n, grads, count, types, nullptr, e, &chunks))
+            return MICONV_ERR_SHAPE;
+        if ((st = ready()) != MICONV_OK)
+            return st;
+        return launch_status(
+            launch_clip(e.data(), (int)e.size(), chunks, 0.f, false, norm, ws, stream));
+    } catch (const std::bad_alloc &) {
+        return MICONV_ERR_LAUNCH;
+    }
 }
 
 int grad_clip(int n, const void *const *grads, const long long *count, const int *types,
@@ -343,35 +385,37 @@ int grad_clip(int n, const void *const *grads, const long long *count, const int
         if ((uintptr_t)out[i] % type_size(types[i]))
             return MICONV_ERR_ALIGN;
     }
-    const size_t need = clip_ws(n, count, types);
+    const size_t need = grad_workspace_size(n, count, types);
     const Buffer nb = flat(norm, 4, 4, true, false);
     if ((st = check(&nb, 1, ws, ws_bytes, need)) != MICONV_OK)
         return st;
     try {
-        std::vector<Span> spans;
-        spans.reserve(2 * (size_t)n + 2);
-        for (int i = 0; i < n; i++) {
-            if (!count[i])
-                continue;
-            const uintptr_t bytes = (uintptr_t)count[i] * type_size(types[i]);
-            const uintptr_t o = (uintptr_t)out[i], g = (uintptr_t)grads[i];
-            spans.push_back(Span{o, o + bytes, true});
-            if (o != g)
-                spans.push_back(Span{g, g + bytes, false});
+        std::vector<GradEntry> e;
+        unsigned chunks = 0;
+        if (!entries(n, grads, count, types, out, e, &chunks))
+            return MICONV_ERR_SHAPE;
+        std::vector<Span> written, read;
+        written.reserve(e.size() + 2);
+        read.reserve(e.size());
+        for (const GradEntry &g : e) {
+            const uintptr_t bytes = (uintptr_t)g.count * type_size(g.type);
+            written.push_back(Span{(uintptr_t)g.out, (uintptr_t)g.out + bytes});
+            if (g.out != g.in)
+                read.push_back(Span{(uintptr_t)g.in, (uintptr_t)g.in + bytes});
         }
         if (norm)
-            spans.push_back(Span{(uintptr_t)norm, (uintptr_t)norm + 4, true});
+            written.push_back(Span{(uintptr_t)norm, (uintptr_t)norm + 4});
         if (need)
-            spans.push_back(Span{(uintptr_t)ws, (uintptr_t)ws + need, true});
-        if (any_overlap(spans))
+            written.push_back(Span{(uintptr_t)ws, (uintptr_t)ws + need});
+        if (any_overlap(written, read))
             return MICONV_ERR_ALIAS;
+        if ((st = ready()) != MICONV_OK)
+            return st;
+        return launch_status(
+            launch_clip(e.data(), (int)e.size(), chunks, max_norm, true, norm, ws, stream));
     } catch (const std::bad_alloc &) {
         return MICONV_ERR_LAUNCH;
     }
-    if ((st = ready()) != MICONV_OK)
-        return st;
-    return launch_status(
-        launch_clip(n, grads, count, types, max_norm, out, norm, (double *)ws, stream));
 }
 
 }  // extern "C"

@@ -380,6 +380,7 @@ def test_logprob_gradient_by_differences():
 SIZES = [
     [1], [0], [], [16384], [16385, 0, 3], [7] * 300, [1000003, 5, 64, 4096 * 11],
     [33] * 111 + [0] * 5 + [2, 50000], [1 << 22],
+    [100] * 112, [100] * 113, [1025 * 16384 + 7, 3], [20000] * 599 + [1], [1] * 4200,
 ]
 
 
