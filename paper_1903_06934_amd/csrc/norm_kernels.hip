@@ -398,25 +398,26 @@ __global__ __launch_bounds__(1024) void norm_bwd_sum(const float *parts, int n, 
     if (!out)
         return;
     const int lane = threadIdx.x & 31, half = threadIdx.x >> 5;
-    const long long c = (long long)blockIdx.x * 32 + lane;
-    const float *in = parts + (size_t)k * cols + c;
-    float s = 0.f;
-    if (c < cols)
-        for (int p = half; p < n; p += 256) {
-            float v[8];
+    for (long long first = blockIdx.x * 32LL; first < cols; first += gridDim.x * 32LL) {
+        const long long c = first + lane;
+        const float *in = parts + (size_t)k * cols + c;
+        float s = 0.f;
+        if (c < cols)
+            for (int p = half; p < n; p += 256) {
+                float v[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                v[i] = p + 32 * i < n ? in[(size_t)(p + 32 * i) * 2 * cols] : 0.f;
-            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-        }
-    lds[half][lane] = s;
-    __syncthreads();
-    // Half-wave h of the transposed block: the 32 sums of column h.
-    s = lds[lane][half];
-    s = wave_reduce(s, 32, Add());
-    const long long col = (long long)blockIdx.x * 32 + half;
-    if (lane == 0 && col < cols)
-        out[col] = (TW)s;
+                for (int i = 0; i < 8; i++)
+                    v[i] = p + 32 * i < n ? in[(size_t)(p + 32 * i) * 2 * cols] : 0.f;
+                s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+            }
+        __syncthreads();
+        lds[half][lane] = s;
+        __syncthreads();
+        // Half-wave h of the transposed block: the 32 sums of column h.
+        s = wave_reduce(lds[lane][half], 32, Add());
+        if (lane == 0 && first + half < cols)
+            out[first + half] = (TW)s;
+    }
 }
 
 // Long rows: sums of g and g u of each piece to sums[row][split][2], four packs
@@ -780,7 +781,7 @@ hipError_t bwd(int xtype, const NormBwdArgs &a, hipStream_t stream)
     }
     // One workgroup (or chunk) has written them itself; without rows they are 0.
     if (n != 1 && (a.dw || a.db)) {
-        const dim3 grid((unsigned)((a.cols + 31) / 32), 2);
+        const dim3 grid((unsigned)std::min(kMaxBlocks, (a.cols + 31) / 32), 2);
         norm_bwd_sum<TW><<<grid, 1024, 0, stream>>>(parts, n, a.cols, (TW *)a.dw, (TW *)a.db);
     }
     return hipGetLastError();
