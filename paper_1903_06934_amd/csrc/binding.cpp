@@ -143,6 +143,26 @@ Tensor empty(at::IntArrayRef sizes, const Tensor &x, at::ScalarType type)
     return at::empty(sizes, x.options().dtype(type));
 }
 
+// Small results side by side in one buffer: its allocation takes the host longer
+// than the views.
+struct Results {
+    Tensor bytes;
+    int64_t used = 0;
+
+    Results(int64_t size, const Tensor &x) : bytes(empty({size}, x, at::kByte)) {}
+
+    // The next tensor; the ones of larger elements come first.
+    Tensor next(at::IntArrayRef sizes, at::ScalarType type)
+    {
+        Tensor t = at::detail::make_tensor<c10::TensorImpl>(
+            c10::Storage(bytes.storage()), bytes.key_set(), c10::scalarTypeToTypeMeta(type));
+        t.unsafeGetTensorImpl()->set_storage_offset(used / (int64_t)c10::elementSize(type));
+        t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+        used += t.numel() * (int64_t)c10::elementSize(type);
+        return t;
+    }
+};
+
 // The caller's workspace, or one of the size that is needed.
 struct Workspace {
     Maybe own;
@@ -192,8 +212,15 @@ std::tuple<Tensor, Tensor, Tensor> layernorm_forward(const Tensor &x, const Mayb
     const void *wp = vector(w, "w", r.cols, wt), *bp = vector(b, "b", r.cols, wt);
     const Tensor y = y_ ? *y_ : empty(x.sizes(), x, x.scalar_type());
     const int64_t ldy = like(y, "y", x, r);
-    const Tensor mean = mean_ ? *mean_ : empty({r.rows}, x, at::kFloat);
-    const Tensor rstd = rstd_ ? *rstd_ : empty({r.rows}, x, at::kFloat);
+    Tensor mean, rstd;
+    if (mean_ && rstd_) {
+        mean = *mean_;
+        rstd = *rstd_;
+    } else {
+        Results out(8 * r.rows, x);
+        mean = mean_ ? *mean_ : out.next({r.rows}, at::kFloat);
+        rstd = rstd_ ? *rstd_ : out.next({r.rows}, at::kFloat);
+    }
     const Workspace s(ws, lib.layernorm_fwd_ws(type, r.rows, r.cols), x.device());
     call(lib.layernorm_fwd(type, w ? type_of(*w) : b ? type_of(*b) : type, r.rows, r.cols,
                            x.data_ptr(), r.ld, wp, bp, (float)eps, y.data_ptr(), ldy,
@@ -264,15 +291,18 @@ std::tuple<Maybe, Tensor, Tensor, Tensor, Maybe, Maybe> logprob_forward(const Te
         v.push_back(n);
         return v;
     };
-    const Tensor lse = empty(shape, z, at::kFloat), entropy = empty(shape, z, at::kFloat);
-    const Tensor stats = empty(last(2), z, at::kFloat);
+    if (top < 0)
+        call(MICONV_ERR_SHAPE, "logprob_fwd");
+    Results out(r.rows * (20 + 12LL * top), z);
     Maybe logp, top_logp, top_index;
-    if (targets)
-        logp = empty(shape, z, at::kFloat);
-    if (top > 0) {
-        top_logp = empty(last(top), z, at::kFloat);
-        top_index = empty(last(top), z, at::kLong);
+    if (top) {
+        top_index = out.next(last(top), at::kLong);
+        top_logp = out.next(last(top), at::kFloat);
     }
+    const Tensor lse = out.next(shape, at::kFloat), entropy = out.next(shape, at::kFloat);
+    const Tensor stats = out.next(last(2), at::kFloat);
+    if (targets)
+        logp = out.next(shape, at::kFloat);
     const Workspace s(ws, lib.logprob_fwd_ws(type, r.rows, r.cols, top), z.device());
     const auto at = [](const Maybe &t) { return t ? t->data_ptr() : nullptr; };
     call(lib.logprob_fwd(type, r.rows, r.cols, z.data_ptr(), r.ld, tp, (float)scale, top,

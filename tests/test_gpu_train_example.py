@@ -32,7 +32,7 @@ def test_step_matches_torch(example):
     logp = F.log_softmax(F.conv2d(a[:, :, None, None], q["w3"], q["b3"])[:, :, 0, 0], 1)
     loss = -logp.gather(1, labels.cpu()[:, None]).mean()
     loss.backward()
-    assert abs(float(-out.logp.mean()) - float(loss)) < 1e-5
+    assert abs(float(-out.logp.mean()) - float(loss.detach())) < 1e-5
     total = sum(float((v.grad ** 2).sum()) for v in q.values()) ** 0.5
     assert abs(float(norm) / total - 1) < 1e-4
     for k in p:
