@@ -341,6 +341,23 @@ def test_top_of_ordered_rows(vocab, kind, rows):
     assert torch.equal(out.top_index.cpu(), want["top_index"].expand(rows, top))
 
 
+@pytest.mark.parametrize("vocab", [1, 2, 7, 33, 63, 64])
+@pytest.mark.parametrize("rows", [1, 700])
+def test_top_of_the_whole_row(vocab, rows):
+    """top = vocab: every token, in order; logits of fewer dimensions."""
+    import paper_1903_06934_amd as m
+    z = torch.round(2 * randn(gen(vocab, rows), rows, vocab))
+    out = m.logprob_fwd(z.cuda(), top=vocab)
+    want = ref.logprob_fwd(z, None, vocab)
+    assert torch.equal(out.top_index.cpu(), want["top_index"])
+    one = m.logprob_fwd(z[0].cuda(), torch.tensor(0, device="cuda"), top=vocab)
+    assert one.lse.shape == () and one.stats.shape == (2,) and one.top_index.shape == (vocab,)
+    assert torch.equal(one.top_index, out.top_index[0])
+    cube = m.logprob_fwd(z.view(rows, 1, vocab).cuda(), top=vocab)
+    assert cube.lse.shape == (rows, 1) and cube.top_logp.shape == (rows, 1, vocab)
+    assert torch.equal(cube.top_logp[:, 0], out.top_logp)
+
+
 def test_logprob_far_from_zero():
     """Logits around 20000: log probabilities and gradient keep their own size's
     accuracy."""
