@@ -6,6 +6,7 @@
 // documentation; it hands over the library's functions once (load).
 #include <stdint.h>
 #include <string.h>
+#include <algorithm>
 #include <array>
 #include <optional>
 #include <string>
@@ -274,6 +275,7 @@ Maybe logprob_workspace(const Tensor &logits, int top)
 {
     Rows r;
     const int type = float_rows(logits, "logits", &r);
+    top = (int)std::min<int64_t>(top, r.cols);
     return workspace(lib.logprob_fwd_ws(type, r.rows, r.cols, top), logits.device());
 }
 
@@ -284,6 +286,7 @@ std::tuple<Maybe, Tensor, Tensor, Tensor, Maybe, Maybe> logprob_forward(const Te
 {
     Rows r;
     const int type = float_rows(z, "logits", &r);
+    top = (int)std::min<int64_t>(top, r.cols);  // a row has no more tokens
     const auto *tp = vector<long long>(targets, "targets", r.rows, at::kLong);
     const at::IntArrayRef shape = z.sizes().slice(0, z.dim() - 1);
     const auto last = [&](int64_t n) {

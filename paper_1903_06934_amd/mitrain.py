@@ -90,8 +90,8 @@ def logprob_workspace(logits, top=0):
 def logprob_fwd(logits, targets=None, top=0, scale=1.0, ws=None):
     """LogProbs of the rows of logits [..., vocab] under softmax(scale * logits):
     the log probabilities of targets [...] (int64; negative: none given), the
-    log of the softmax's sum, its entropy, the top likeliest tokens, and the
-    statistics that logprob_bwd takes."""
+    log of the softmax's sum, its entropy, the top (at most 64, or vocab where that
+    is fewer) likeliest tokens, and the statistics that logprob_bwd takes."""
     return LogProbs(*_binding().logprob_fwd(logits, targets, top, scale, ws))
 
 

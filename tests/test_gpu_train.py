@@ -353,6 +353,8 @@ def test_top_of_the_whole_row(vocab, rows):
     one = m.logprob_fwd(z[0].cuda(), torch.tensor(0, device="cuda"), top=vocab)
     assert one.lse.shape == () and one.stats.shape == (2,) and one.top_index.shape == (vocab,)
     assert torch.equal(one.top_index, out.top_index[0])
+    more = m.logprob_fwd(z.cuda(), top=vocab + 9)  # a row has no more tokens
+    assert torch.equal(more.top_index, out.top_index)
     cube = m.logprob_fwd(z.view(rows, 1, vocab).cuda(), top=vocab)
     assert cube.lse.shape == (rows, 1) and cube.top_logp.shape == (rows, 1, vocab)
     assert torch.equal(cube.top_logp[:, 0], out.top_logp)
