@@ -167,34 +167,65 @@ __device__ __forceinline__ Moments wave_merge(Moments m)
 }
 
 constexpr int kPieces = 64;
+// Packs in flight a thread of norm_fwd_pieces (1000 x 100000 bf16: 131 us, with 4
+// 137; 1 x 100000 11.5 and 14.0, with 1 10.4; 300 x 40000 fp32 31.0, 30.4 and 32.1).
+constexpr int kFwdPacks = 2;
 
 // Rows cut into `splits` (at most kPieces) pieces of `piece` elements (a multiple of a pack):
 // the moments of each piece to ws[row][split].
 template <class T>
 __global__ __launch_bounds__(256) void norm_fwd_pieces(NormFwdArgs a, long long piece, int splits)
 {
-    constexpr int N = Pack<T>::N;
+    constexpr int N = Pack<T>::N, F = kFwdPacks;
     __shared__ Moments part[4];
     const long long row = blockIdx.x / splits;
     const int split = (int)(blockIdx.x - row * splits);
     const long long first = split * piece;
     const long long end = min(first + piece, a.cols);
     const T *xr = (const T *)a.x.p + row * a.x.ld;
+    const T *x = xr + first;
+    const int len = (int)(end - first);
     Moments m{0.f, 0.f, 0.f};
-    for (long long c = first + threadIdx.x * N; c < end; c += 256 * N) {
-        const int left = (int)min((long long)N, end - c);
-        const auto raw = load_pack<T>(xr + c, left, (T)0.f);
+    for (int c = threadIdx.x * N; c < len; c += F * 256 * N) {
+        typename Pack<T>::V raw[F];
+#pragma unroll
+        for (int i = 0; i < F; i++) {
+            const int at = c + i * 256 * N;
+            raw[i] = typename Pack<T>::V{};
+            if (at < len)
+                raw[i] = load_pack<T>(x + at, len - at, (T)0.f);
+        }
         float s = 0.f, q = 0.f;
 #pragma unroll
-        for (int j = 0; j < N; j++)
-            s += (float)raw[j];
-        const float mean = s / left;
+        for (int i = 0; i < F; i++)
 #pragma unroll
-        for (int j = 0; j < N; j++) {
-            const float d = (float)raw[j] - mean;
-            q += j < left ? d * d : 0.f;
+            for (int j = 0; j < N; j++)
+                s += (float)raw[i][j];
+        if (c + ((F - 1) * 256 + 1) * N <= len) {
+            const float mean = s * (1.f / (F * N));
+#pragma unroll
+            for (int i = 0; i < F; i++)
+#pragma unroll
+                for (int j = 0; j < N; j++) {
+                    const float d = (float)raw[i][j] - mean;
+                    q += d * d;
+                }
+            m = merge(m, Moments{(float)(F * N), mean, q});
+        } else {  // the last packs, of which some are short or missing
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < F; i++)
+                n += max(0, min(N, len - c - i * 256 * N));
+            const float mean = s / (float)n;
+#pragma unroll
+            for (int i = 0; i < F; i++)
+#pragma unroll
+                for (int j = 0; j < N; j++) {
+                    const float d = (float)raw[i][j] - mean;
+                    q += c + i * 256 * N + j < len ? d * d : 0.f;
+                }
+            m = merge(m, Moments{(float)n, mean, q});
         }
-        m = merge(m, Moments{(float)left, mean, q});
     }
     m = wave_merge(m);
     if ((threadIdx.x & 63) == 0)
@@ -213,7 +244,7 @@ __global__ __launch_bounds__(256) void norm_fwd_pieces(NormFwdArgs a, long long 
 template <class T, class TW>
 __global__ __launch_bounds__(256) void norm_fwd_apply(NormFwdArgs a, long long piece, int splits)
 {
-    constexpr int N = Pack<T>::N;
+    constexpr int N = Pack<T>::N, F = 2;
     const long long row = blockIdx.x / splits;
     const int split = (int)(blockIdx.x - row * splits);
     const Moments *parts = (const Moments *)a.ws + row * splits;
@@ -231,20 +262,33 @@ __global__ __launch_bounds__(256) void norm_fwd_apply(NormFwdArgs a, long long p
     }
     const long long first = split * piece;
     const long long end = min(first + piece, a.cols);
-    const T *xr = (const T *)a.x.p + row * a.x.ld;
-    T *yr = (T *)a.y.p + row * a.y.ld;
+    const int len = (int)(end - first);
+    const T *x = (const T *)a.x.p + row * a.x.ld + first;
+    T *y = (T *)a.y.p + row * a.y.ld + first;
     const TW *w = (const TW *)a.w, *b = (const TW *)a.b;
-    for (long long c = first + threadIdx.x * N; c < end; c += 256 * N) {
-        const int left = (int)min((long long)N, end - c);
-        const auto raw = load_pack<T>(xr + c, left, (T)0.f);
-        float wv[N], bv[N];
-        load_weights<N>(w, c, a.cols, 1.f, wv);
-        load_weights<N>(b, c, a.cols, 0.f, bv);
-        typename Pack<T>::V v;
+    for (int c0 = threadIdx.x * N; c0 < len; c0 += F * 256 * N) {
+        typename Pack<T>::V raw[F];
+        float wv[F][N], bv[F][N];
 #pragma unroll
-        for (int j = 0; j < N; j++)
-            v[j] = (T)(((float)raw[j] - mean) * rstd * wv[j] + bv[j]);
-        store_pack<T>(yr + c, left, v);
+        for (int i = 0; i < F; i++) {
+            const int c = c0 + i * 256 * N;
+            raw[i] = typename Pack<T>::V{};
+            if (c < len)
+                raw[i] = load_pack<T>(x + c, len - c, (T)0.f);
+            load_weights<N>(w, first + c, end, 1.f, wv[i]);
+            load_weights<N>(b, first + c, end, 0.f, bv[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < F; i++) {
+            const int c = c0 + i * 256 * N;
+            if (c >= len)
+                continue;
+            typename Pack<T>::V v;
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                v[j] = (T)(((float)raw[i][j] - mean) * rstd * wv[i][j] + bv[i][j]);
+            store_pack<T>(y + c, len - c, v);
+        }
     }
 }
 
@@ -275,11 +319,16 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
     }
     typename Pack<T>::V rx[NV], rd[NV], nx[NV], nd[NV];
     float mean = 0.f, rstd = 0.f, nmean = 0.f, nrstd = 0.f;
+    const long long step = (long long)gridDim.x * groups;
+    long long row = (long long)blockIdx.x * groups + group;
+    // Where the row to load begins, and the row of dx to store.
+    const T *xr = (const T *)a.x.p + row * a.x.ld, *dyr = (const T *)a.dy.p + row * a.dy.ld;
+    T *dxr = (T *)a.dx.p + row * a.dx.ld;
+    const float *meanr = a.mean + row, *rstdr = a.rstd + row;
+    const long long x_step = step * a.x.ld, dy_step = step * a.dy.ld, dx_step = step * a.dx.ld;
     const auto load = [&](long long row) {
         if (row >= a.rows)
             return;
-        const T *xr = (const T *)a.x.p + row * a.x.ld;
-        const T *dyr = (const T *)a.dy.p + row * a.dy.ld;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const int c = (t + i * tpr) * N;
@@ -294,11 +343,13 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
                 }
             }
         }
-        nmean = a.mean[row];
-        nrstd = a.rstd[row];
+        nmean = *meanr;
+        nrstd = *rstdr;
+        xr += x_step;
+        dyr += dy_step;
+        meanr += step;
+        rstdr += step;
     };
-    const long long step = (long long)gridDim.x * groups;
-    long long row = (long long)blockIdx.x * groups + group;
     load(row);
     int turn = 0;
     for (; row < a.rows; row += step) {  // one row for the workgroup where it meets at the barrier
@@ -340,7 +391,6 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
             }
             turn ^= 1;
         }
-        T *dxr = (T *)a.dx.p + row * a.dx.ld;
         const float c1 = s1 * inv_n, c2 = s2 * inv_n;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
@@ -355,6 +405,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
             }
             store_pack<T>(dxr + c, cols - c, v);
         }
+        dxr += dx_step;
     }
     if (!a.dw && !a.db)
         return;
@@ -405,26 +456,45 @@ __global__ __launch_bounds__(1024) void norm_bwd_sum(const float *parts, int n, 
     if (!out)
         return;
     const int lane = threadIdx.x & 31, half = threadIdx.x >> 5;
-    for (long long first = blockIdx.x * 32LL; first < cols; first += gridDim.x * 32LL) {
-        const long long c = first + lane;
-        const float *in = parts + (size_t)k * cols + c;
-        float s = 0.f;
-        if (c < cols)
-            for (int p = half; p < n; p += 256) {
-                float v[8];
+    const long long c = blockIdx.x * 32LL + lane;
+    const float *in = parts + (size_t)k * cols + c;
+    float s = 0.f;
+    if (c < cols)
+        for (int p = half; p < n; p += 256) {
+            float v[8];
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    v[i] = p + 32 * i < n ? in[(size_t)(p + 32 * i) * 2 * cols] : 0.f;
-                s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-            }
-        __syncthreads();
-        lds[half][lane] = s;
-        __syncthreads();
-        // Half-wave h of the transposed block: the 32 sums of column h.
-        s = wave_reduce(lds[lane][half], 32, Add());
-        if (lane == 0 && first + half < cols)
-            out[first + half] = (TW)s;
-    }
+            for (int i = 0; i < 8; i++)
+                v[i] = p + 32 * i < n ? in[(size_t)(p + 32 * i) * 2 * cols] : 0.f;
+            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
+    lds[half][lane] = s;
+    __syncthreads();
+    // Half-wave h of the transposed block: the 32 sums of column h.
+    s = wave_reduce(lds[lane][half], 32, Add());
+    const long long col = blockIdx.x * 32LL + half;
+    if (lane == 0 && col < cols)
+        out[col] = (TW)s;
+}
+
+// The same for few parts of many columns: a thread a column (187 x 35904 bf16, 7
+// parts: 21.4 us in all, with half-waves 25.8).
+constexpr int kFewParts = 32;
+
+template <class TW>
+__global__ __launch_bounds__(256) void norm_bwd_sum_few(const float *parts, int n, long long cols,
+                                                        TW *dw, TW *db)
+{
+    const int k = blockIdx.y;
+    TW *out = k ? db : dw;
+    const long long c = blockIdx.x * 256LL + threadIdx.x;
+    if (!out || c >= cols)
+        return;
+    const float *in = parts + (size_t)k * cols + c;
+    float s = 0.f;
+#pragma unroll 8
+    for (int p = 0; p < n; p++)
+        s += in[(size_t)p * 2 * cols];
+    out[c] = (TW)s;
 }
 
 // Long rows: sums of g and g u of each piece to sums[row][split][2], four packs
@@ -443,27 +513,27 @@ __global__ __launch_bounds__(256) void norm_bwd_pieces(NormBwdArgs a, long long 
     const TW *w = (const TW *)a.w;
     const float mean = a.mean[row], rstd = a.rstd[row];
     float s1 = 0.f, s2 = 0.f;
-    for (long long c0 = first + threadIdx.x * N; c0 < end; c0 += F * 256 * N) {
-        typename Pack<T>::V rx[F], rd[F];
+    const int len = (int)(end - first);
+    for (int c0 = threadIdx.x * N; c0 < len; c0 += F * 256 * N) {
+        typename Pack<T>::V rx[F], rd[F];  // zeros in dy past the end
         float wv[F][N];
 #pragma unroll
         for (int i = 0; i < F; i++) {
-            const long long c = c0 + i * 256 * N;
+            const int c = c0 + i * 256 * N;
             rx[i] = rd[i] = typename Pack<T>::V{};
-            if (c < end) {
-                rx[i] = load_pack<T>(xr + c, a.cols - c, (T)0.f);
-                rd[i] = load_pack<T>(dyr + c, a.cols - c, (T)0.f);
+            if (c < len) {
+                rx[i] = load_pack<T>(xr + first + c, len - c, (T)0.f);
+                rd[i] = load_pack<T>(dyr + first + c, len - c, (T)0.f);
             }
-            load_weights<N>(w, c, end, 1.f, wv[i]);
+            load_weights<N>(w, first + c, end, 1.f, wv[i]);
         }
 #pragma unroll
         for (int i = 0; i < F; i++)
 #pragma unroll
             for (int j = 0; j < N; j++) {
-                const bool in = c0 + i * 256 * N + j < end;
-                const float g = in ? (float)rd[i][j] * wv[i][j] : 0.f;
+                const float g = (float)rd[i][j] * wv[i][j];
                 s1 += g;
-                s2 += in ? g * (((float)rx[i][j] - mean) * rstd) : 0.f;
+                s2 += g * (((float)rx[i][j] - mean) * rstd);
             }
     }
     s1 = group_reduce(s1, 256, red[0], Add());
@@ -687,33 +757,35 @@ bool streams(long long rows, long long cols, size_t elem, std::initializer_list<
     return lines;
 }
 
-// Pieces of long rows: forward as many as give every CU eight workgroups, of at
-// least 2048 elements (4 x 32768 bf16 9.3 us, with four of 4096 9.9), backward
-// four, of at least 4096 (32 x 100352 fp32 16.9 us, with eight of 2048 17.7);
-// at most kPieces a row.
+// Pieces of long rows: forward as many as give every CU eight workgroups, of
+// whole rounds of kFwdPacks packs, backward four, of at least 4096 elements (32 x
+// 100352 fp32 16.9 us, with eight of 2048 17.7); at most kPieces a row.
 struct PiecePlan {
     long long piece;
     int splits;
 };
 
-PiecePlan piece_plan(long long rows, long long cols, bool forward)
+PiecePlan piece_plan(int xtype, long long rows, long long cols, bool forward)
 {
-    const long long per_cu = forward ? 8 : 4, least = forward ? 2048 : 4096;
+    const long long per_cu = forward ? 8 : 4;
+    const long long least = forward ? 256 * kFwdPacks * pack_of(xtype) : 4096;
+    const long long unit = forward ? least : 2048;
     const long long want = std::max(1LL, per_cu * num_cus() / std::max(1LL, rows));
     const long long most = std::min((long long)kPieces, std::max(1LL, cols / least));
     const long long splits = std::min(want, most);
-    const long long piece = ((cols + splits - 1) / splits + 2047) / 2048 * 2048;
+    const long long piece = ((cols + splits - 1) / splits + unit - 1) / unit * unit;
     return PiecePlan{piece, (int)((cols + piece - 1) / piece)};
 }
 
-// Chunks of rows of norm_bwd_cols: one below 128 rows, which then needs no sum
-// over the chunks; else as many as give every CU two workgroups.
+// Chunks of rows of norm_bwd_cols: one up to 64 rows, which then needs no sum
+// over the chunks; else as many as give every CU two workgroups, of 16 rows at
+// least (169 x 25083 f16: 24.1 us, of 64 32.1).
 int row_chunks(int xtype, long long rows, long long cols)
 {
     const int n = pack_of(xtype);
     const long long tiles = (cols + 64 * n - 1) / (64 * n);
     const long long want = std::max(1LL, 2LL * num_cus() / tiles);
-    return (int)std::max(1LL, std::min(want, rows / 64));
+    return rows <= 64 ? 1 : (int)std::max(1LL, std::min(want, rows / 16));
 }
 
 template <class T, class TW, int NV, bool HOLD>
@@ -747,7 +819,7 @@ hipError_t fwd(int xtype, const NormFwdArgs &a, hipStream_t stream)
     if (p.nv)
         return hipGetLastError();
     // rows * cols is below 2^37 and a row above 2^15: below 2^23 workgroups.
-    const PiecePlan s = piece_plan(a.rows, a.cols, true);
+    const PiecePlan s = piece_plan(xtype, a.rows, a.cols, true);
     const dim3 grid((unsigned)(a.rows * s.splits));
     norm_fwd_pieces<T><<<grid, 256, 0, stream>>>(a, s.piece, s.splits);
     norm_fwd_apply<T, TW><<<grid, 256, 0, stream>>>(a, s.piece, s.splits);
@@ -784,7 +856,7 @@ hipError_t bwd(int xtype, const NormBwdArgs &a, hipStream_t stream)
         else
             bwd_rows<T, TW, kValues / N>(a, p, n, stream);
     } else if (a.rows) {
-        const PiecePlan s = piece_plan(a.rows, a.cols, false);
+        const PiecePlan s = piece_plan(xtype, a.rows, a.cols, false);
         n = row_chunks(xtype, a.rows, a.cols);
         float *out = (float *)((char *)a.ws +
                                up16((size_t)a.rows * s.splits * 2 * sizeof(float)));
@@ -797,8 +869,14 @@ hipError_t bwd(int xtype, const NormBwdArgs &a, hipStream_t stream)
     }
     // One workgroup (or chunk) has written them itself; without rows they are 0.
     if (n != 1 && (a.dw || a.db)) {
-        const dim3 grid((unsigned)std::min(kMaxBlocks, (a.cols + 31) / 32), 2);
-        norm_bwd_sum<TW><<<grid, 1024, 0, stream>>>(parts, n, a.cols, (TW *)a.dw, (TW *)a.db);
+        TW *dw = (TW *)a.dw, *db = (TW *)a.db;
+        if (n <= kFewParts && a.cols >= 4096) {
+            const dim3 grid((unsigned)((a.cols + 255) / 256), 2);
+            norm_bwd_sum_few<TW><<<grid, 256, 0, stream>>>(parts, n, a.cols, dw, db);
+        } else {
+            const dim3 grid((unsigned)((a.cols + 31) / 32), 2);
+            norm_bwd_sum<TW><<<grid, 1024, 0, stream>>>(parts, n, a.cols, dw, db);
+        }
     }
     return hipGetLastError();
 }
@@ -809,7 +887,7 @@ size_t norm_fwd_ws(int xtype, long long rows, long long cols)
 {
     if (row_plan(xtype, rows, cols, true).nv)
         return 0;
-    return (size_t)rows * piece_plan(rows, cols, true).splits * sizeof(Moments);
+    return (size_t)rows * piece_plan(xtype, rows, cols, true).splits * sizeof(Moments);
 }
 
 size_t norm_bwd_ws(int xtype, long long rows, long long cols)
@@ -818,7 +896,7 @@ size_t norm_bwd_ws(int xtype, long long rows, long long cols)
     const size_t part = 2 * (size_t)cols * sizeof(float);
     if (p.nv)
         return bwd_blocks(p, rows) * part;
-    return up16((size_t)rows * piece_plan(rows, cols, false).splits * 2 * sizeof(float)) +
+    return up16((size_t)rows * piece_plan(xtype, rows, cols, false).splits * 2 * sizeof(float)) +
            row_chunks(xtype, rows, cols) * part;
 }
 
