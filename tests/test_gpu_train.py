@@ -400,6 +400,7 @@ SIZES = [
     [1], [0], [], [16384], [16385, 0, 3], [7] * 300, [1000003, 5, 64, 4096 * 11],
     [33] * 111 + [0] * 5 + [2, 50000], [1 << 22],
     [100] * 112, [100] * 113, [1025 * 16384 + 7, 3], [20000] * 599 + [1], [1] * 4200,
+    [5] * 148, [70000, 1] * 148 + [3], [16384, 16385] * 74 + [40000],
 ]
 
 
