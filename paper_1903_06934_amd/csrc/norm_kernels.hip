@@ -680,10 +680,15 @@ RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
     if (forward && cols > 16384 && rows <= 64)
         return RowPlan{0, 0, 0};
     // Backward by pieces above 8192 elements (1024 threads have too few registers:
-    // 4096 x 16384 fp32 285 us, by pieces 232; bf16 113 and 121), and few rows
-    // from 4096 on (4 x 8192 bf16 14.9 and 8.4, 1024 x 4096 23.3 and 18.1, 4096 x
-    // 4096 34.1 and 36.4; 64 x 8192 fp32 13.9 and 11.1, 1024 x 8192 29.0 and 34.2).
-    if (!forward && (cols > 8192 || (cols >= 4096 && rows <= (n == 4 ? cols / 128 : 1024))))
+    // 4096 x 16384 fp32 285 us, by pieces 232; bf16 113 and 121), and where the
+    // rows' partial sums of dw and db would be about as many as their elements:
+    // up to 2048 rows from 4096 16-bit elements on (1040 x 4096 23.6 and 16.2, 4 x
+    // 8192 14.9 and 8.4; 3100 x 8192 45.2 and 48.8), of 256 rows at least from 2048
+    // on (520 x 2048 15.2 and 12.5; 60 x 2048 9.1 and 11.0), up to 512 rows from
+    // 4096 fp32 elements on (260 x 8192 19.7 and 15.0; 1040 x 8192 29.9 and 35.1).
+    const bool sums = n == 4 ? cols >= 4096 && rows <= 512
+                             : rows <= 2048 && cols >= (rows < 256 ? 4096 : 2048);
+    if (!forward && (cols > 8192 || sums))
         return RowPlan{0, 0, 0};
     if (packs <= 64) {
         int tpr = 1;

@@ -63,8 +63,8 @@ hipError_t launch_logprob_fwd(int xtype, const LogprobArgs &a, hipStream_t strea
 hipError_t launch_logprob_bwd(int xtype, const LogprobBwdArgs &a, hipStream_t stream);
 
 // ------------------------------------------------------------------ clipping
+constexpr int kGradChunk = 16384;  // bytes of a tensor that a workgroup takes at once
 // A tensor with elements; first: the chunks of the tensors before it.
-constexpr int kGradChunk = 16384;  // elements that a workgroup takes at once
 struct GradEntry {
     const void *in;
     void *out;
@@ -73,7 +73,7 @@ struct GradEntry {
     int type;
 };
 size_t clip_ws(int n);
-// The norm of n tensors of some chunks, and if scale is set their clipping.
+// The norm of n tensors, and if scale is set their clipping.
 hipError_t launch_clip(const GradEntry *e, int n, unsigned chunks, float max_norm, bool scale,
                        float *norm, void *ws, hipStream_t stream);
 

@@ -179,7 +179,8 @@ bool entries(int n, const void *const *grads, const long long *count, const int 
         if (!count[i])
             continue;
         e.push_back(GradEntry{grads[i], out ? out[i] : nullptr, count[i], (unsigned)c, types[i]});
-        c += (unsigned long long)((count[i] + kGradChunk - 1) / kGradChunk);
+        const long long most = kGradChunk / (long long)type_size(types[i]);
+        c += (unsigned long long)((count[i] + most - 1) / most);
         if (c >> 31)
             return false;
     }
