@@ -171,8 +171,8 @@ constexpr int kPieces = 64;
 // 137; 1 x 100000 11.5 and 14.0, with 1 10.4; 300 x 40000 fp32 31.0, 30.4 and 32.1).
 constexpr int kFwdPacks = 2;
 
-// Rows cut into `splits` (at most kPieces) pieces of `piece` elements (a multiple of a pack):
-// the moments of each piece to ws[row][split].
+// Rows cut into `splits` (at most kPieces) pieces of `piece` elements (a multiple
+// of a pack): the moments of each piece to ws[row][split].
 template <class T>
 __global__ __launch_bounds__(256) void norm_fwd_pieces(NormFwdArgs a, long long piece, int splits)
 {
@@ -182,8 +182,7 @@ __global__ __launch_bounds__(256) void norm_fwd_pieces(NormFwdArgs a, long long 
     const int split = (int)(blockIdx.x - row * splits);
     const long long first = split * piece;
     const long long end = min(first + piece, a.cols);
-    const T *xr = (const T *)a.x.p + row * a.x.ld;
-    const T *x = xr + first;
+    const T *x = (const T *)a.x.p + row * a.x.ld + first;
     const int len = (int)(end - first);
     Moments m{0.f, 0.f, 0.f};
     for (int c = threadIdx.x * N; c < len; c += F * 256 * N) {
@@ -298,7 +297,8 @@ __global__ __launch_bounds__(256) void norm_fwd_apply(NormFwdArgs a, long long p
 // columns' share of dw and db in registers over the rows of its group.  The
 // groups of a workgroup meet in LDS, the workgroups in
 // parts[workgroup][2][cols], or, if there is one only, it writes dw and db.
-// Elements past the row's end are zeros in dy.
+// Elements past the row's end are zeros in dy (and g u is summed as g (x - mean),
+// whose zero times the finite -mean is 0).
 template <class T, class TW, int NV, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, bool stream)
 {
@@ -366,12 +366,12 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
         for (int i = 0; i < NV; i++)
 #pragma unroll
             for (int j = 0; j < N; j++) {
-                const float d = (float)rd[i][j], u = ((float)rx[i][j] - mean) * rstd;
+                const float d = (float)rd[i][j], off = (float)rx[i][j] - mean;
                 const float g = d * wv[i][j];
-                sw[i][j] += d * u;
+                sw[i][j] += d * (off * rstd);
                 sb[i][j] += d;
                 s1 += g;
-                s2 += g * u;
+                s2 += g * off;
             }
         if (!a.dx.p)
             continue;
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
             }
             turn ^= 1;
         }
-        const float c1 = s1 * inv_n, c2 = s2 * inv_n;
+        const float c1 = s1 * inv_n, c2 = s2 * rstd * inv_n;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const int c = (t + i * tpr) * N;
@@ -533,11 +533,11 @@ __global__ __launch_bounds__(256) void norm_bwd_pieces(NormBwdArgs a, long long 
             for (int j = 0; j < N; j++) {
                 const float g = (float)rd[i][j] * wv[i][j];
                 s1 += g;
-                s2 += g * (((float)rx[i][j] - mean) * rstd);
+                s2 += g * ((float)rx[i][j] - mean);
             }
     }
     s1 = group_reduce(s1, 256, red[0], Add());
-    s2 = group_reduce(s2, 256, red[1], Add());
+    s2 = group_reduce(s2, 256, red[1], Add()) * rstd;
     if (threadIdx.x == 0) {
         float *out = a.ws + ((size_t)row * splits + split) * 2;
         out[0] = s1;

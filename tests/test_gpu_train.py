@@ -179,6 +179,19 @@ def test_layernorm_special_rows(cols):
         assert torch.isfinite(y[r]).all()
 
 
+@pytest.mark.parametrize("cols", [3, 9, 21])
+def test_layernorm_of_large_equal_elements(cols):
+    """|mean| rstd beyond 32 bits: the places past the row's end add nothing."""
+    import paper_1903_06934_amd as m
+    x = torch.full((4, cols), 1e37)
+    dy = randn(gen(cols, 8), 4, cols)
+    y, mean, rstd = m.layernorm_fwd(x.cuda())
+    # Sums of up to 21 equal numbers are off by a few roundings: so is the mean.
+    dx = m.layernorm_bwd(dy.cuda(), x.cuda(), x[:, 0].cuda(), torch.full((4,), 300.0).cuda())[0]
+    want = 300.0 * (dy - dy.double().mean(1, keepdim=True))
+    assert_close(dx, want, 32 * U * 300 * (dy.abs() + 1), "dx")
+
+
 def test_layernorm_gradient_by_differences():
     """dx, dw and db against differences of the forward pass along random
     directions."""
