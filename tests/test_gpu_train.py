@@ -542,6 +542,76 @@ def test_operators_replay_in_a_graph(rows, cols, xt):
         del junk
 
 
+def test_clip_of_many_tensors_in_a_graph():
+    """Lists that go through a table: the graph holds their pointers."""
+    import paper_1903_06934_amd as m
+    g = gen(31)
+    src = [randn(g, int(n)) for n in torch.randint(1, 9000, (250,), generator=g)]
+    grads = [t.cuda() for t in src]
+    out = [torch.empty_like(t) for t in grads]
+    norm, ws = torch.empty(1, device="cuda"), m.grad_workspace(grads)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        m.grad_clip(grads, 3.0, out=out, norm=norm, ws=ws)
+    for rep in range(3):
+        for t, s in zip(grads, src):
+            t.copy_(s * (rep + 1))
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = [torch.empty_like(t) for t in grads]
+        want = m.grad_clip(grads, 3.0, out=eager)
+        assert torch.equal(norm, want)
+        for a, b in zip(out, eager):
+            assert torch.equal(a, b)
+
+
+def test_binding_refuses_on_the_gpu():
+    """Types, layouts and sizes that the binding does not take."""
+    import paper_1903_06934_amd as m
+    x = torch.zeros(4, 8, device="cuda")
+    w, f64 = torch.zeros(8, device="cuda"), torch.zeros(4, 8, device="cuda", dtype=torch.float64)
+    lab = torch.zeros(4, dtype=torch.int64, device="cuda")
+    y, mean, rstd = m.layernorm_fwd(x, w, w)
+    st = m.logprob_fwd(x).stats
+    bad = [
+        lambda: m.layernorm_fwd(f64), lambda: m.layernorm_fwd(x, w[:7]),
+        lambda: m.layernorm_fwd(x, w, w.half()), lambda: m.layernorm_fwd(x, w.cpu()),
+        lambda: m.layernorm_fwd(x, y=y[:3]), lambda: m.layernorm_fwd(x, y=y.half()),
+        lambda: m.layernorm_fwd(x.t()), lambda: m.layernorm_fwd(x, mean=mean[:3]),
+        lambda: m.layernorm_bwd(x.half(), x, mean, rstd), lambda: m.layernorm_bwd(x, x, rstd[:2], rstd),
+        lambda: m.layernorm_bwd(x[:1].expand(4, 8), x, mean, rstd),
+        lambda: m.logprob_fwd(x, lab.int()), lambda: m.logprob_fwd(x, lab[:3]),
+        lambda: m.logprob_bwd(x, st[:3], lab, mean), lambda: m.logprob_bwd(x, st, lab, mean.half()),
+        lambda: m.logprob_bwd(x, st, lab, mean, dlogits=y.half()),
+        lambda: m.grad_clip([x, w.double()], 1.0), lambda: m.grad_clip([x.t()], 1.0),
+        lambda: m.grad_clip([x, "w"], 1.0), lambda: m.grad_clip([x], 1.0, out=[]),
+        lambda: m.grad_clip([x], 1.0, out=[w]), lambda: m.grad_clip([x], 1.0, norm=mean),
+    ]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    refused = [
+        lambda: m.layernorm_fwd(x, y=x), lambda: m.layernorm_fwd(x, eps=-1.0),
+        lambda: m.layernorm_fwd(x.bfloat16(), w.half(), w.half()),
+        lambda: m.layernorm_fwd(x[:, :0]), lambda: m.logprob_fwd(x, scale=0.0),
+        lambda: m.logprob_fwd(x, top=-1), lambda: m.logprob_fwd(torch.zeros(1, 99).cuda(), top=65),
+        lambda: m.logprob_bwd(x, st), lambda: m.logprob_bwd(x, st, dlogp=mean),
+        lambda: m.logprob_bwd(x[:, :7], st, lab, mean, dlogits=x[:, 1:]),
+        lambda: m.grad_clip([w, w], 1.0), lambda: m.grad_clip([w], float("nan")),
+        lambda: m.layernorm_bwd(x, x, mean, rstd, ws=torch.empty(0, device="cuda")),
+    ]
+    for call in refused:
+        with pytest.raises((m.MiconvError, ValueError)):
+            call()
+    # Nothing was launched that left an error behind.
+    torch.cuda.synchronize()
+    assert torch.isfinite(m.layernorm_fwd(x + 1, w, w)[0]).all()
+
+
 def test_operators_on_two_streams():
     import paper_1903_06934_amd as m
     data = [_data(m, 500, 900, BF16, 2), _data(m, 4, 50000, F32, 3)]

@@ -21,7 +21,7 @@ inf, nan = float("inf"), float("nan")
 
 @pytest.fixture(scope="module")
 def L():
-    if not os.path.exists(libbuild.LIBRARY):
+    if not (os.path.exists(libbuild.LIBRARY) and os.path.exists(libbuild.BINDING)):
         libbuild.build()
     return m.lib()
 
@@ -228,7 +228,7 @@ def test_workspace_sizes(L):
         assert L.logprob_fwd_workspace_size(*bad, 0) == 0
 
 
-def test_binding_refuses():
+def test_binding_refuses(L):
     """The binding's own checks, on CPU tensors and layouts that no row stride covers."""
     import torch
     x = torch.zeros(4, 8)
