@@ -111,13 +111,12 @@ __device__ __forceinline__ uint64_t key(float z, uint32_t index)
 // short rows a wave, four of which share a workgroup and never meet.
 template <int SIZE>
 struct Team {
-    static constexpr int kGroups = SIZE < 128 ? SIZE : 128;  // >= MITRAIN_TOP_MAX
-    static constexpr int kPer = SIZE / kGroups;              // threads a group
+    static constexpr int kSize = SIZE;
     static constexpr int kWaves = SIZE / 64;
     static constexpr int kKeys = SIZE < 128 ? 256 : 1024;    // tokens at or above the bound in LDS
 
     struct Shared {
-        alignas(16) float group[kGroups];
+        alignas(16) float group[SIZE < 128 ? 64 : 128];
         Soft soft[kWaves];
         float bound;
         int count, nactive;
@@ -169,30 +168,38 @@ struct Team {
     }
 };
 
-// A lower bound of the k-th largest logit: the k-th largest of the groups'
-// maxima (so at least k elements reach it, and few more where large logits lie
-// anywhere).  mine: the thread's maximum.
+// A lower bound of the k-th largest logit: the k-th largest of the maxima of 64
+// groups of threads, or 128 where a workgroup looks for more than 32 (so at least
+// k elements reach it, and few more where large logits lie anywhere: about
+// -G ln(1 - k / G) of G groups).  mine: the thread's maximum.
 template <class Tm>
 __device__ __forceinline__ float top_bound(typename Tm::Shared &sh, float mine, int k)
 {
     const int t = Tm::thread();
-    const float gm = wave_reduce(mine, Tm::kPer, Max());
-    if (t % Tm::kPer == 0)
-        sh.group[t / Tm::kPer] = gm;
+    const int groups = Tm::kSize > 64 && k > 32 ? 128 : 64, per = Tm::kSize / groups;
+    const float gm = wave_reduce(mine, per, Max());
+    if (t % per == 0)
+        sh.group[t / per] = gm;
     if (t == 0)
         sh.count = sh.nactive = 0;
     Tm::sync();
-    if (t < Tm::kGroups) {
-        const float own = sh.group[t];
-        int above = 0, reach = 0;
+    if (t < 64) {
+        // The largest that k of them reach.
+        float bound = -kInf;
+        for (int g = t; g < groups; g += 64) {
+            const float own = sh.group[g];
+            int reach = 0;
 #pragma unroll 8
-        for (int i = 0; i < Tm::kGroups; i += 4) {
-            const float4 o = *(const float4 *)&sh.group[i];
-            above += (o.x > own) + (o.y > own) + (o.z > own) + (o.w > own);
-            reach += (o.x >= own) + (o.y >= own) + (o.z >= own) + (o.w >= own);
+            for (int i = 0; i < groups; i += 4) {
+                const float4 o = *(const float4 *)&sh.group[i];
+                reach += (o.x >= own) + (o.y >= own) + (o.z >= own) + (o.w >= own);
+            }
+            if (reach >= k)
+                bound = fmaxf(bound, own);
         }
-        if (above < k && reach >= k)
-            sh.bound = own;  // one value, whoever has it
+        bound = wave_reduce(bound, 64, Max());
+        if (t == 0)
+            sh.bound = bound;
     }
     Tm::sync();
     return sh.bound;
@@ -217,7 +224,7 @@ __device__ __forceinline__ void put_ranked(const uint64_t *keys, int n, int k, i
 // Of n keys in LDS, those that can be among the first k: a bound as above from
 // the keys dealt out to the groups, where the first one let many through (a row
 // with elements in few groups).  Ranking them all takes n^2 steps: 2 x 130 bf16
-// with 20 alternatives 14.0 us, so 8.3.  They stay in LDS; returns their number.
+// with 20 alternatives 14.0 us, so 7.9.  They stay in LDS; returns their number.
 template <class Tm, int SIZE>
 __device__ __forceinline__ int fewer_keys(typename Tm::Shared &sh, int n, int k)
 {
@@ -254,27 +261,35 @@ __device__ int count_above(typename Tm::Shared &sh, const T *z, int n, float v)
     return Tm::sum(sh, c);
 }
 
-// The keys of the top k of z[0, n) where too many elements reach the bound
-// (equal logits, or large ones in few threads): the k-th largest value by
-// bisection, then the elements above it, and of those equal to it the first.
+// The keys of the top k of z[0, n) (and of some more, kKeys at most) where too
+// many elements reach the bound: by bisection a larger one that few enough lie
+// above, or, where equal elements stand in the way, the elements above them and
+// of them the first.  Returns the keys' number.
 template <class T, class Tm, int SIZE>
-__device__ __noinline__ void top_by_value(typename Tm::Shared &sh, const T *z, int n,
-                                          uint32_t first, int k, float bound, float most)
+__device__ __noinline__ int top_by_value(typename Tm::Shared &sh, const T *z, int n,
+                                         uint32_t first, int k, float bound, float most)
 {
     constexpr int N = Pack<T>::N;
     uint32_t lo = order(ranked(bound)), hi = order(ranked(most));
-    if (count_above<T, Tm, SIZE>(sh, z, n, bound) < k) {
-        hi = lo;
-    } else {
-        while (hi - lo > 1) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (count_above<T, Tm, SIZE>(sh, z, n, unorder(mid)) < k)
-                hi = mid;
-            else
-                lo = mid;
+    int above = count_above<T, Tm, SIZE>(sh, z, n, bound);
+    bool equal_ones = above < k;  // elements equal to the bound are in the top
+    while (!equal_ones && above > Tm::kKeys) {
+        // k or more lie above lo, fewer above hi.
+        if (hi - lo == 1) {
+            lo = hi;
+            equal_ones = true;
+            break;
+        }
+        const uint32_t mid = lo + (hi - lo) / 2;
+        const int c = count_above<T, Tm, SIZE>(sh, z, n, unorder(mid));
+        if (c < k) {
+            hi = mid;
+        } else {
+            lo = mid;
+            above = c;
         }
     }
-    const float v = unorder(hi);  // fewer than k elements lie above it, k reach it
+    const float v = unorder(lo);
     const int t = Tm::thread();
     Tm::sync();
     if (t == 0)
@@ -289,6 +304,8 @@ __device__ __noinline__ void top_by_value(typename Tm::Shared &sh, const T *z, i
     }
     Tm::sync();
     int have = sh.count;
+    if (!equal_ones)
+        return have;
     for (int base = 0; base < n && have < k; base += SIZE) {
         const int i = base + t;
         const bool equal = i < n && ranked((float)z[i]) == v;
@@ -307,6 +324,7 @@ __device__ __noinline__ void top_by_value(typename Tm::Shared &sh, const T *z, i
             sh.keys[at] = key(v, first + i);
     }
     Tm::sync();
+    return k;
 }
 
 // The sums' results.
@@ -452,12 +470,10 @@ __global__ __launch_bounds__(SIZE < 256 ? 256 : SIZE) void logprob_rows(LogprobA
     }
     Tm::sync();
     int found = sh.count;
-    if (found > Tm::kKeys) {
-        top_by_value<T, Tm, SIZE>(sh, z, n, first, k, bound, p.m);
-        found = k;
-    } else if (found > 2 * k + 8) {
+    if (found > Tm::kKeys)
+        found = top_by_value<T, Tm, SIZE>(sh, z, n, first, k, bound, p.m);
+    if (found > 2 * k + 8)
         found = fewer_keys<Tm, SIZE>(sh, found, k);
-    }
     if (splits == 1)
         put_ranked(sh.keys, found, k, t, SIZE,
                    [&](int rank, uint64_t ky) { put_top(a, row, rank, ky, p, d); });
@@ -580,7 +596,7 @@ int pack_of(int xtype) { return xtype == 0 ? 4 : 8; }
 // Pieces of a row, and the threads of a team.
 // Pieces: with a quarter of the CUs' number of rows or fewer, as many as fill
 // the CUs, of at least 4096 elements, up to kPieces (4 x 131072 bf16 with 20
-// alternatives: 13.9 us, whole rows 17.7; in two pieces 100 rows take 25.3,
+// alternatives: 13.1 us, whole rows 17.7; in two pieces 100 rows take 25.3,
 // whole 19.1: joining them costs 5).
 // A wave a row up to 16 packs a lane (8000 x 1000 bf16 with 5 alternatives:
 // 14.7 us, by workgroups 36.1; 8000 x 4000: 22 and 40), but with fewer rows than

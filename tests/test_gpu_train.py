@@ -354,6 +354,23 @@ def test_top_of_ordered_rows(vocab, kind, rows):
     assert torch.equal(out.top_index.cpu(), want["top_index"].expand(rows, top))
 
 
+@pytest.mark.parametrize("rows", [1, 300])
+@pytest.mark.parametrize("wide,levels", [(256, 0), (600, 0), (256, 40), (600, 3), (1500, 2)])
+@pytest.mark.parametrize("top", [3, 40])
+def test_top_of_many_large_logits_in_few_threads(rows, wide, levels, top):
+    """More logits above the rest than are held at once, all different or of a few
+    values, where the threads' maxima say little."""
+    import paper_1903_06934_amd as m
+    j = torch.arange(50000)
+    large = 1 + torch.rand(50000, generator=gen(wide), dtype=torch.float64)
+    if levels:
+        large = torch.round(large * levels) / levels
+    z = torch.where(j % 2048 < wide, large, -(j % 7).double()).float().repeat(rows, 1)
+    out = m.logprob_fwd(z.cuda(), top=top)
+    want = ref.logprob_fwd(z[:1], None, top)
+    assert torch.equal(out.top_index.cpu(), want["top_index"].expand(rows, top))
+
+
 @pytest.mark.parametrize("vocab", [1, 2, 7, 33, 63, 64])
 @pytest.mark.parametrize("rows", [1, 700])
 def test_top_of_the_whole_row(vocab, rows):
