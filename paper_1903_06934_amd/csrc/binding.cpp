@@ -144,22 +144,22 @@ Tensor empty(at::IntArrayRef sizes, const Tensor &x, at::ScalarType type)
     return at::empty(sizes, x.options().dtype(type));
 }
 
-// Small results side by side in one buffer: its allocation takes the host longer
-// than the views.
+// Small float results side by side in one buffer: its allocation takes the host
+// longer than the views.  Only floats: tensors of several types in one storage
+// cannot be saved together.
 struct Results {
-    Tensor bytes;
+    Tensor floats;
     int64_t used = 0;
 
-    Results(int64_t size, const Tensor &x) : bytes(empty({size}, x, at::kByte)) {}
+    Results(int64_t n, const Tensor &x) : floats(empty({n}, x, at::kFloat)) {}
 
-    // The next tensor; the ones of larger elements come first.
-    Tensor next(at::IntArrayRef sizes, at::ScalarType type)
+    Tensor next(at::IntArrayRef sizes)
     {
         Tensor t = at::detail::make_tensor<c10::TensorImpl>(
-            c10::Storage(bytes.storage()), bytes.key_set(), c10::scalarTypeToTypeMeta(type));
-        t.unsafeGetTensorImpl()->set_storage_offset(used / (int64_t)c10::elementSize(type));
+            c10::Storage(floats.storage()), floats.key_set(), floats.dtype());
+        t.unsafeGetTensorImpl()->set_storage_offset(used);
         t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
-        used += t.numel() * (int64_t)c10::elementSize(type);
+        used += t.numel();
         return t;
     }
 };
@@ -218,9 +218,9 @@ std::tuple<Tensor, Tensor, Tensor> layernorm_forward(const Tensor &x, const Mayb
         mean = *mean_;
         rstd = *rstd_;
     } else {
-        Results out(8 * r.rows, x);
-        mean = mean_ ? *mean_ : out.next({r.rows}, at::kFloat);
-        rstd = rstd_ ? *rstd_ : out.next({r.rows}, at::kFloat);
+        Results out(2 * r.rows, x);
+        mean = mean_ ? *mean_ : out.next({r.rows});
+        rstd = rstd_ ? *rstd_ : out.next({r.rows});
     }
     const Workspace s(ws, lib.layernorm_fwd_ws(type, r.rows, r.cols), x.device());
     call(lib.layernorm_fwd(type, w ? type_of(*w) : b ? type_of(*b) : type, r.rows, r.cols,
@@ -296,16 +296,16 @@ std::tuple<Maybe, Tensor, Tensor, Tensor, Maybe, Maybe> logprob_forward(const Te
     };
     if (top < 0)
         call(MICONV_ERR_SHAPE, "logprob_fwd");
-    Results out(r.rows * (20 + 12LL * top), z);
+    Results out(r.rows * (5LL + top), z);
     Maybe logp, top_logp, top_index;
-    if (top) {
-        top_index = out.next(last(top), at::kLong);
-        top_logp = out.next(last(top), at::kFloat);
-    }
-    const Tensor lse = out.next(shape, at::kFloat), entropy = out.next(shape, at::kFloat);
-    const Tensor stats = out.next(last(2), at::kFloat);
+    const Tensor stats = out.next(last(2));
+    const Tensor lse = out.next(shape), entropy = out.next(shape);
     if (targets)
-        logp = out.next(shape, at::kFloat);
+        logp = out.next(shape);
+    if (top) {
+        top_logp = out.next(last(top));
+        top_index = empty(last(top), z, at::kLong);
+    }
     const Workspace s(ws, lib.logprob_fwd_ws(type, r.rows, r.cols, top), z.device());
     const auto at = [](const Maybe &t) { return t ? t->data_ptr() : nullptr; };
     call(lib.logprob_fwd(type, r.rows, r.cols, z.data_ptr(), r.ld, tp, (float)scale, top,

@@ -390,6 +390,35 @@ def test_top_of_the_whole_row(vocab, rows):
     assert torch.equal(cube.top_logp[:, 0], out.top_logp)
 
 
+@pytest.mark.parametrize("inference", [False, True])
+def test_results_are_ordinary_tensors(inference):
+    """Results that share a buffer: written in place, differentiated, saved apart."""
+    import io
+
+    import paper_1903_06934_amd as m
+    z = randn(gen(77), 6, 50)
+    with torch.inference_mode(inference):
+        out = m.logprob_fwd(z.cuda(), torch.arange(6, device="cuda"), top=3)
+        again = m.logprob_fwd(z.cuda(), torch.arange(6, device="cuda"), top=3)
+        _, mean, rstd = m.layernorm_fwd(z.cuda())
+        both = mean.clone(), rstd.clone()
+        mean.zero_()
+        assert torch.equal(rstd, both[1])
+        for i, t in enumerate(out):
+            t.fill_(7)
+            for j, (u, v) in enumerate(zip(out, again)):
+                assert torch.equal(u, v) == (j > i)
+    if not inference:
+        w = again.logp.requires_grad_()
+        (w * w).sum().backward()
+        assert torch.allclose(w.grad, 2 * w.detach())
+    buf = io.BytesIO()
+    torch.save([t.detach() for t in again], buf)
+    buf.seek(0)
+    for t, s in zip(torch.load(buf, weights_only=True), again):
+        assert torch.equal(t, s)
+
+
 def test_logprob_far_from_zero():
     """Logits around 20000: log probabilities and gradient keep their own size's
     accuracy."""
