@@ -52,7 +52,9 @@ __device__ __forceinline__ void load_weights(const TW *w, long long c, long long
 // waves) holds a row: thread t the vectors t, t + tpr, ..., NV of them.
 // The variance is taken about the mean, from the registers.  Groups take row
 // after row; HOLD: with their weights and biases in registers.
-template <class T, class TW, int NV, bool HOLD, int BLOCK>
+// TAIL: all packs are whole, and beside them a thread holds one element of the
+// row's last tpr places, some of which may be missing.
+template <class T, class TW, int NV, bool TAIL, bool HOLD, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, bool stream)
 {
     constexpr int N = Pack<T>::N;
@@ -62,13 +64,18 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, b
     const int t = tpr > 64 ? threadIdx.x : threadIdx.x & (tpr - 1);
     const int groups = blockDim.x / tpr;
     const float n = (float)cols;
-    float wv[HOLD ? NV : 1][N], bv[HOLD ? NV : 1][N];
+    const int last = NV * N * tpr + t;  // the column beside the packs
+    float wv[HOLD ? NV : 1][N], bv[HOLD ? NV : 1][N], w1 = 1.f, b1 = 0.f;
     if constexpr (HOLD)
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             load_weights<N>(w, (t + i * tpr) * N, cols, 1.f, wv[i]);
             load_weights<N>(b, (t + i * tpr) * N, cols, 0.f, bv[i]);
         }
+    if constexpr (TAIL) {
+        load_weights<1>(w, last, cols, 1.f, &w1);
+        load_weights<1>(b, last, cols, 0.f, &b1);
+    }
     int turn = 0;
     for (long long row = (long long)blockIdx.x * groups + threadIdx.x / tpr; row < a.rows;
          row += (long long)gridDim.x * groups) {
@@ -77,15 +84,17 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, b
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const int c = (t + i * tpr) * N;
+            const int left = TAIL ? N : cols - c;
             raw[i] = typename Pack<T>::V{};
-            if (c < cols) {
+            if (left > 0) {
                 if (stream)
-                    raw[i] = load_pack<T, true>(xr + c, cols - c, (T)0.f);
+                    raw[i] = load_pack<T, true>(xr + c, left, (T)0.f);
                 else
-                    raw[i] = load_pack<T>(xr + c, cols - c, (T)0.f);
+                    raw[i] = load_pack<T>(xr + c, left, (T)0.f);
             }
         }
-        float s = 0.f;
+        const float x1 = TAIL && last < cols ? (float)xr[last] : 0.f;
+        float s = x1;
 #pragma unroll
         for (int i = 0; i < NV; i++)
 #pragma unroll
@@ -95,7 +104,7 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, b
         float q = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
-            const int left = cols - (t + i * tpr) * N;
+            const int left = TAIL ? N : cols - (t + i * tpr) * N;
             if (left >= N) {
 #pragma unroll
                 for (int j = 0; j < N; j++) {
@@ -110,6 +119,8 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, b
                 }
             }
         }
+        if (TAIL)
+            q += last < cols ? (x1 - mean) * (x1 - mean) : 0.f;
         const float var = group_reduce(q, tpr, red[turn][1], Add()) / n;
         turn ^= 1;
         const float rstd = 1.f / sqrtf(var + a.eps);
@@ -123,7 +134,8 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, b
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const int c = (t + i * tpr) * N, h = HOLD ? i : 0;
-            if (c >= cols)
+            const int left = TAIL ? N : cols - c;
+            if (left <= 0)
                 continue;
             if constexpr (!HOLD) {
                 load_weights<N>(w, c, cols, 1.f, wv[0]);
@@ -133,8 +145,10 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, b
 #pragma unroll
             for (int j = 0; j < N; j++)
                 v[j] = (T)(((float)raw[i][j] - mean) * rstd * wv[h][j] + bv[h][j]);
-            store_pack<T>(yr + c, cols - c, v);
+            store_pack<T>(yr + c, left, v);
         }
+        if (TAIL && last < cols)
+            yr[last] = (T)((x1 - mean) * rstd * w1 + b1);
     }
 }
 
@@ -299,25 +313,28 @@ __global__ __launch_bounds__(256) void norm_fwd_apply(NormFwdArgs a, long long p
 // parts[workgroup][2][cols], or, if there is one only, it writes dw and db.
 // Elements past the row's end are zeros in dy (and g u is summed as g (x - mean),
 // whose zero times the finite -mean is 0).
-template <class T, class TW, int NV, int BLOCK>
+template <class T, class TW, int NV, bool TAIL, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, bool stream)
 {
-    constexpr int N = Pack<T>::N;
+    constexpr int N = Pack<T>::N, K = NV * N + TAIL;  // elements a thread
     extern __shared__ float lds[];
     __shared__ float red[2][2][16];
     const int cols = (int)a.cols;
     const int t = tpr > 64 ? threadIdx.x : threadIdx.x & (tpr - 1);
     const int groups = blockDim.x / tpr, group = tpr > 64 ? 0 : threadIdx.x / tpr;
+    const int last = NV * N * tpr + t;  // the column beside the packs
     const float inv_n = 1.f / (float)cols;
-    float wv[NV][N], sw[NV][N], sb[NV][N];
+    float wv[K], sw[K], sb[K];
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        load_weights<N>((const TW *)a.w, (t + i * tpr) * N, cols, 1.f, wv[i]);
+    for (int i = 0; i < NV; i++)
+        load_weights<N>((const TW *)a.w, (t + i * tpr) * N, cols, 1.f, wv + i * N);
+    if (TAIL)
+        load_weights<1>((const TW *)a.w, last, cols, 1.f, wv + NV * N);
 #pragma unroll
-        for (int j = 0; j < N; j++)
-            sw[i][j] = sb[i][j] = 0.f;
-    }
+    for (int i = 0; i < K; i++)
+        sw[i] = sb[i] = 0.f;
     typename Pack<T>::V rx[NV], rd[NV], nx[NV], nd[NV];
+    T rx1 = (T)0.f, rd1 = (T)0.f, nx1 = (T)0.f, nd1 = (T)0.f;
     float mean = 0.f, rstd = 0.f, nmean = 0.f, nrstd = 0.f;
     const long long step = (long long)gridDim.x * groups;
     long long row = (long long)blockIdx.x * groups + group;
@@ -332,16 +349,21 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const int c = (t + i * tpr) * N;
+            const int left = TAIL ? N : cols - c;
             nx[i] = nd[i] = typename Pack<T>::V{};
-            if (c < cols) {
+            if (left > 0) {
                 if (stream) {
-                    nx[i] = load_pack<T, true>(xr + c, cols - c, (T)0.f);
-                    nd[i] = load_pack<T, true>(dyr + c, cols - c, (T)0.f);
+                    nx[i] = load_pack<T, true>(xr + c, left, (T)0.f);
+                    nd[i] = load_pack<T, true>(dyr + c, left, (T)0.f);
                 } else {
-                    nx[i] = load_pack<T>(xr + c, cols - c, (T)0.f);
-                    nd[i] = load_pack<T>(dyr + c, cols - c, (T)0.f);
+                    nx[i] = load_pack<T>(xr + c, left, (T)0.f);
+                    nd[i] = load_pack<T>(dyr + c, left, (T)0.f);
                 }
             }
+        }
+        if (TAIL && last < cols) {
+            nx1 = xr[last];
+            nd1 = dyr[last];
         }
         nmean = *meanr;
         nrstd = *rstdr;
@@ -358,21 +380,26 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
             rx[i] = nx[i];
             rd[i] = nd[i];
         }
+        rx1 = nx1;
+        rd1 = nd1;
         mean = nmean;
         rstd = nrstd;
         load(row + step);
         float s1 = 0.f, s2 = 0.f;
+        const auto sum = [&](int k, float d, float off) {
+            const float g = d * wv[k];
+            sw[k] += d * (off * rstd);
+            sb[k] += d;
+            s1 += g;
+            s2 += g * off;
+        };
 #pragma unroll
         for (int i = 0; i < NV; i++)
 #pragma unroll
-            for (int j = 0; j < N; j++) {
-                const float d = (float)rd[i][j], off = (float)rx[i][j] - mean;
-                const float g = d * wv[i][j];
-                sw[i][j] += d * (off * rstd);
-                sb[i][j] += d;
-                s1 += g;
-                s2 += g * off;
-            }
+            for (int j = 0; j < N; j++)
+                sum(i * N + j, (float)rd[i][j], (float)rx[i][j] - mean);
+        if (TAIL)
+            sum(NV * N, (float)rd1, (float)rx1 - mean);
         if (!a.dx.p)
             continue;
         s1 = wave_reduce(s1, tpr, Add());
@@ -392,19 +419,23 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
             turn ^= 1;
         }
         const float c1 = s1 * inv_n, c2 = s2 * rstd * inv_n;
+        const auto result = [&](int k, T d, T x) {
+            return (T)(rstd * ((float)d * wv[k] - c1 - ((float)x - mean) * rstd * c2));
+        };
 #pragma unroll
         for (int i = 0; i < NV; i++) {
             const int c = (t + i * tpr) * N;
-            if (c >= cols)
+            const int left = TAIL ? N : cols - c;
+            if (left <= 0)
                 continue;
             typename Pack<T>::V v;
 #pragma unroll
-            for (int j = 0; j < N; j++) {
-                const float d = (float)rd[i][j], u = ((float)rx[i][j] - mean) * rstd;
-                v[j] = (T)(rstd * (d * wv[i][j] - c1 - u * c2));
-            }
-            store_pack<T>(dxr + c, cols - c, v);
+            for (int j = 0; j < N; j++)
+                v[j] = result(i * N + j, rd[i][j], rx[i][j]);
+            store_pack<T>(dxr + c, left, v);
         }
+        if (TAIL && last < cols)
+            dxr[last] = result(NV * N, rd1, rx1);
         dxr += dx_step;
     }
     if (!a.dw && !a.db)
@@ -422,23 +453,21 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
         if (groups > 1)
             __syncthreads();
 #pragma unroll
-        for (int i = 0; i < NV; i++)
-#pragma unroll
-            for (int j = 0; j < N; j++) {
-                const int c = (t + i * tpr) * N + j;
-                const float v = k ? sb[i][j] : sw[i][j];
-                if (groups > 1)
-                    lds[group * tpr * NV * N + c] = v;
-                else if (c < cols)
-                    put(k, c, v);
-            }
+        for (int i = 0; i < K; i++) {
+            const int c = i < NV * N ? (t + i / N * tpr) * N + i % N : last;
+            const float v = k ? sb[i] : sw[i];
+            if (groups > 1)
+                lds[group * tpr * K + c] = v;
+            else if (c < cols)
+                put(k, c, v);
+        }
         if (groups == 1)
             continue;
         __syncthreads();
         for (int c = threadIdx.x; c < cols; c += blockDim.x) {
             float v = lds[c];
             for (int g = 1; g < groups; g++)
-                v += lds[g * tpr * NV * N + c];
+                v += lds[g * tpr * K + c];
             put(k, c, v);
         }
     }
@@ -665,10 +694,11 @@ size_t up16(size_t v) { return (v + 15) / 16 * 16; }
 // twice as many without.
 constexpr int kValues = 16;
 
-// Threads a row, packs a thread and threads a workgroup of the register
-// kernels; nv = 0: the row is too long for them.
+// Threads a row, packs a thread, threads a workgroup and the form of the last
+// places of the register kernels; nv = 0: the row is too long for them.
 struct RowPlan {
     int tpr, nv, block;
+    bool tail;
 };
 
 RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
@@ -678,7 +708,7 @@ RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
     // Few rows above 16384 elements: by pieces over more CUs (16 x 32768 bf16
     // 9.5 us, by registers 10.8; 256 rows 18.4 and 13.2).
     if (forward && cols > 16384 && rows <= 64)
-        return RowPlan{0, 0, 0};
+        return RowPlan{0, 0, 0, false};
     // Backward by pieces above 8192 elements (1024 threads have too few registers:
     // 4096 x 16384 fp32 285 us, by pieces 232; bf16 113 and 121), and where the
     // rows' partial sums of dw and db would be about as many as their elements:
@@ -689,12 +719,12 @@ RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
     const bool sums = n == 4 ? cols >= 4096 && rows <= 512
                              : rows <= 2048 && cols >= (rows < 256 ? 4096 : 2048);
     if (!forward && (cols > 8192 || sums))
-        return RowPlan{0, 0, 0};
+        return RowPlan{0, 0, 0, false};
     if (packs <= 64) {
         int tpr = 1;
         while (packs > tpr)
             tpr *= 2;
-        return RowPlan{tpr, 1, 256};
+        return RowPlan{tpr, 1, 256, false};
     }
     // As few idle places as can be; then more packs a thread before more
     // threads, as a row inside a wave needs no barrier.  Forward, few rows are
@@ -716,10 +746,27 @@ RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
     if (!best) {
         best = 2 * kValues / n;
         if (!forward || waves(best) > most)
-            return RowPlan{0, 0, 0};
+            return RowPlan{0, 0, 0, false};
     }
     const int tpr = 64 * (int)waves(best);
-    return RowPlan{tpr, best, tpr > 64 ? tpr : 256};
+    RowPlan p{tpr, best, tpr > 64 ? tpr : 256, false};
+    if (forward && rows * waves(best) <= 8LL * num_cus())
+        return p;
+    // A row a little longer than whole packs of all its threads: one element a
+    // thread beside them instead of a pack, where a thread then holds fewer places
+    // and the row takes no more threads (forward 12544 x 1025 bf16 12.3 us, by packs
+    // 18.1; 9000 x 3080 fp32 51.0 and 82.0; 4000 x 2049 fp32 14.6 and 14.2. Backward
+    // 12544 x 513 fp32 21.0 and 22.9; 9000 x 3073 f16 55.2 and 68.9).  Not backward
+    // over several waves in fp32 (9000 x 2049 55.8 and 49.8).
+    int cost = tpr / 64 * best * n;
+    for (int nv = 1; nv * n <= kValues; nv++)
+        for (int w = 1; w <= (!forward && n == 4 ? 1 : tpr / 64); w++)
+            if (64LL * w * nv * n <= cols && cols <= 64LL * w * (nv * n + 1) &&
+                w * (nv * n + 1) < cost) {
+                cost = w * (nv * n + 1);
+                p = RowPlan{64 * w, nv, w > 1 ? 64 * w : 256, true};
+            }
+    return p;
 }
 
 // Workgroups of the register kernels.  Forward: 1536 threads a CU (16384 rows
@@ -793,15 +840,24 @@ int row_chunks(int xtype, long long rows, long long cols)
     return rows <= 64 ? 1 : (int)std::max(1LL, std::min(want, rows / 16));
 }
 
-template <class T, class TW, int NV, bool HOLD>
+template <class T, class TW, int NV, bool TAIL, bool HOLD>
 void fwd_rows(const NormFwdArgs &a, const RowPlan &p, hipStream_t stream)
 {
     const int n = fwd_blocks(p, a.rows);
     const bool through = streams(a.rows, a.cols, sizeof(T), {a.x});
     if (p.block <= 256)
-        norm_fwd_rows<T, TW, NV, HOLD, 256><<<n, p.block, 0, stream>>>(a, p.tpr, through);
+        norm_fwd_rows<T, TW, NV, TAIL, HOLD, 256><<<n, p.block, 0, stream>>>(a, p.tpr, through);
     else
-        norm_fwd_rows<T, TW, NV, HOLD, 1024><<<n, p.block, 0, stream>>>(a, p.tpr, through);
+        norm_fwd_rows<T, TW, NV, TAIL, HOLD, 1024><<<n, p.block, 0, stream>>>(a, p.tpr, through);
+}
+
+template <class T, class TW, int NV>
+void fwd_rows(const NormFwdArgs &a, const RowPlan &p, hipStream_t stream)
+{
+    if (p.tail)
+        fwd_rows<T, TW, NV, true, true>(a, p, stream);
+    else
+        fwd_rows<T, TW, NV, false, true>(a, p, stream);
 }
 
 template <class T, class TW>
@@ -812,15 +868,15 @@ hipError_t fwd(int xtype, const NormFwdArgs &a, hipStream_t stream)
         return hipSuccess;
     const RowPlan p = row_plan(xtype, a.rows, a.cols, true);
     if (p.nv == 1)
-        fwd_rows<T, TW, 1, true>(a, p, stream);
+        fwd_rows<T, TW, 1>(a, p, stream);
     else if (p.nv == 2)
-        fwd_rows<T, TW, 2, true>(a, p, stream);
+        fwd_rows<T, TW, 2>(a, p, stream);
     else if (p.nv == 3 && N == 4)
-        fwd_rows<T, TW, N == 4 ? 3 : 1, true>(a, p, stream);
+        fwd_rows<T, TW, N == 4 ? 3 : 1>(a, p, stream);
     else if (p.nv == 4 && N == 4)
-        fwd_rows<T, TW, kValues / N, true>(a, p, stream);
+        fwd_rows<T, TW, kValues / N>(a, p, stream);
     else if (p.nv)
-        fwd_rows<T, TW, 2 * kValues / N, false>(a, p, stream);
+        fwd_rows<T, TW, 2 * kValues / N, false, false>(a, p, stream);
     if (p.nv)
         return hipGetLastError();
     // rows * cols is below 2^37 and a row above 2^15: below 2^23 workgroups.
@@ -831,16 +887,25 @@ hipError_t fwd(int xtype, const NormFwdArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-template <class T, class TW, int NV>
+template <class T, class TW, int NV, bool TAIL>
 void bwd_rows(const NormBwdArgs &a, const RowPlan &p, int n, hipStream_t stream)
 {
     const size_t lds =
-        p.block > p.tpr ? (size_t)p.block * NV * Pack<T>::N * sizeof(float) : 0;
+        p.block > p.tpr ? (size_t)p.block * (NV * Pack<T>::N + TAIL) * sizeof(float) : 0;
     const bool through = streams(a.rows, a.cols, sizeof(T), {a.x, a.dy});
     if (p.block <= 256)
-        norm_bwd_rows<T, TW, NV, 256><<<n, p.block, lds, stream>>>(a, p.tpr, through);
+        norm_bwd_rows<T, TW, NV, TAIL, 256><<<n, p.block, lds, stream>>>(a, p.tpr, through);
     else
-        norm_bwd_rows<T, TW, NV, 512><<<n, p.block, lds, stream>>>(a, p.tpr, through);
+        norm_bwd_rows<T, TW, NV, TAIL, 512><<<n, p.block, lds, stream>>>(a, p.tpr, through);
+}
+
+template <class T, class TW, int NV>
+void bwd_rows(const NormBwdArgs &a, const RowPlan &p, int n, hipStream_t stream)
+{
+    if (p.tail)
+        bwd_rows<T, TW, NV, true>(a, p, n, stream);
+    else
+        bwd_rows<T, TW, NV, false>(a, p, n, stream);
 }
 
 template <class T, class TW>

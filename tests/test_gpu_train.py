@@ -128,6 +128,36 @@ def test_layernorm_row_lengths(rows, xt):
             assert_close(got, val, 300 * U * mag + half_ulp(val, xt) * 1.01, f"{name} {cols}")
 
 
+@pytest.mark.parametrize("xt", [F32, BF16, F16])
+@pytest.mark.parametrize("cols", [256, 257, 320, 321, 513, 576, 769, 1025, 1088, 1089, 2049, 2176,
+                                  3080, 4100])
+def test_layernorm_row_tails(cols, xt):
+    """Many rows some elements longer than whole vectors of a wave or some waves:
+    the elements beside them, and what lies beside the rows."""
+    import paper_1903_06934_amd as m
+    rows = 2100
+    g = gen(cols, 31)
+    x, dy = randn(g, rows, cols).to(xt), randn(g, rows, cols).to(xt)
+    w, b = randn(g, cols), randn(g, cols)
+    xv, _ = strided(x, 3, 1)
+    dyv, _ = strided(dy, 0, 1)
+    yv, wide = strided(torch.zeros(rows, cols, dtype=xt), 1, 2)
+    y, mean, rstd = m.layernorm_fwd(xv, w.cuda(), b.cuda(), y=yv)
+    ry, rmean, rrstd, size, msize = ref.layernorm_fwd(x, w, b)
+    k = norm_terms(cols) * U
+    assert_close(mean, rmean, k * msize, "mean")
+    assert_close(rstd, rrstd, rrstd * (k + (k * msize * rrstd) ** 2), "rstd")
+    assert_close(y, ry, 2 * k * size + half_ulp(ry, xt) * 1.01, "y")
+    untouched(yv, wide)
+    dxv, wide = strided(torch.zeros(rows, cols, dtype=xt), 2, 1)
+    dx, dw, db = m.layernorm_bwd(dyv, xv, mean, rstd, w.cuda(), dx=dxv)
+    want = ref.layernorm_bwd(dy, x, mean.cpu(), rstd.cpu(), w)
+    assert_close(dx, want[0][0], k * want[0][1] + half_ulp(want[0][0], xt) * 1.01, "dx")
+    untouched(dxv, wide)
+    for got, (val, mag), name in ((dw, want[1], "dw"), (db, want[2], "db")):
+        assert_close(got, val, (300 + rows / 256) * U * mag, name)
+
+
 @pytest.mark.parametrize("rows", [0, 1, 2, 255, 4097])
 @pytest.mark.parametrize("cols,xt", [(48, BF16), (513, F32), (3000, BF16), (40000, F32)])
 def test_layernorm_rows(rows, cols, xt):
