@@ -129,8 +129,9 @@ def test_layernorm_row_lengths(rows, xt):
 
 
 @pytest.mark.parametrize("xt", [F32, BF16, F16])
-@pytest.mark.parametrize("cols", [256, 257, 320, 321, 513, 576, 769, 1025, 1088, 1089, 2049, 2176,
-                                  3080, 4100])
+@pytest.mark.parametrize("cols", [5, 9, 10, 33, 69, 80, 81, 130, 140, 144, 145, 256, 257, 288,
+                                  320, 321, 513, 576, 769, 1025, 1088, 1089, 2049, 2176, 3080,
+                                  4100])
 def test_layernorm_row_tails(cols, xt):
     """Many rows some elements longer than whole vectors of a wave or some waves:
     the elements beside them, and what lies beside the rows."""
