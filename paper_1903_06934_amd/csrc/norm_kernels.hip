@@ -19,6 +19,89 @@ namespace miconv {
 
 namespace {
 
+// A pack that the row's end cuts short holds the elements that are left in
+// halves: of 8 places the first four a half pack's (if four are left at least),
+// the next two a quarter's, the seventh a single one.  Each is one load or store
+// of whole registers; element by element two of 16 bits would meet in a register,
+// for which the loads have to be waited for where they are issued, and all loads
+// before them (16009 x 4369 f16 backward 127 us, element by element 195; forward
+// 82 and 97).
+// place: the element of place j in a pack of which `left` (>= 1) are left, or -1.
+template <int N>
+__device__ __forceinline__ int place(int j, int left)
+{
+    if (left >= N)
+        return j;
+#pragma unroll
+    for (int h = N / 2, at = 0, from = 0; h; h /= 2) {
+        if (j < at + h)
+            return (left & h) ? from + j - at : -1;
+        at += h;
+        from += left & h;
+    }
+    return -1;
+}
+
+// Register parts of a pack, and as they lie in memory.
+template <class T, int H>
+struct Part {
+    typedef T V __attribute__((ext_vector_type(H)));
+    typedef V At __attribute__((aligned(sizeof(T))));
+};
+
+// The elements at p of which `left` (>= 1) are in the row, the others 0.
+template <class T, bool STREAM = false>
+__device__ __forceinline__ typename Pack<T>::V load_places(const T *p, int left)
+{
+    constexpr int N = Pack<T>::N;
+    if (left >= N) {
+        const auto *at = (const typename Pack<T>::At *)p;
+        return STREAM ? __builtin_nontemporal_load(at) : *at;
+    }
+    uint32_t r[4] = {0, 0, 0, 0};
+    if (left & (N / 2)) {
+        const auto v = __builtin_bit_cast(uint2, *(const typename Part<T, N / 2>::At *)p);
+        r[0] = v.x;
+        r[1] = v.y;
+        p += N / 2;
+    }
+    if constexpr (N == 8) {
+        if (left & 2) {
+            r[2] = __builtin_bit_cast(uint32_t, *(const typename Part<T, 2>::At *)p);
+            p += 2;
+        }
+        if (left & 1)
+            r[3] = __builtin_bit_cast(uint16_t, *p);
+    } else if (left & 1) {
+        r[2] = __builtin_bit_cast(uint32_t, *p);
+    }
+    return __builtin_bit_cast(typename Pack<T>::V, r);
+}
+
+template <class T>
+__device__ __forceinline__ void store_places(T *p, int left, typename Pack<T>::V v)
+{
+    constexpr int N = Pack<T>::N;
+    if (left >= N) {
+        __builtin_nontemporal_store(v, (typename Pack<T>::At *)p);
+        return;
+    }
+    if (left & (N / 2)) {
+        if constexpr (N == 8)
+            *(typename Part<T, 4>::At *)p = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+        else
+            *(typename Part<T, 2>::At *)p = __builtin_shufflevector(v, v, 0, 1);
+        p += N / 2;
+    }
+    if constexpr (N == 8)
+        if (left & 2) {
+            *(typename Part<T, 2>::At *)p = __builtin_shufflevector(v, v, 4, 5);
+            p += 2;
+        }
+    if (left & 1)
+        *p = v[N - 2];
+}
+
 // The N weights at column c of a row of cols (`none` without weights).
 template <int N, class TW>
 __device__ __forceinline__ void load_weights(const TW *w, long long c, long long cols, float none,
@@ -40,10 +123,17 @@ __device__ __forceinline__ void load_weights(const TW *w, long long c, long long
                 f[i + j] = (float)v[j];
         }
     } else {
+        const int left = (int)(cols - c);
+        const TW *p = w + c;
+        int at = 0;
 #pragma unroll
-        for (int j = 0; j < N; j++)
-            if (c + j < cols)
-                f[j] = (float)w[c + j];
+        for (int h = N / 2; h; at += h, h /= 2)
+            if (left & h) {
+#pragma unroll
+                for (int j = 0; j < h; j++)
+                    f[at + j] = (float)p[j];
+                p += h;
+            }
     }
 }
 
@@ -88,9 +178,9 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, b
             raw[i] = typename Pack<T>::V{};
             if (left > 0) {
                 if (stream)
-                    raw[i] = load_pack<T, true>(xr + c, left, (T)0.f);
+                    raw[i] = load_places<T, true>(xr + c, left);
                 else
-                    raw[i] = load_pack<T>(xr + c, left, (T)0.f);
+                    raw[i] = load_places<T>(xr + c, left);
             }
         }
         const float x1 = TAIL && last < cols ? (float)xr[last] : 0.f;
@@ -115,7 +205,7 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, b
 #pragma unroll
                 for (int j = 0; j < N; j++) {
                     const float d = (float)raw[i][j] - mean;
-                    q += j < left ? d * d : 0.f;
+                    q += left > 0 && place<N>(j, left) >= 0 ? d * d : 0.f;
                 }
             }
         }
@@ -145,7 +235,7 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(NormFwdArgs a, int tpr, b
 #pragma unroll
             for (int j = 0; j < N; j++)
                 v[j] = (T)(((float)raw[i][j] - mean) * rstd * wv[h][j] + bv[h][j]);
-            store_pack<T>(yr + c, left, v);
+            store_places<T>(yr + c, left, v);
         }
         if (TAIL && last < cols)
             yr[last] = (T)((x1 - mean) * rstd * w1 + b1);
@@ -206,7 +296,7 @@ __global__ __launch_bounds__(256) void norm_fwd_pieces(NormFwdArgs a, long long 
             const int at = c + i * 256 * N;
             raw[i] = typename Pack<T>::V{};
             if (at < len)
-                raw[i] = load_pack<T>(x + at, len - at, (T)0.f);
+                raw[i] = load_places<T>(x + at, len - at);
         }
         float s = 0.f, q = 0.f;
 #pragma unroll
@@ -235,7 +325,8 @@ __global__ __launch_bounds__(256) void norm_fwd_pieces(NormFwdArgs a, long long 
 #pragma unroll
                 for (int j = 0; j < N; j++) {
                     const float d = (float)raw[i][j] - mean;
-                    q += c + i * 256 * N + j < len ? d * d : 0.f;
+                    const int left = len - c - i * 256 * N;
+                    q += left > 0 && place<N>(j, left) >= 0 ? d * d : 0.f;
                 }
             m = merge(m, Moments{(float)n, mean, q});
         }
@@ -287,7 +378,7 @@ __global__ __launch_bounds__(256) void norm_fwd_apply(NormFwdArgs a, long long p
             const int c = c0 + i * 256 * N;
             raw[i] = typename Pack<T>::V{};
             if (c < len)
-                raw[i] = load_pack<T>(x + c, len - c, (T)0.f);
+                raw[i] = load_places<T>(x + c, len - c);
             load_weights<N>(w, first + c, end, 1.f, wv[i]);
             load_weights<N>(b, first + c, end, 0.f, bv[i]);
         }
@@ -300,7 +391,7 @@ __global__ __launch_bounds__(256) void norm_fwd_apply(NormFwdArgs a, long long p
 #pragma unroll
             for (int j = 0; j < N; j++)
                 v[j] = (T)(((float)raw[i][j] - mean) * rstd * wv[i][j] + bv[i][j]);
-            store_pack<T>(y + c, len - c, v);
+            store_places<T>(y + c, len - c, v);
         }
     }
 }
@@ -353,11 +444,11 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
             nx[i] = nd[i] = typename Pack<T>::V{};
             if (left > 0) {
                 if (stream) {
-                    nx[i] = load_pack<T, true>(xr + c, left, (T)0.f);
-                    nd[i] = load_pack<T, true>(dyr + c, left, (T)0.f);
+                    nx[i] = load_places<T, true>(xr + c, left);
+                    nd[i] = load_places<T, true>(dyr + c, left);
                 } else {
-                    nx[i] = load_pack<T>(xr + c, left, (T)0.f);
-                    nd[i] = load_pack<T>(dyr + c, left, (T)0.f);
+                    nx[i] = load_places<T>(xr + c, left);
+                    nd[i] = load_places<T>(dyr + c, left);
                 }
             }
         }
@@ -432,7 +523,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
 #pragma unroll
             for (int j = 0; j < N; j++)
                 v[j] = result(i * N + j, rd[i][j], rx[i][j]);
-            store_pack<T>(dxr + c, left, v);
+            store_places<T>(dxr + c, left, v);
         }
         if (TAIL && last < cols)
             dxr[last] = result(NV * N, rd1, rx1);
@@ -454,7 +545,14 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(NormBwdArgs a, int tpr, b
             __syncthreads();
 #pragma unroll
         for (int i = 0; i < K; i++) {
-            const int c = i < NV * N ? (t + i / N * tpr) * N + i % N : last;
+            int c = last;
+            if (i < NV * N) {
+                const int first = (t + i / N * tpr) * N;
+                const int at = TAIL ? i % N : place<N>(i % N, max(1, cols - first));
+                if (at < 0)
+                    continue;
+                c = first + at;
+            }
             const float v = k ? sb[i] : sw[i];
             if (groups > 1)
                 lds[group * tpr * K + c] = v;
@@ -551,8 +649,8 @@ __global__ __launch_bounds__(256) void norm_bwd_pieces(NormBwdArgs a, long long 
             const int c = c0 + i * 256 * N;
             rx[i] = rd[i] = typename Pack<T>::V{};
             if (c < len) {
-                rx[i] = load_pack<T>(xr + first + c, len - c, (T)0.f);
-                rd[i] = load_pack<T>(dyr + first + c, len - c, (T)0.f);
+                rx[i] = load_places<T>(xr + first + c, len - c);
+                rd[i] = load_places<T>(dyr + first + c, len - c);
             }
             load_weights<N>(w, first + c, end, 1.f, wv[i]);
         }
@@ -634,8 +732,8 @@ __global__ __launch_bounds__(512) void norm_bwd_cols(NormBwdArgs a, int splits, 
                     const long long row = base + r;
                     mean[i] = a.mean[row];
                     rstd[i] = a.rstd[row];
-                    rx[i] = load_pack<T>((const T *)a.x.p + row * a.x.ld + c, left, (T)0.f);
-                    rd[i] = load_pack<T>((const T *)a.dy.p + row * a.dy.ld + c, left, (T)0.f);
+                    rx[i] = load_places<T>((const T *)a.x.p + row * a.x.ld + c, left);
+                    rd[i] = load_places<T>((const T *)a.dy.p + row * a.dy.ld + c, left);
                 }
             }
 #pragma unroll
@@ -654,7 +752,7 @@ __global__ __launch_bounds__(512) void norm_bwd_cols(NormBwdArgs a, int splits, 
                     v[j] = (T)(rstd[i] * (d * wv[j] - s1 - u * s2));
                 }
                 if (a.dx.p)
-                    store_pack<T>((T *)a.dx.p + (base + r) * a.dx.ld + c, left, v);
+                    store_places<T>((T *)a.dx.p + (base + r) * a.dx.ld + c, left, v);
             }
         }
     }
@@ -662,8 +760,11 @@ __global__ __launch_bounds__(512) void norm_bwd_cols(NormBwdArgs a, int splits, 
         return;
 #pragma unroll
     for (int j = 0; j < N; j++) {
-        lds[wave][0][lane * N + j] = sw[j];
-        lds[wave][1][lane * N + j] = sb[j];
+        const int at = place<N>(j, max(1, left));
+        if (at < 0)
+            continue;
+        lds[wave][0][lane * N + at] = sw[j];
+        lds[wave][1][lane * N + at] = sb[j];
     }
     __syncthreads();
     float *part = parts + (size_t)blockIdx.y * 2 * a.cols;

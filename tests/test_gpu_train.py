@@ -128,6 +128,33 @@ def test_layernorm_row_lengths(rows, xt):
             assert_close(got, val, 300 * U * mag + half_ulp(val, xt) * 1.01, f"{name} {cols}")
 
 
+@pytest.mark.parametrize("xt,wt", [(F32, F32), (BF16, F32), (F16, F16)])
+@pytest.mark.parametrize("base", [40, 1200, 4352, 9000, 20000, 40000])
+def test_layernorm_short_vectors(base, xt, wt):
+    """Every number of elements that the row's end leaves of a vector, in every form."""
+    import paper_1903_06934_amd as m
+    rows = 90 if base > 16384 else 37
+    for cols in range(base, base + 8):
+        g = gen(cols, 37)
+        x, dy = randn(g, rows, cols).to(xt), randn(g, rows, cols).to(xt)
+        w, b = randn(g, cols).to(wt), randn(g, cols).to(wt)
+        yv, wide = strided(torch.zeros(rows, cols, dtype=xt), 3, 1)
+        y, mean, rstd = m.layernorm_fwd(x.cuda(), w.cuda(), b.cuda(), y=yv)
+        ry, rmean, rrstd, size, msize = ref.layernorm_fwd(x, w, b)
+        k = norm_terms(cols) * U
+        assert_close(rstd, rrstd, rrstd * (k + (k * msize * rrstd) ** 2), f"rstd {cols}")
+        assert_close(y, ry, 2 * k * size + half_ulp(ry, xt) * 1.01, f"y {cols}")
+        untouched(yv, wide)
+        dxv, wide = strided(torch.zeros(rows, cols, dtype=xt), 1, 1)
+        dx, dw, db = m.layernorm_bwd(dy.cuda(), x.cuda(), mean, rstd, w.cuda(), dx=dxv)
+        want = ref.layernorm_bwd(dy, x, mean.cpu(), rstd.cpu(), w)
+        assert_close(dx, want[0][0], k * want[0][1] + half_ulp(want[0][0], xt) * 1.01,
+                     f"dx {cols}")
+        untouched(dxv, wide)
+        for got, (val, mag), name in ((dw, want[1], "dw"), (db, want[2], "db")):
+            assert_close(got, val, 300 * U * mag + half_ulp(val, wt) * 1.01, f"{name} {cols}")
+
+
 @pytest.mark.parametrize("xt", [F32, BF16, F16])
 @pytest.mark.parametrize("cols", [5, 9, 10, 33, 69, 80, 81, 130, 140, 144, 145, 256, 257, 288,
                                   320, 321, 513, 576, 769, 1025, 1088, 1089, 2049, 2176, 3080,
