@@ -11,8 +11,8 @@
 //
 // Bound by memory in large calls (4096 x 32000 bf16: 46 us, 5.7 TB/s; of about
 // 11 instructions an element the exponential takes the time of four), by
-// latencies in small ones (128 x 1000 fp32 with 5 alternatives: 6.0 us, one
-// row a wave).  Backward, every element is read and written once and its
+// latencies in small ones (128 x 1000 fp32 with 5 alternatives: 5.4 us, one
+// row a workgroup).  Backward, every element is read and written once and its
 // probability computed from the row's two statistics: 4096 x 32000 bf16 in
 // 90 us, 5.8 TB/s.
 #include <algorithm>
@@ -596,13 +596,14 @@ int pack_of(int xtype) { return xtype == 0 ? 4 : 8; }
 // Pieces of a row, and the threads of a team.
 // Pieces: with a quarter of the CUs' number of rows or fewer, as many as fill
 // the CUs, of at least 4096 elements, up to kPieces (4 x 131072 bf16 with 20
-// alternatives: 13.1 us, whole rows 17.7; in two pieces 100 rows take 25.3,
-// whole 19.1: joining them costs 5).
+// alternatives: 13.1 us, whole rows 17.0; in two pieces 100 rows take 25.0,
+// whole 18.1: joining them costs 5).
 // A wave a row up to 16 packs a lane (8000 x 1000 bf16 with 5 alternatives:
-// 14.7 us, by workgroups 36.1; 8000 x 4000: 22 and 40), but with fewer rows than
-// two a CU up to four (100 x 4000: by waves 8.5, by workgroups 7.8); a workgroup
-// of 1024 threads from 12 packs a thread on (200 x 131072 bf16 with 20: 19.8 us,
-// with 256 threads 34.4; 2000 x 40000 fp32, 10 packs: 72 and 61).
+// 13.3 us, by workgroups 26.2; 8000 x 4000: 21 and 29), but with fewer rows than
+// two a CU up to two (100 x 4000 bf16: by waves 8.4, by workgroups 7.1; 128 x 1000
+// fp32, four packs: 6.8 and 6.4); a workgroup of 1024 threads from 12 packs a
+// thread on (200 x 131072 bf16 with 20: 18.9 us, with 256 threads 34.2; 2000 x
+// 40000 fp32, 10 packs: 57.8 and 55.4).
 struct Cut {
     int piece, splits, team;
 };
@@ -620,7 +621,7 @@ Cut cut(int xtype, long long rows, long long vocab)
         splits = (vocab + piece - 1) / piece;
     }
     int team = 256;
-    if (splits == 1 && vocab <= 64LL * n * (rows >= 2LL * num_cus() ? 16 : 4))
+    if (splits == 1 && vocab <= 64LL * n * (rows >= 2LL * num_cus() ? 16 : 2))
         team = 64;
     else if (splits == 1 && vocab >= 1024LL * n * 12)
         team = 1024;
@@ -640,8 +641,8 @@ hipError_t forward(int xtype, const LogprobArgs &a, hipStream_t stream)
     uint64_t *keys = (uint64_t *)((char *)a.ws + parts_bytes(a.rows, s.splits));
     const long long teams = s.team < 256 ? 256 / s.team : 1;
     // Loads that leave nothing in the caches, for logits larger than the
-    // last-level one holds beside the rest (4096 x 32000 bf16: 48.4 us instead of
-    // 53.7; 500 x 8191 bf16: 7.1 with them, 6.1 without).
+    // last-level one holds beside the rest (4096 x 32000 bf16: 49.3 us instead of
+    // 54.4; 500 x 8191 bf16: 7.3 with them, 6.0 without).
     const bool through = a.rows * a.vocab * (long long)sizeof(T) > 100LL << 20;
     const long long most = s.splits > 1 ? a.rows : kMaxBlocks * teams;  // rows of a launch
     for (long long first = 0; first < a.rows; first += most) {

@@ -885,10 +885,10 @@ int fwd_blocks(const RowPlan &p, long long rows)
 // Backward: each workgroup adds 2 x cols partial sums to write and to read
 // again, so 512 threads a CU (16384 x 4096 bf16: 83.7 us; with 768 and 1024
 // 92.5 and 102.4); 1024 where a thread holds one pack, too little in flight,
-// and takes at least five rows (31000 x 1700 bf16: 101 us instead of 149;
-// 3000 x 1500, three rows: 26.6 instead of 22.6).  A single workgroup, which
-// needs no sum after it, takes up to two rows a group (7 x 1024 bf16: 8.6 us
-// instead of 9.8).
+// and takes at least five rows (31000 x 1500 bf16: 68.6 us instead of 94.0;
+// 3000 x 1500, three rows: 24.9 instead of 18.8; with an element beside the pack
+// 30000 x 300 fp32 26.7 instead of 24.7).  A single workgroup, which needs no sum
+// after it, takes up to two rows a group (7 x 1024 bf16: 8.6 us instead of 9.8).
 int bwd_blocks(const RowPlan &p, long long rows)
 {
     const long long groups = std::max(1, p.block / p.tpr);
@@ -897,15 +897,15 @@ int bwd_blocks(const RowPlan &p, long long rows)
     const auto blocks = [&](int threads) {
         return (long long)std::max(1, threads / p.block) * num_cus();
     };
-    const bool more = p.nv == 1 && rows >= 5 * groups * blocks(1024);
+    const bool more = p.nv == 1 && !p.tail && rows >= 5 * groups * blocks(1024);
     return (int)std::min((rows + groups - 1) / groups, blocks(more ? 1024 : 512));
 }
 
 // Loads that leave nothing in the caches, for inputs larger than the last-level
 // one holds beside the rest (from 100 MB on: 16384 x 4096 bf16 49.2 us instead
 // of 51.4 forward, 83.5 instead of 86.7 backward; 9000 x 4096 26.7 with them 29.6),
-// of whole cache lines (31000 x 1700 bf16, lines shared by rows: 48.9 with them,
-// 45.6 without).
+// of whole cache lines (16009 x 4369 bf16, lines shared by rows: 97.6 with them,
+// 81.2 without).
 bool streams(long long rows, long long cols, size_t elem, std::initializer_list<Rows> in)
 {
     bool lines = rows * cols * (long long)elem > 100LL << 20;
