@@ -349,6 +349,7 @@ struct List {
         if (!fast)
             throw py::error_already_set();
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(fast.ptr());
+        const int current = c10::hip::current_device();
         p.reserve(n);
         count.reserve(n);
         type.reserve(n);
@@ -358,17 +359,14 @@ struct List {
                 refuse(name, " must hold tensors");
             const Tensor &t = THPVariable_Unpack(o);
             const int k = type_of(t);
-            if (k < 0 || !here(t) || !t.is_contiguous())
+            if (k < 0 || !t.is_cuda() || t.get_device() != current || !t.is_contiguous())
                 refuse(name, " must hold contiguous float32, bfloat16 or float16 tensors on the "
                              "current device");
             p.push_back(t.data_ptr());
             count.push_back(t.numel());
             type.push_back(k);
-            if (!device)
-                device = t.device();
         }
-        if (!device)
-            device = at::Device(at::kCUDA, c10::hip::current_device());
+        device = at::Device(at::kCUDA, current);
     }
     int n() const { return (int)p.size(); }
     size_t need() const { return lib.grad_ws(n(), count.data(), type.data()); }
