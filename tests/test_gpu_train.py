@@ -518,6 +518,7 @@ SIZES = [
     [33] * 111 + [0] * 5 + [2, 50000], [1 << 22],
     [100] * 112, [100] * 113, [1025 * 16384 + 7, 3], [20000] * 599 + [1], [1] * 4200,
     [5] * 148, [70000, 1] * 148 + [3], [16384, 16385] * 74 + [40000],
+    [70000, 3] * 112, [9000] * 225, [40000, 0, 8191, 8193] * 150,
     [4095, 4096, 4097, 8191, 8192, 8193], [4096] * 1030, [8200] * 1030,
 ]
 
