@@ -349,7 +349,7 @@ struct List {
         if (!fast)
             throw py::error_already_set();
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(fast.ptr());
-        const int current = c10::hip::current_device();
+        int current = -1;  // asked for once, where there is a device tensor
         p.reserve(n);
         count.reserve(n);
         type.reserve(n);
@@ -359,6 +359,8 @@ struct List {
                 refuse(name, " must hold tensors");
             const Tensor &t = THPVariable_Unpack(o);
             const int k = type_of(t);
+            if (current < 0 && t.is_cuda())
+                current = c10::hip::current_device();
             if (k < 0 || !t.is_cuda() || t.get_device() != current || !t.is_contiguous())
                 refuse(name, " must hold contiguous float32, bfloat16 or float16 tensors on the "
                              "current device");
@@ -366,7 +368,7 @@ struct List {
             count.push_back(t.numel());
             type.push_back(k);
         }
-        device = at::Device(at::kCUDA, current);
+        device = at::Device(at::kCUDA, n ? current : c10::hip::current_device());
     }
     int n() const { return (int)p.size(); }
     size_t need() const { return lib.grad_ws(n(), count.data(), type.data()); }
