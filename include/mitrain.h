@@ -86,6 +86,9 @@ int layernorm_bwd(int xtype, int wtype, long long rows, long long cols, const vo
  *     above vocab: logp and the row's gradient are NaN.
  *   - a logit of -inf bans its token (p = 0).  A row that bans all: lse and
  *     every log probability -inf, entropy 0, stats {-inf, 0}, the gradient 0.
+ *     Tokens at the type's lowest value are not banned: a row of nothing else
+ *     is as likely for all of them at any scale, though its lse may be beyond
+ *     32 bits, and then is -inf.
  *   - a NaN or +inf in a row makes its lse, log probabilities, entropy,
  *     stats' sum and gradient NaN; for top_index a NaN counts as -inf.
  * 1e-6 <= scale <= 1e6 (else MICONV_ERR_VALUE).  vocab >= 1; 0 <= top <=

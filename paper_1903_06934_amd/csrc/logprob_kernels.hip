@@ -327,22 +327,24 @@ __device__ __noinline__ int top_by_value(typename Tm::Shared &sh, const T *z, in
     return k;
 }
 
-// The sums' results.
+// The sums' results.  none: the row bans every token (lse alone does not tell: a
+// row of the type's lowest value times a scale above 1 is beyond 32 bits too).
 struct Done {
     float lse, entropy, log_s;
+    bool none;
 };
 
 __device__ __forceinline__ Done finish(Soft p, float scale)
 {
     if (p.m == -kInf && p.s == 0.f)
-        return Done{-kInf, 0.f, 0.f};
+        return Done{-kInf, 0.f, 0.f, true};
     const float log_s = logf(p.s);
-    return Done{p.m * scale + log_s, log_s - scale * (p.t / p.s), log_s};
+    return Done{p.m * scale + log_s, log_s - scale * (p.t / p.s), log_s, false};
 }
 
 __device__ __forceinline__ float log_prob(float z, Soft p, Done d, float scale)
 {
-    if (d.lse == -kInf)
+    if (d.none)
         return -kInf;
     return (z - p.m) * scale - d.log_s;
 }

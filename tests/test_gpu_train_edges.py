@@ -1,0 +1,58 @@
+"""The training step's operators on the GPU where rows and lists are unlike any
+that training data makes: masks beyond 32 bits, equal elements, factors below
+32 bits, tensors that nobody else holds.  Plain 64-bit forms from train_ref.py."""
+import math
+
+import pytest
+import torch
+
+import train_ref as ref
+from train_ref import INF, U, assert_close, half_ulp
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+NAN = math.nan
+
+
+def randn(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed))
+
+
+# --------------------------------------------------------- log probabilities
+# A wave a row, a workgroup of 256 or 1024 threads, pieces and their join.
+@pytest.mark.parametrize("rows,vocab", [(600, 5), (600, 300), (8, 3000), (600, 9001), (100, 50001),
+                                        (6, 70000)])
+@pytest.mark.parametrize("xt", [F32, BF16])
+@pytest.mark.parametrize("scale", [1.25, 2.0, 1e6])
+def test_logprob_of_a_lowest_value_mask_beyond_32_bits(rows, vocab, xt, scale):
+    """Rows masked with the type's lowest value, which times the scale is beyond 32
+    bits: equally likely tokens all the same, not banned ones."""
+    import paper_1903_06934_amd as m
+    z = torch.full((6, vocab), float(torch.finfo(xt).min), dtype=xt)
+    z[1, ::2] = -INF                                    # some banned as well
+    z[2] = -INF                                         # all banned
+    z[3] = (3 * randn(1, vocab)).to(xt)
+    z[4, vocab // 2] = 0.0                              # one token left
+    z[5, 1:] = -INF                                     # one masked, the others banned
+    t = torch.tensor([1, 1, 0, vocab - 1, vocab // 2, 0])
+    top = min(vocab, 20)
+    out = m.logprob_fwd(z.repeat(rows // 6, 1).cuda(), t.repeat(rows // 6).cuda(), top=top,
+                        scale=scale)
+    want = ref.logprob_fwd(z, t, top, scale)
+    base = 64 * U * (2 + math.log(vocab)) + vocab / 2048 * U
+    last = slice((rows // 6 - 1) * 6, rows // 6 * 6)
+    for name in ("lse", "logp", "entropy", "top_logp"):
+        # What lies beyond 32 bits is infinite in the result.
+        w = want[name].float().double()
+        size = w.abs().nan_to_num(0, 0, 0)
+        bound = base * (2 + math.log(vocab)) + 4 * U * size
+        for got in (getattr(out, name)[:6], getattr(out, name)[last]):
+            assert_close(got, w, bound, name)
+    assert torch.equal(out.top_index[:6].cpu(), want["top_index"])
+    assert_close(out.stats[:6], want["stats"], base + 4 * U * want["stats"].abs().nan_to_num(0, 0, 0),
+                 "stats")
+    dl = randn(2, 6)
+    dz = m.logprob_bwd(z.cuda(), out.stats[:6], t.cuda(), dl.cuda(), scale=scale)
+    rz, size = ref.logprob_bwd(z, t, scale, out.stats[:6].cpu(), dl)
+    assert_close(dz, rz, 8 * U * size + half_ulp(rz, xt) * 1.01 + 1e-37, "dlogits")
