@@ -337,15 +337,18 @@ Tensor logprob_backward(const Tensor &z, const Tensor &stats, const Maybe &targe
 
 // ------------------------------------------------------------------ clipping
 struct List {
+    // Of a generator's tensors this is the only holder: until the launches are
+    // enqueued, so that neither workspace nor results are given their memory.
+    py::object fast;
     std::vector<void *> p;
     std::vector<long long> count;
     std::vector<int> type;
     std::optional<at::Device> device;
 
     List(const py::handle &tensors, const char *name)
+        : fast(py::reinterpret_steal<py::object>(
+              PySequence_Fast(tensors.ptr(), "a list of tensors is wanted")))
     {
-        const py::object fast = py::reinterpret_steal<py::object>(
-            PySequence_Fast(tensors.ptr(), "a list of tensors is wanted"));
         if (!fast)
             throw py::error_already_set();
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(fast.ptr());

@@ -56,3 +56,38 @@ def test_logprob_of_a_lowest_value_mask_beyond_32_bits(rows, vocab, xt, scale):
     dz = m.logprob_bwd(z.cuda(), out.stats[:6], t.cuda(), dl.cuda(), scale=scale)
     rz, size = ref.logprob_bwd(z, t, scale, out.stats[:6].cpu(), dl)
     assert_close(dz, rz, 8 * U * size + half_ulp(rz, xt) * 1.01 + 1e-37, "dlogits")
+
+
+# ------------------------------------------------------------------ clipping
+@pytest.mark.parametrize("sizes", [[1], [300] * 3, [1000] * 150, [3, 70000, 2048, 1] * 5])
+@pytest.mark.parametrize("iterable", [tuple, iter, lambda ts: (t * 2 for t in ts)],
+                         ids=["tuple", "iterator", "temporaries"])
+def test_gradients_from_any_iterable(sizes, iterable):
+    """Gradients that only the call holds stay whole until it has read them, though
+    norm and workspace are allocated after them."""
+    import paper_1903_06934_amd as m
+    dev = [randn(i, n).cuda() for i, n in enumerate(sizes)]
+    given = [t.cpu() for t in iterable(dev)]
+    norm, want = ref.clip(given, 0.25)
+    for _ in range(3):
+        assert_close(m.grad_norm(iterable(dev)), torch.tensor([norm]), 2 * U * norm, "norm")
+        assert m.grad_workspace(iterable(dev)).numel() == m.grad_workspace(dev).numel()
+        out = [torch.full_like(t, NAN) for t in dev]
+        got = m.grad_clip(iterable(dev), 0.25, out=iter(out))
+        assert_close(got, torch.tensor([norm]), 2 * U * norm, "norm")
+        for o, w in zip(out, want):
+            assert_close(o, w, 4 * U * w.abs() + half_ulp(w, F32) * 1.01, "clipped")
+
+
+def test_lists_that_are_none():
+    import paper_1903_06934_amd as m
+    for bad in (3, None):
+        with pytest.raises(TypeError):
+            m.grad_norm(bad)
+
+    def broken():
+        yield torch.ones(3, device="cuda")
+        raise KeyError("from the generator")
+
+    with pytest.raises(KeyError):
+        m.grad_norm(broken())
