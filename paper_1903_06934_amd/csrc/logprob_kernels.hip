@@ -451,8 +451,8 @@ __global__ __launch_bounds__(SIZE < 256 ? 256 : SIZE) void logprob_rows(LogprobA
         }
     };
     const int rounds = (n + SIZE * N - 1) / (SIZE * N);  // packs of a thread
-    if (rounds <= F) {  // in its registers still
-        if (mine >= bound)
+    if (rounds <= F) {  // in its registers still, if it has any
+        if (t * N < n && mine >= bound)
 #pragma unroll
             for (int f = 0; f < F; f++)
                 collect(raw[f], (t + f * SIZE) * N);
@@ -683,8 +683,8 @@ hipError_t backward(const LogprobBwdArgs &a, hipStream_t stream)
     int tpr = 1;
     while (tpr < 256 && (long long)tpr * NV < packs)
         tpr *= 2;
-    // A vocabulary below 2^29 makes at most 2^17 pieces; rows of a launch by the
-    // grid's limits.
+    // A vocabulary below 2^29 makes at most 2^18 pieces (fp32, 2048 elements each);
+    // rows of a launch by the grid's limits.
     const long long pieces = tpr == 256 ? (packs + 256 * NV - 1) / (256 * NV) : 1;
     const long long most =
         tpr == 256 ? std::min(65535LL, std::max(1LL, 4 * kMaxBlocks / pieces)) : kMaxBlocks;

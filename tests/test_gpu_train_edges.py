@@ -58,6 +58,24 @@ def test_logprob_of_a_lowest_value_mask_beyond_32_bits(rows, vocab, xt, scale):
     assert_close(dz, rz, 8 * U * size + half_ulp(rz, xt) * 1.01 + 1e-37, "dlogits")
 
 
+@pytest.mark.parametrize("rows", [6, 1200])
+@pytest.mark.parametrize("vocab,left,top", [(9, 1, 9), (70, 3, 64), (500, 10, 64), (1100, 5, 40)])
+@pytest.mark.parametrize("xt", [F32, BF16])
+def test_top_of_rows_that_ban_nearly_all(rows, vocab, left, top, xt):
+    """Fewer tokens left than are asked for, in rows that leave threads without an
+    element: the banned ones follow in the order of their indices."""
+    import paper_1903_06934_amd as m
+    z = torch.full((6, vocab), -INF)
+    for r in range(6):
+        z[r, torch.randperm(vocab, generator=torch.Generator().manual_seed(r))[:left * r // 2]] = r
+    z = z.to(xt)
+    out = m.logprob_fwd(z.repeat(rows // 6, 1).cuda(), top=top)
+    want = ref.logprob_fwd(z, None, top)
+    assert torch.equal(out.top_index.cpu(), want["top_index"].repeat(rows // 6, 1))
+    logp = want["top_logp"].repeat(rows // 6, 1)
+    assert_close(out.top_logp, logp, 64 * U * (2 + math.log(vocab)), "top_logp")
+
+
 # ------------------------------------------------------------------ clipping
 @pytest.mark.parametrize("sizes", [[1], [300] * 3, [1000] * 150, [3, 70000, 2048, 1] * 5])
 @pytest.mark.parametrize("iterable", [tuple, iter, lambda ts: (t * 2 for t in ts)],
