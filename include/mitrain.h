@@ -48,7 +48,9 @@ extern "C" {
  * MITRAIN_F32 (else MICONV_ERR_TYPE); either may be NULL (w = 1, b = 0).  mean
  * and rstd [rows] are fp32, what the backward pass takes; each may be NULL.
  * eps >= 0 and finite (else MICONV_ERR_VALUE).  cols >= 1.  A row of equal
- * elements with eps = 0 has no norm (NaN), nor has one with an infinity or NaN.
+ * elements has that number as its mean and b as its result, but with eps = 0 no
+ * norm (NaN), nor has one with an infinity or NaN.  A row's sum and its sum of
+ * squares about the mean are held in 32 bits, and have to be within their range.
  */
 size_t layernorm_fwd_workspace_size(int xtype, long long rows, long long cols);
 int layernorm_fwd(int xtype, int wtype, long long rows, long long cols, const void *x,

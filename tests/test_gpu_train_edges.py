@@ -19,6 +19,59 @@ def randn(seed, *shape):
     return torch.randn(shape, generator=torch.Generator().manual_seed(seed))
 
 
+# ---------------------------------------------------------------- layer norm
+# Groups inside a wave, waves, workgroups, single elements beside packs, rows too
+# long for held weights, pieces; each with few rows and with many.
+EQUAL_COLS = [1, 3, 7, 20, 69, 197, 513, 700, 1025, 2049, 3080, 5000, 8193, 16385, 20011, 40001,
+              100352]
+
+
+@pytest.mark.parametrize("xt", [F32, BF16, F16])
+@pytest.mark.parametrize("cols", EQUAL_COLS)
+@pytest.mark.parametrize("rows", [5, 2100])
+def test_layernorm_of_equal_elements(rows, cols, xt):
+    """A row of one number has that number as its mean, no variance, and b as its
+    result, whatever a sum of its elements rounds to; with eps = 0 it has no norm."""
+    import paper_1903_06934_amd as m
+    if rows * cols > 1 << 24:
+        rows = 90
+    values = torch.tensor([0.1, 1.7, -2.3e-4, 1.0e4, 2.5] + ([] if xt == F16 else [-3.3e7, 1e30]))
+    x = values.to(xt)[torch.arange(rows) % len(values)][:, None].repeat(1, cols)
+    w, b = randn(1, cols), randn(2, cols)
+    y, mean, rstd = m.layernorm_fwd(x.cuda(), w.cuda(), b.cuda(), 1e-5)
+    assert torch.equal(mean.cpu(), x[:, 0].float())
+    want = torch.full((rows,), 1 / math.sqrt(float(torch.tensor(1e-5))), dtype=torch.float64)
+    assert_close(rstd, want, 4 * U * want, "rstd")
+    assert torch.equal(y.cpu(), b.to(xt).expand(rows, cols))
+    y, mean, rstd = m.layernorm_fwd(x.cuda(), w.cuda(), b.cuda(), 0.0)
+    assert torch.equal(mean.cpu(), x[:, 0].float())
+    assert (rstd == INF).all() and torch.isnan(y).all()
+
+
+@pytest.mark.parametrize("cols", [2, 9, 64, 197, 513, 1025, 3080, 16384])
+@pytest.mark.parametrize("rows", [5, 2100])
+def test_layernorm_of_neighbouring_numbers(rows, cols):
+    """Elements that differ in their last places: the differences from the mean are
+    whole numbers of these places, so the variance keeps its accuracy, and y is off
+    by the rounding of the mean (u |mean| rstd) beside its own few."""
+    import paper_1903_06934_amd as m
+    if rows * cols > 1 << 24:
+        rows = 90
+    k = torch.randint(0, 4, (rows, cols), generator=torch.Generator().manual_seed(cols))
+    k[:, 0], k[:, 1] = 0, 1  # no row of equal elements
+    x = 8200.0 + k * 2.0 ** -10
+    assert torch.equal(x.double(), 8200.0 + k.double() * 2.0 ** -10)
+    y, mean, rstd = m.layernorm_fwd(x.cuda(), eps=1e-9)
+    d = x.double()
+    rmean = d.mean(1)
+    rrstd = 1 / torch.sqrt(((d - rmean[:, None]) ** 2).mean(1) + float(torch.tensor(1e-9)))
+    assert_close(mean, rmean, 1.01 * U * rmean.abs() + U * U, "mean")
+    # Sums of small whole numbers; a thread's and the tree's roundings.
+    assert_close(rstd, rrstd, 64 * U * rrstd, "rstd")
+    ry = (d - rmean[:, None]) * rrstd[:, None]
+    assert_close(y, ry, (1.05 * U * rmean.abs() * rrstd)[:, None] + 70 * U * ry.abs(), "y")
+
+
 # --------------------------------------------------------- log probabilities
 # A wave a row, a workgroup of 256 or 1024 threads, pieces and their join.
 @pytest.mark.parametrize("rows,vocab", [(600, 5), (600, 300), (8, 3000), (600, 9001), (100, 50001),
