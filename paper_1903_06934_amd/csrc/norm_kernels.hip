@@ -294,7 +294,8 @@ __device__ __forceinline__ Moments merge(Moments a, Moments b)
     if (a.n == 0.f)
         return b;
     const float d = b.mean - a.mean, f = b.n / n;
-    return Moments{n, a.mean + d * f, a.m2 + b.m2 + d * d * a.n * f};
+    const float mean = __builtin_isfinite(a.mean) ? a.mean + d * f : a.mean + b.mean;
+    return Moments{n, mean, a.m2 + b.m2 + d * d * a.n * f};
 }
 
 __device__ __forceinline__ Moments wave_merge(Moments m)

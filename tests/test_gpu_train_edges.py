@@ -72,6 +72,21 @@ def test_layernorm_of_neighbouring_numbers(rows, cols):
     assert_close(y, ry, (1.05 * U * rmean.abs() * rrstd)[:, None] + 70 * U * ry.abs(), "y")
 
 
+@pytest.mark.parametrize("cols", [20, 700, 40001])
+@pytest.mark.parametrize("bad", [INF, -INF, NAN])
+def test_layernorm_mean_of_infinite_rows(cols, bad):
+    """An infinity among a row's elements is its mean; the row has no norm."""
+    import paper_1903_06934_amd as m
+    x = randn(3, 4, cols)
+    x[1, cols - 1] = x[2, 0] = bad
+    y, mean, rstd = (t.cpu() for t in m.layernorm_fwd(x.cuda()))
+    for r in (1, 2):
+        assert torch.isnan(y[r]).all() and torch.isnan(rstd[r])
+        assert torch.isnan(mean[r]) if bad != bad else mean[r] == bad
+    for r in (0, 3):
+        assert torch.isfinite(y[r]).all()
+
+
 # --------------------------------------------------------- log probabilities
 # A wave a row, a workgroup of 256 or 1024 threads, pieces and their join.
 @pytest.mark.parametrize("rows,vocab", [(600, 5), (600, 300), (8, 3000), (600, 9001), (100, 50001),
