@@ -221,15 +221,16 @@ __global__ __launch_bounds__(256) void norm_only(const double *parts, int n, flo
         *norm = (float)v;
 }
 
+// g f 2^shift.
 template <class T>
-__device__ __forceinline__ void chunk_scale(const T *p, T *out, int n, float f)
+__device__ __forceinline__ void chunk_scale(const T *p, T *out, int n, float f, int shift)
 {
     constexpr int N = Pack<T>::N;
     each_pack<T, 4, true>(p, n, [&](typename Pack<T>::V raw, int i) {
         typename Pack<T>::V v;
 #pragma unroll
         for (int j = 0; j < N; j++)
-            v[j] = (T)((float)raw[j] * f);
+            v[j] = (T)ldexpf((float)raw[j] * f, shift);
         if (i < n)
             store_pack<T>(out + i, n - i, v);
     });
@@ -245,7 +246,11 @@ __device__ __forceinline__ void scale_share(const GradEntry *e, int n, unsigned 
     const double v = norm_of(parts, nparts, lds);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0)
         *norm = (float)v;
-    const float f = v <= (double)max_norm ? 1.f : (float)((double)max_norm / v);
+    // The factor in 32 bits; one below their normal numbers (large gradients and a
+    // small max_norm) is shifted into them, and its product with g back.
+    const double factor = v <= (double)max_norm ? 1. : (double)max_norm / v;
+    const int shift = factor < 0x1p-126 && factor > 0. ? ilogb(factor) + 126 : 0;
+    const float f = (float)ldexp(factor, -shift);
     const Share w = share_of(chunks);
     if (w.first == w.end)
         return;
@@ -259,11 +264,11 @@ __device__ __forceinline__ void scale_share(const GradEntry *e, int n, unsigned 
         const long long at = (long long)(c - e[i].first) * most;
         const int k = (int)min((long long)most, e[i].count - at);
         if (e[i].type == 0)
-            chunk_scale((const float *)e[i].in + at, (float *)e[i].out + at, k, f);
+            chunk_scale((const float *)e[i].in + at, (float *)e[i].out + at, k, f, shift);
         else if (e[i].type == 1)
-            chunk_scale((const __bf16 *)e[i].in + at, (__bf16 *)e[i].out + at, k, f);
+            chunk_scale((const __bf16 *)e[i].in + at, (__bf16 *)e[i].out + at, k, f, shift);
         else
-            chunk_scale((const _Float16 *)e[i].in + at, (_Float16 *)e[i].out + at, k, f);
+            chunk_scale((const _Float16 *)e[i].in + at, (_Float16 *)e[i].out + at, k, f, shift);
     }
 }
 

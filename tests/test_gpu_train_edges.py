@@ -177,3 +177,23 @@ def test_lists_that_are_none():
 
     with pytest.raises(KeyError):
         m.grad_norm(broken())
+
+
+@pytest.mark.parametrize("max_norm", [1e-5, 1e-9, 3e-12, 1e-20, 1e-38])
+@pytest.mark.parametrize("count", [1, 5, 200])
+def test_clip_by_factors_below_32_bits(max_norm, count):
+    """max_norm / norm below 32 bits' smallest numbers: the clipped gradients have
+    their own size's accuracy all the same, in place and beside."""
+    import paper_1903_06934_amd as m
+    grads = [randn(i, 700 + i) * 2e30 for i in range(count)]
+    grads.append((randn(9, 333) * 1e30).to(BF16))
+    norm, want = ref.clip(grads, max_norm)
+    dev = [t.cuda() for t in grads]
+    out = [torch.full_like(t, NAN) for t in dev]
+    got = m.grad_clip(dev, max_norm, out=out)
+    assert_close(got, torch.tensor([norm]), 2 * U * norm, "norm")
+    m.grad_clip(dev, max_norm)
+    for o, i, w in zip(out, dev, want):
+        # The factor, the product and a shift, which rounds below the normal numbers.
+        assert_close(o, w, 4 * U * w.abs() + 2.0 ** -149 + half_ulp(w, o.dtype) * 1.01, "clipped")
+        assert torch.equal(o, i)
