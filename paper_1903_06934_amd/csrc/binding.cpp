@@ -144,6 +144,20 @@ Tensor empty(at::IntArrayRef sizes, const Tensor &x, at::ScalarType type)
     return at::empty(sizes, x.options().dtype(type));
 }
 
+// A tensor that a call has written, as torch's own calls in place count it: one
+// that autograd has saved before is reported when it is used.
+void written(const Tensor &t)
+{
+    if (!t.is_inference())
+        t.unsafeGetTensorImpl()->bump_version();
+}
+
+void written(const Maybe &m)
+{
+    if (m)
+        written(*m);
+}
+
 // Small float results side by side in one buffer: its allocation takes the host
 // longer than the views.  Only floats: tensors of several types in one storage
 // cannot be saved together.
@@ -229,6 +243,9 @@ std::tuple<Tensor, Tensor, Tensor> layernorm_forward(const Tensor &x, const Mayb
                            vector<float>(rstd, "rstd", r.rows, at::kFloat), s.p, s.bytes,
                            stream()),
          "layernorm_fwd");
+    written(y);
+    written(mean);
+    written(rstd);
     return {y, mean, rstd};
 }
 
@@ -267,6 +284,9 @@ std::tuple<Maybe, Maybe, Maybe> layernorm_backward(const Tensor &dy, const Tenso
                            vector(dw, "dw", r.cols, wt), vector(db, "db", r.cols, wt), s.p,
                            s.bytes, stream()),
          "layernorm_bwd");
+    written(dx);
+    written(dw);
+    written(db);
     return {dx, dw, db};
 }
 
@@ -332,6 +352,7 @@ Tensor logprob_backward(const Tensor &z, const Tensor &stats, const Maybe &targe
                          vector<float>(dentropy, "dentropy", r.rows, at::kFloat), dz.data_ptr(),
                          ldd, stream()),
          "logprob_bwd");
+    written(dz);
     return dz;
 }
 
@@ -374,6 +395,10 @@ struct List {
         device = at::Device(at::kCUDA, n ? current : c10::hip::current_device());
     }
     int n() const { return (int)p.size(); }
+    const Tensor &operator[](int i) const
+    {
+        return THPVariable_Unpack(PySequence_Fast_GET_ITEM(fast.ptr(), i));
+    }
     size_t need() const { return lib.grad_ws(n(), count.data(), type.data()); }
 };
 
@@ -398,6 +423,7 @@ Tensor gradient_norm(const py::object &grads, const Maybe &norm_, const Maybe &w
     call(lib.grad_norm(g.n(), g.p.data(), g.count.data(), g.type.data(), (float *)norm.data_ptr(),
                        s.p, s.bytes, stream()),
          "grad_norm");
+    written(norm);
     return norm;
 }
 
@@ -417,6 +443,9 @@ Tensor gradient_clip(const py::object &grads, double max_norm, const py::object 
                        o ? o->p.data() : g.p.data(), (float *)norm.data_ptr(), s.p, s.bytes,
                        stream()),
          "grad_clip");
+    written(norm);
+    for (int i = 0; i < g.n(); i++)
+        written((o ? *o : g)[i]);
     return norm;
 }
 

@@ -9,6 +9,10 @@ any strides that one row stride covers (a slice of a wider matrix's columns or
 rows, say).  What is left out of the output and workspace arguments is
 allocated.  ValueError: a tensor of another type, layout, size or device;
 MiconvError: what the library refuses.
+
+Autograd does not record the calls: results have no history, whether or not an
+input requires a gradient.  A given tensor that a call writes counts as changed
+in place, so that torch reports a backward pass that had saved it.
 """
 from __future__ import annotations
 

@@ -197,3 +197,50 @@ def test_clip_by_factors_below_32_bits(max_norm, count):
         # The factor, the product and a shift, which rounds below the normal numbers.
         assert_close(o, w, 4 * U * w.abs() + 2.0 ** -149 + half_ulp(w, o.dtype) * 1.01, "clipped")
         assert torch.equal(o, i)
+
+
+# ------------------------------------------------------------ results in place
+def test_results_in_given_tensors_are_seen_by_autograd():
+    """A tensor that torch has saved for a backward pass and that a call overwrites
+    afterwards is reported, not used."""
+    import paper_1903_06934_amd as m
+    x, w = randn(1, 6, 50).cuda(), torch.ones(50, device="cuda")
+    t, dl = torch.arange(6, device="cuda"), torch.ones(6, device="cuda")
+    y, mean, rstd = m.layernorm_fwd(x, w, w)
+    stats = m.logprob_fwd(x, t).stats
+    new = lambda *s: torch.zeros(s, device="cuda")
+
+    def layernorm(a, b, c):
+        m.layernorm_fwd(x, w, w, y=a, mean=b, rstd=c)
+
+    def layernorm_back(a, b, c):
+        m.layernorm_bwd(x, x, mean, rstd, w, dx=a, dw=b, db=c)
+
+    cases = [(layernorm, [new(6, 50), new(6), new(6)]),
+             (layernorm_back, [new(6, 50), new(50), new(50)]),
+             (lambda a: m.logprob_bwd(a, stats, t, dl, dlogits=a), [x.clone()]),
+             (lambda a: m.logprob_bwd(x, stats, t, dl, dlogits=a), [new(6, 50)]),
+             (lambda a, b: m.grad_clip([a, b], 1.0), [x.clone(), w.clone()]),
+             (lambda a, b, n: m.grad_clip([x, w], 1.0, out=[a, b], norm=n),
+              [new(6, 50), new(50), new(1)]),
+             (lambda n: m.grad_norm([x, w], norm=n), [new(1)])]
+    for call, given in cases:
+        v = torch.ones(1, device="cuda", requires_grad=True)
+        saved = [(g * v).sum() for g in given]  # each product saves its tensor
+        before = [g._version for g in given]
+        call(*given)
+        for g, b, s in zip(given, before, saved):
+            assert g._version > b
+            with pytest.raises(RuntimeError, match="inplace"):
+                s.backward()
+    # What is only read keeps its version; tensors of inference mode have none.
+    before = x._version
+    m.layernorm_fwd(x, w, w)
+    m.grad_norm([x, w])
+    m.grad_clip([x, w], 1.0, out=[new(6, 50), new(50)])
+    assert x._version == before
+    with torch.inference_mode():
+        z = x.clone()
+        m.grad_clip([z], 1.0)
+        m.layernorm_fwd(x, w, w, y=z)
+    m.layernorm_fwd(x, w, w, y=z)
