@@ -1125,10 +1125,13 @@ size_t norm_bwd_ws(int xtype, long long rows, long long cols)
 {
     const RowPlan p = row_plan(xtype, rows, cols, false);
     const size_t part = 2 * (size_t)cols * sizeof(float);
+    if (!rows)
+        return 0;
     if (p.nv)
         return bwd_blocks(p, rows) * part;
+    const int n = row_chunks(xtype, rows, cols);  // one writes dw and db itself
     return up16((size_t)rows * piece_plan(xtype, rows, cols, false).splits * 2 * sizeof(float)) +
-           row_chunks(xtype, rows, cols) * part;
+           (n > 1 ? n * part : 0);
 }
 
 hipError_t launch_norm_fwd(int xtype, bool w32, const NormFwdArgs &a, hipStream_t stream)

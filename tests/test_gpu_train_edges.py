@@ -87,6 +87,27 @@ def test_layernorm_mean_of_infinite_rows(cols, bad):
         assert torch.isfinite(y[r]).all()
 
 
+@pytest.mark.parametrize("rows,cols,xt", [(0, 64, F32), (0, 20000, BF16), (1, 100352, F32),
+                                          (32, 40001, BF16), (64, 9000, F32), (65, 9000, F32),
+                                          (3, 700, F32), (600, 700, BF16)])
+def test_layernorm_bwd_stays_inside_its_workspace(rows, cols, xt):
+    """A workspace of the size asked for, between elements that stay as they are."""
+    import paper_1903_06934_amd as m
+    x, dy, w = (t.to(xt).cuda() for t in (randn(1, rows, cols), randn(2, rows, cols),
+                                          randn(3, cols)))
+    _, mean, rstd = m.layernorm_fwd(x, w)
+    want = m.layernorm_bwd(dy, x, mean, rstd, w)
+    need = m.layernorm_workspace(True, x)
+    n = 0 if need is None else need.numel()
+    room = torch.full((512 + n + 4096,), 77, dtype=torch.uint8, device="cuda")
+    got = m.layernorm_bwd(dy, x, mean, rstd, w, ws=room[512:512 + n] if n else None)
+    for p, q in zip(got, want):
+        assert torch.equal(p, q)
+    assert (room[:512] == 77).all() and (room[512 + n:] == 77).all()
+    if not rows:
+        assert n == 0 and (got[1] == 0).all() and (got[2] == 0).all()
+
+
 # --------------------------------------------------------- log probabilities
 # A wave a row, a workgroup of 256 or 1024 threads, pieces and their join.
 @pytest.mark.parametrize("rows,vocab", [(600, 5), (600, 300), (8, 3000), (600, 9001), (100, 50001),
