@@ -90,8 +90,9 @@ def build(verbose: bool = False) -> str:
     from paper_1903_06934_amd import isa_check
     isa_check.check(HIPCC, FLAGS, os.path.join(CSRC, "conv_kernels.hip"))
     os.replace(tmp, LIBRARY)
-    os.replace(_binding(verbose), BINDING)
     os.replace(_compile(PEAK_SOURCES, PEAK_LIBRARY, verbose), PEAK_LIBRARY)
+    # Last, as it alone needs torch's headers and a host compiler.
+    os.replace(_binding(verbose), BINDING)
     return LIBRARY
 
 

@@ -48,3 +48,28 @@ def test_long_rows_in_one_chunk_need_their_own_sums_only(L, xtype, rows):
                                          cols, H, W, ws, n, None)
     assert call(S, need - 1) == WS and call(None, 0) == WS
     assert call(S, need) == launched()
+
+
+def test_build_leaves_the_libraries_where_the_binding_fails(monkeypatch, tmp_path):
+    """The binding needs torch's headers and a host compiler; the convolutions and
+    the reference points need neither, and are built before it."""
+    from paper_1903_06934_amd import isa_check
+
+    def compiled(sources, out, verbose):
+        with open(out + ".tmp", "w") as f:
+            f.write(" ".join(sources))
+        return out + ".tmp"
+
+    def no_headers(verbose):
+        raise RuntimeError("no headers")
+
+    for name in ("LIBRARY", "PEAK_LIBRARY", "BINDING"):
+        monkeypatch.setattr(libbuild, name, str(tmp_path / name))
+    monkeypatch.setattr(libbuild, "_compile", compiled)
+    monkeypatch.setattr(libbuild, "_binding", no_headers)
+    monkeypatch.setattr(isa_check, "check", lambda *a: None)
+    with pytest.raises(RuntimeError, match="no headers"):
+        libbuild.build()
+    assert (tmp_path / "LIBRARY").read_text().split() == libbuild.SOURCES
+    assert (tmp_path / "PEAK_LIBRARY").read_text().split() == libbuild.PEAK_SOURCES
+    assert not (tmp_path / "BINDING").exists()
