@@ -299,10 +299,10 @@ Maybe logprob_workspace(const Tensor &logits, int top)
     return workspace(lib.logprob_fwd_ws(type, r.rows, r.cols, top), logits.device());
 }
 
-std::tuple<Maybe, Tensor, Tensor, Tensor, Maybe, Maybe> logprob_forward(const Tensor &z,
-                                                                        const Maybe &targets,
-                                                                        int top, double scale,
-                                                                        const Maybe &ws)
+std::tuple<Maybe, Tensor, Tensor, Tensor, Maybe, Maybe>
+logprob_forward(const Tensor &z, const Maybe &targets, int top, double scale, Maybe logp,
+                Maybe lse, Maybe entropy, Maybe stats, Maybe top_logp, Maybe top_index,
+                const Maybe &ws)
 {
     Rows r;
     const int type = float_rows(z, "logits", &r);
@@ -316,24 +316,36 @@ std::tuple<Maybe, Tensor, Tensor, Tensor, Maybe, Maybe> logprob_forward(const Te
     };
     if (top < 0)
         call(MICONV_ERR_SHAPE, "logprob_fwd");
-    Results out(r.rows * (5LL + top), z);
-    Maybe logp, top_logp, top_index;
-    const Tensor stats = out.next(last(2));
-    const Tensor lse = out.next(shape), entropy = out.next(shape);
-    if (targets)
-        logp = out.next(shape);
-    if (top) {
-        top_logp = out.next(last(top));
-        top_index = empty(last(top), z, at::kLong);
+    const bool new_logp = targets && !logp, new_top = top && !top_logp;
+    const int64_t floats = (stats ? 0 : 2) + !lse + !entropy + new_logp + (new_top ? top : 0);
+    if (floats) {
+        Results out(r.rows * floats, z);
+        if (!stats)
+            stats = out.next(last(2));
+        if (!lse)
+            lse = out.next(shape);
+        if (!entropy)
+            entropy = out.next(shape);
+        if (new_logp)
+            logp = out.next(shape);
+        if (new_top)
+            top_logp = out.next(last(top));
     }
+    if (top && !top_index)
+        top_index = empty(last(top), z, at::kLong);
     const Workspace s(ws, lib.logprob_fwd_ws(type, r.rows, r.cols, top), z.device());
-    const auto at = [](const Maybe &t) { return t ? t->data_ptr() : nullptr; };
     call(lib.logprob_fwd(type, r.rows, r.cols, z.data_ptr(), r.ld, tp, (float)scale, top,
-                         (float *)at(logp), (float *)lse.data_ptr(), (float *)entropy.data_ptr(),
-                         (float *)stats.data_ptr(), (float *)at(top_logp),
-                         (long long *)at(top_index), s.p, s.bytes, stream()),
+                         vector<float>(logp, "logp", r.rows, at::kFloat),
+                         vector<float>(lse, "lse", r.rows, at::kFloat),
+                         vector<float>(entropy, "entropy", r.rows, at::kFloat),
+                         vector<float>(stats, "stats", 2 * r.rows, at::kFloat),
+                         vector<float>(top_logp, "top_logp", r.rows * top, at::kFloat),
+                         vector<long long>(top_index, "top_index", r.rows * top, at::kLong), s.p,
+                         s.bytes, stream()),
          "logprob_fwd");
-    return {logp, lse, entropy, stats, top_logp, top_index};
+    for (const Maybe *t : {&logp, &lse, &entropy, &stats, &top_logp, &top_index})
+        written(*t);
+    return {logp, *lse, *entropy, *stats, top_logp, top_index};
 }
 
 Tensor logprob_backward(const Tensor &z, const Tensor &stats, const Maybe &targets,

@@ -91,12 +91,15 @@ def logprob_workspace(logits, top=0):
     return _binding().logprob_workspace(logits, top)
 
 
-def logprob_fwd(logits, targets=None, top=0, scale=1.0, ws=None):
+def logprob_fwd(logits, targets=None, top=0, scale=1.0, ws=None, logp=None, lse=None,
+                entropy=None, stats=None, top_logp=None, top_index=None):
     """LogProbs of the rows of logits [..., vocab] under softmax(scale * logits):
     the log probabilities of targets [...] (int64; negative: none given), the
     log of the softmax's sum, its entropy, the top (at most 64, or vocab where that
-    is fewer) likeliest tokens, and the statistics that logprob_bwd takes."""
-    return LogProbs(*_binding().logprob_fwd(logits, targets, top, scale, ws))
+    is fewer) likeliest tokens, and the statistics that logprob_bwd takes.  Given
+    results have as many elements as LogProbs states, side by side."""
+    return LogProbs(*_binding().logprob_fwd(logits, targets, top, scale, logp, lse, entropy, stats,
+                                            top_logp, top_index, ws))
 
 
 def logprob_bwd(logits, stats, targets=None, dlogp=None, entropy=None, dentropy=None, scale=1.0,

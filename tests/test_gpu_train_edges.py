@@ -265,3 +265,42 @@ def test_results_in_given_tensors_are_seen_by_autograd():
         m.grad_clip([z], 1.0)
         m.layernorm_fwd(x, w, w, y=z)
     m.layernorm_fwd(x, w, w, y=z)
+
+
+@pytest.mark.parametrize("shape", [(6, 50), (2, 3, 9000), (1, 70001), (500,)])
+@pytest.mark.parametrize("given", ["logp", "lse", "entropy", "stats", "top_logp", "top_index",
+                                   "all"])
+def test_logprob_into_given_tensors(shape, given):
+    """Any of the results, or all, in the caller's tensors; the others are new."""
+    import paper_1903_06934_amd as m
+    z = randn(4, *shape).cuda()
+    t = torch.zeros(shape[:-1], dtype=torch.int64, device="cuda")
+    want = m.logprob_fwd(z, t, top=4, scale=0.7)
+    mine = {k: torch.full_like(v, 77) for k, v in want._asdict().items() if given in (k, "all")}
+    version = {k: v._version for k, v in mine.items()}
+    got = m.logprob_fwd(z, t, top=4, scale=0.7, **mine)
+    for k, v in want._asdict().items():
+        assert torch.equal(getattr(got, k), v), k
+    for k, v in mine.items():
+        assert getattr(got, k).data_ptr() == v.data_ptr() and v._version > version[k]
+        assert torch.equal(v, getattr(want, k))
+
+
+def test_logprob_refuses_given_tensors():
+    import paper_1903_06934_amd as m
+    z, t = randn(5, 6, 50).cuda(), torch.arange(6, device="cuda")
+    new = lambda *s: torch.zeros(s, device="cuda")
+    for bad in ({"lse": new(5)}, {"lse": new(6).double()}, {"entropy": new(6).cpu()},
+                {"stats": new(6)}, {"stats": new(2, 6).t()}, {"top_logp": new(6, 2)},
+                {"top_index": new(6, 3)}, {"logp": new(12)[::2]}):
+        with pytest.raises(ValueError):
+            m.logprob_fwd(z, t, top=3, **bad)
+    with pytest.raises(ValueError):
+        m.logprob_fwd(z, t, top_logp=new(6, 3))  # without a top
+    both = new(6)
+    for bad in ({"lse": both, "entropy": both}, {"lse": z[0, :6]}):
+        with pytest.raises(m.MiconvError):
+            m.logprob_fwd(z, t, top=3, **bad)
+    with pytest.raises(m.MiconvError):
+        m.logprob_fwd(z, logp=new(6))  # of no targets
+    assert m.logprob_fwd(z, ws=None).logp is None
