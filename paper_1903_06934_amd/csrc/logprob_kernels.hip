@@ -346,7 +346,8 @@ __device__ __forceinline__ float log_prob(float z, Soft p, Done d, float scale)
 {
     if (d.none)
         return -kInf;
-    return (z - p.m) * scale - d.log_s;
+    const float u = z - p.m;  // beyond 32 bits where the scaled one need not be
+    return (u == -kInf && z > -kInf ? z * scale - p.m * scale : u * scale) - d.log_s;
 }
 
 // The logit of a row's given token.

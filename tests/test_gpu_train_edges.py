@@ -147,6 +147,27 @@ def test_logprob_of_a_lowest_value_mask_beyond_32_bits(rows, vocab, xt, scale):
     assert_close(dz, rz, 8 * U * size + half_ulp(rz, xt) * 1.01 + 1e-37, "dlogits")
 
 
+@pytest.mark.parametrize("rows,vocab", [(600, 70), (8, 3000), (600, 9001), (2, 70000)])
+@pytest.mark.parametrize("scale", [1e-6, 0.25])
+def test_logprob_of_logits_further_apart_than_32_bits(rows, vocab, scale):
+    """The difference of two logits may be beyond 32 bits where its scaled one, the
+    log probability, is not."""
+    import paper_1903_06934_amd as m
+    big = 3e38
+    z = torch.full((2, vocab), -big)
+    z[0, 7] = z[1, 3] = big
+    z[1, 4], z[1, 5] = 0.0, -INF
+    t = torch.tensor([0, 2])
+    top = 9
+    out = m.logprob_fwd(z.repeat(rows // 2, 1).cuda(), t.repeat(rows // 2).cuda(), top=top,
+                        scale=scale)
+    want = ref.logprob_fwd(z, t, top, scale)
+    for name in ("lse", "logp", "entropy", "top_logp"):
+        w = want[name].repeat(rows // 2, *[1] * (want[name].dim() - 1))
+        assert_close(getattr(out, name), w, 4 * U * w.abs().nan_to_num(0, 0, 0) + 64 * U, name)
+    assert torch.equal(out.top_index.cpu(), want["top_index"].repeat(rows // 2, 1))
+
+
 @pytest.mark.parametrize("rows", [6, 1200])
 @pytest.mark.parametrize("vocab,left,top", [(9, 1, 9), (70, 3, 64), (500, 10, 64), (1100, 5, 40)])
 @pytest.mark.parametrize("xt", [F32, BF16])
