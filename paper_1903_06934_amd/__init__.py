@@ -1,7 +1,7 @@
 """MI355X-native fp32 convolution training passes (forward, backward-data,
 backward-weight) behind a C ABI (include/miconv.h), and the operators that
-begin and end a training step around them (include/mitrain.h), with a thin
-ctypes binding.  The library is loaded on first use; see ``miconv.lib``."""
+begin and end a training step around them (include/mitrain.h), with thin
+bindings.  The library is loaded on first use; see ``miconv.lib``."""
 from .miconv import (MiconvError, conv_bwd_data, conv_bwd_weight, conv_fwd, conv_tune, lib,
                      output_size, plan_clear, plan_count, plan_get, plan_name, plan_set,
                      plan_workspace_size, pool_bwd, pool_fwd, pool_output_size, workspace_size,

@@ -2,12 +2,14 @@
 //
 // norm = sqrt(sum g^2) over all tensors, then g min(1, max_norm / norm): two
 // passes, as the factor needs every gradient.  Bound by memory: the first reads
-// them (61 M fp32 gradients: 44 us, 5.5 TB/s), the second reads and writes them
+// them (61 M fp32 gradients: 43 us, 5.7 TB/s), the second reads and writes them
 // (75 us, 6.5 TB/s, as the caches hold a part of what the first has read).  The
 // squares are summed in 64 bits (they overflow 32 from 2e19 on, and the
 // instructions are hidden behind the loads); every workgroup of the second pass
 // adds the first one's 1024 partial sums itself, in one order, which saves a
 // launch between the two.
+// The figures at the rules below are of whole calls replayed from a graph on
+// three inputs in turn, both sides of a rule in one run.
 #include <algorithm>
 
 #include "internal.h"
@@ -22,7 +24,7 @@ namespace {
 // no table of them has to reach the device before; more of them are first
 // written to a table in the workspace, kTensors a launch.
 constexpr int kTensors = 112;
-constexpr int kMaxParts = 1024;  // workgroups, and partial sums (2048: 122 -> 125 us)
+constexpr int kMaxParts = 1024;  // workgroups, and partial sums (2048: 123 -> 124 us)
 
 struct TensorList {
     GradEntry e[kTensors];
@@ -31,8 +33,8 @@ struct TensorList {
 static_assert(sizeof(TensorList) <= 3584, "kernel arguments");
 
 // Tensors scaled in place, or not at all, need half the arguments: their chunks
-// before each are counted here (280 small tensors: 25 us a call on the host, with
-// kTensors a launch 30; 1000 tensors 50 and 65).
+// before each are counted here (280 small tensors: 20 us a call on the host, with
+// kTensors a launch 23; 1000 tensors 47 and 62).
 constexpr int kInPlace = 2 * kTensors;
 
 struct InPlaceList {
@@ -130,7 +132,7 @@ __device__ __forceinline__ double block_sum(double v, double *lds)
 
 // F packs of the n elements at p in flight, a pack a thread and step.  LAST: the
 // last time that they are read (clipping 75 M gradients of which the caches
-// hold a part, 288 tensors: 82 us instead of 90).
+// hold a part, 288 tensors: 84 us instead of 91).
 template <class T, int F, bool LAST, class Use>
 __device__ __forceinline__ void each_pack(const T *p, int n, Use use)
 {
@@ -294,8 +296,8 @@ TensorList list_of(const GradEntry *e, int n)
 }
 
 // Workgroups: their shares differ by a chunk at most, so that few more chunks than
-// kMaxParts are two for each of half as many (36 tensors of 9.4 M bf16: 15.2 us,
-// in 1024 shares 17.6).
+// kMaxParts are two for each of half as many (36 tensors of 9.4 M bf16: 15.7 us,
+// in 1024 shares 18.2).
 int blocks_of(unsigned chunks)
 {
     const unsigned rounds = (chunks + kMaxParts - 1) / kMaxParts;

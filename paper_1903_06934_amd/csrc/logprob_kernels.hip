@@ -15,6 +15,9 @@
 // row a workgroup).  Backward, every element is read and written once and its
 // probability computed from the row's two statistics: 4096 x 32000 bf16 in
 // 90 us, 5.8 TB/s.
+// The figures at the rules below are of whole calls replayed from a graph on
+// three inputs in turn, both sides of a rule in one run: launches and their gaps
+// (1.6 us and more) are in them.
 #include <algorithm>
 
 #include "internal.h"
@@ -224,7 +227,7 @@ __device__ __forceinline__ void put_ranked(const uint64_t *keys, int n, int k, i
 // Of n keys in LDS, those that can be among the first k: a bound as above from
 // the keys dealt out to the groups, where the first one let many through (a row
 // with elements in few groups).  Ranking them all takes n^2 steps: 2 x 130 bf16
-// with 20 alternatives 14.0 us, so 7.9.  They stay in LDS; returns their number.
+// with 20 alternatives 14.0 us, so 8.2.  They stay in LDS; returns their number.
 template <class Tm, int SIZE>
 __device__ __forceinline__ int fewer_keys(typename Tm::Shared &sh, int n, int k)
 {
@@ -396,7 +399,8 @@ __global__ __launch_bounds__(SIZE < 256 ? 256 : SIZE) void logprob_rows(LogprobA
 {
     using Tm = Team<SIZE>;
     // Two packs in flight a thread: more lengthen the short rows (8000 x 1000 bf16
-    // 8.0 us, with 4 and 8 packs 9.2 and 12.3) and gain little on the long ones.
+    // 8.0 us, with 4 and 8 packs 9.4 and 12.7) and gain little on the long ones
+    // (4096 x 32000 49.8, 49.6 and 49.3; with one 53.1).
     constexpr int N = Pack<T>::N, F = 2, TEAMS = SIZE < 256 ? 256 / SIZE : 1;
     __shared__ typename Tm::Shared shared[TEAMS];
     const int team = TEAMS > 1 ? threadIdx.x / SIZE : 0;
@@ -541,7 +545,7 @@ __global__ __launch_bounds__(256) void logprob_join(LogprobArgs a, int piece, in
 // -------------------------------------------------------------------- backward
 // Groups of tpr threads (a power of two up to 256) take NV packs each: of a row
 // each, or, as a workgroup, of the piece blockIdx.x of row blockIdx.y.  NV = 2
-// (4096 x 32000 bf16: 92 us; with 1, 3, 4 and 8 packs 102, 102, 94 and 103).
+// (4096 x 32000 bf16: 96 us; with 1, 3, 4 and 8 packs 105, 104, 96 and 105).
 // An element in place is read before its thread writes it, and by no other.
 template <class T, int NV>
 __global__ __launch_bounds__(256) void logprob_back(LogprobBwdArgs a, int tpr)
@@ -599,14 +603,14 @@ int pack_of(int xtype) { return xtype == 0 ? 4 : 8; }
 // Pieces of a row, and the threads of a team.
 // Pieces: with a quarter of the CUs' number of rows or fewer, as many as fill
 // the CUs, of at least 4096 elements, up to kPieces (4 x 131072 bf16 with 20
-// alternatives: 13.1 us, whole rows 17.0; in two pieces 100 rows take 25.0,
-// whole 18.1: joining them costs 5).
+// alternatives: 13.3 us, whole rows 17.0; in two pieces 100 rows take 24.9,
+// whole 18.4: joining them costs 5).
 // A wave a row up to 16 packs a lane (8000 x 1000 bf16 with 5 alternatives:
-// 13.3 us, by workgroups 26.2; 8000 x 4000: 21 and 29), but with fewer rows than
-// two a CU up to two (100 x 4000 bf16: by waves 8.4, by workgroups 7.1; 128 x 1000
-// fp32, four packs: 6.8 and 6.4); a workgroup of 1024 threads from 12 packs a
-// thread on (200 x 131072 bf16 with 20: 18.9 us, with 256 threads 34.2; 2000 x
-// 40000 fp32, 10 packs: 57.8 and 55.4).
+// 13.4 us, by workgroups 25.9; 8000 x 4000: 21 and 30), but with fewer rows than
+// two a CU up to two (100 x 4000 bf16: by waves 5.9, by workgroups 5.0; 128 x 1000
+// fp32 with 5, four packs: 6.9 and 6.4); a workgroup of 1024 threads from 12 packs
+// a thread on (200 x 131072 bf16 with 20: 19.1 us, with 256 threads 34.6; 2000 x
+// 40000 fp32, 10 packs: 57.3 and 55.1).
 struct Cut {
     int piece, splits, team;
 };
@@ -644,8 +648,8 @@ hipError_t forward(int xtype, const LogprobArgs &a, hipStream_t stream)
     uint64_t *keys = (uint64_t *)((char *)a.ws + parts_bytes(a.rows, s.splits));
     const long long teams = s.team < 256 ? 256 / s.team : 1;
     // Loads that leave nothing in the caches, for logits larger than the
-    // last-level one holds beside the rest (4096 x 32000 bf16: 49.3 us instead of
-    // 54.4; 500 x 8191 bf16: 7.3 with them, 6.0 without).
+    // last-level one holds beside the rest (4096 x 32000 bf16: 49.8 us instead of
+    // 54.5; 500 x 8191 bf16: 7.4 with them, 5.9 without).
     const bool through = a.rows * a.vocab * (long long)sizeof(T) > 100LL << 20;
     const long long most = s.splits > 1 ? a.rows : kMaxBlocks * teams;  // rows of a launch
     for (long long first = 0; first < a.rows; first += most) {

@@ -4,10 +4,14 @@
 // statistics and its result (16384 x 4096 bf16: forward 47 us, 5.7 TB/s; backward
 // 80 us with the sums of dw and db, 5.0 TB/s, against the 5.3 of a large copy).
 // Backward, about 17 instructions an element take nearly half of the time that
-// the memory does, and the two overlap but in part.  Rows too long for the
-// registers, and long rows of which there are few, go by pieces and are read
-// twice (32 x 100352 fp32 backward: 15 us).  Calls of few rows are bound by
+// the memory does, and the two overlap but in part.  Rows longer than
+// what a workgroup is given to hold (32768 elements forward, 8192 backward), and
+// long rows of which there are few, go by pieces and are read twice (32 x 100352
+// fp32 backward: 15 us).  Calls of few rows are bound by
 // launches and latencies (4 x 2048 bf16 forward: 3.4 us of kernel).
+// The figures at the rules below are of whole calls replayed from a graph on
+// three inputs in turn, both sides of a rule in one run: launches and their gaps
+// (1.6 us and more) are in them.
 #include <algorithm>
 #include <initializer_list>
 
@@ -24,8 +28,8 @@ namespace {
 // the next two a quarter's, the seventh a single one.  Each is one load or store
 // of whole registers; element by element two of 16 bits would meet in a register,
 // for which the loads have to be waited for where they are issued, and all loads
-// before them (16009 x 4369 f16 backward 127 us, element by element 195; forward
-// 82 and 97).
+// before them (16009 x 4369 f16 backward 129 us, element by element 188; forward
+// 86 and 101).
 // place: the element of place j in a pack of which `left` (>= 1) are left, or -1.
 template <int N>
 __device__ __forceinline__ int place(int j, int left)
@@ -146,7 +150,7 @@ __device__ __forceinline__ void load_weights(const TW *w, long long c, long long
 // row is read again by elements, and summed one sum at a time: such rows take
 // longer (16384 x 4096 bf16 of nothing else 134 us instead of 48), but all others
 // keep the registers that they need (4000 x 16384 fp32: 105 us, with these sums
-// taken from the packs 118).
+// taken from the packs 116).
 constexpr float kNear = 0x1p-16f;
 
 template <class T>
@@ -309,8 +313,8 @@ __device__ __forceinline__ Moments wave_merge(Moments m)
 }
 
 constexpr int kPieces = 64;
-// Packs in flight a thread of norm_fwd_pieces (1000 x 100000 bf16: 131 us, with 4
-// 137; 1 x 100000 11.5 and 14.0, with 1 10.4; 300 x 40000 fp32 31.0, 30.4 and 32.1).
+// Packs in flight a thread of norm_fwd_pieces (1000 x 100000 bf16: 130 us, with 4
+// 136; 1 x 100000 11.5 and 13.9, with 1 10.5; 300 x 40000 fp32 31.3, 30.6 and 32.3).
 constexpr int kFwdPacks = 2;
 
 // Rows cut into `splits` (at most kPieces) pieces of `piece` elements (a multiple
@@ -336,8 +340,8 @@ __global__ __launch_bounds__(256) void norm_fwd_pieces(NormFwdArgs a, long long 
             if (at < len)
                 raw[i] = load_places<T>(x + at, len - at);
         }
-        // Equal elements have that number as their mean: by sums of halves, which
-        // then are exact, and where some are missing by a correction as there.
+        // Equal elements have that number as their mean: sums of halves are exact
+        // for them, and where places are missing the mean is corrected as above.
         float half[F * N], q = 0.f;
 #pragma unroll
         for (int i = 0; i < F; i++)
@@ -660,7 +664,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_sum(const float *parts, int n, 
 }
 
 // The same for few parts of many columns: a thread a column (187 x 35904 bf16, 7
-// parts: 21.4 us in all, with half-waves 25.8).
+// parts: 21.7 us in all, with half-waves 24.6).
 constexpr int kFewParts = 32;
 
 template <class TW>
@@ -862,17 +866,18 @@ RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
 {
     const int n = pack_of(xtype);
     const long long packs = (cols + n - 1) / n;
-    // Few rows above 16384 elements: by pieces over more CUs (16 x 32768 bf16
-    // 9.5 us, by registers 10.8; 256 rows 18.4 and 13.2).
+    // Few rows above 16384 elements: by pieces over more CUs, which is faster in
+    // the longest fp32 rows and about level else (16 x 32768 fp32 9.8 us, by
+    // registers 11.8; bf16 9.8 and 9.6, 64 rows 10.5 and 9.8, 256 rows 17.9 and 12.0).
     if (forward && cols > 16384 && rows <= 64)
         return RowPlan{0, 0, 0, false};
     // Backward by pieces above 8192 elements (1024 threads have too few registers:
-    // 4096 x 16384 fp32 285 us, by pieces 232; bf16 113 and 121), and where the
+    // 4096 x 16384 fp32 285 us, by pieces 231; bf16 113 and 121), and where the
     // rows' partial sums of dw and db would be about as many as their elements:
-    // up to 2048 rows from 4096 16-bit elements on (1040 x 4096 23.6 and 16.2, 4 x
-    // 8192 14.9 and 8.4; 3100 x 8192 45.2 and 48.8), of 256 rows at least from 2048
-    // on (520 x 2048 15.2 and 12.5; 60 x 2048 9.1 and 11.0), up to 512 rows from
-    // 4096 fp32 elements on (260 x 8192 19.7 and 15.0; 1040 x 8192 29.9 and 35.1).
+    // up to 2048 rows from 4096 16-bit elements on (1040 x 4096 23.8 and 17.0, 4 x
+    // 8192 14.8 and 8.5; 3100 x 8192 45.7 and 49.8), of 256 rows at least from 2048
+    // on (520 x 2048 14.5 and 12.5; 60 x 2048 9.0 and 11.5), up to 512 rows from
+    // 4096 fp32 elements on (260 x 8192 19.7 and 15.3; 1040 x 8192 30.5 and 36.0).
     const bool sums = n == 4 ? cols >= 4096 && rows <= 512
                              : rows <= 2048 && cols >= (rows < 256 ? 4096 : 2048);
     if (!forward && (cols > 8192 || sums))
@@ -882,15 +887,15 @@ RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
         while (packs > tpr)
             tpr *= 2;
         // Half the threads with an element more each where that holds the row
-        // (30000 x 270 f16: forward 10.3 us instead of 17.4, backward 17.9 instead
-        // of 26.7).
+        // (30000 x 270 f16: forward 11.5 us instead of 17.7, backward 18.6 instead
+        // of 22.9).
         const bool tail = tpr > 1 && cols <= tpr / 2 * (n + 1);
         return RowPlan{tail ? tpr / 2 : tpr, 1, 256, tail};
     }
     // As few idle places as can be; then more packs a thread before more
     // threads, as a row inside a wave needs no barrier.  Forward, few rows are
-    // spread over more threads (4 x 2048 bf16: 3.4 us on 256 threads a row,
-    // 8.5 on 64).
+    // spread over more threads (4 x 2048 bf16: 5.4 us on 256 threads a row, 5.6 on
+    // 128; 128 x 1000 fp32 5.4 and 5.6; 256 x 4096 fp32 6.5 and 6.2).
     const auto waves = [&](int nv) { return (packs + 64 * nv - 1) / (64 * nv); };
     const auto idle = [&](int nv) {
         const long long w = waves(nv);
@@ -916,9 +921,9 @@ RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
     // A row a little longer than whole packs of all its threads: one element a
     // thread beside them instead of a pack, where a thread then holds fewer places
     // and the row takes no more threads (forward 12544 x 1025 bf16 12.3 us, by packs
-    // 18.1; 9000 x 3080 fp32 51.0 and 82.0; 4000 x 2049 fp32 14.6 and 14.2. Backward
-    // 12544 x 513 fp32 21.0 and 22.9; 9000 x 3073 f16 55.2 and 68.9).  Not backward
-    // over several waves in fp32 (9000 x 2049 55.8 and 49.8).
+    // 19.2; 9000 x 3080 fp32 50.7 and 85.2; 4000 x 2049 fp32 14.9 and 14.8. Backward
+    // 12544 x 513 fp32 21.1 and 22.8; 9000 x 3073 f16 55.2 and 58.3).  Not backward
+    // over several waves in fp32 (9000 x 2049 55.6 and 50.1).
     int cost = tpr / 64 * best * n;
     for (int nv = 1; nv * n <= kValues; nv++)
         for (int w = 1; w <= (!forward && n == 4 ? 1 : tpr / 64); w++)
@@ -931,7 +936,7 @@ RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
 }
 
 // Workgroups of the register kernels.  Forward: 1536 threads a CU (16384 rows
-// of 4096 bf16: 51.6 us; with 1024, 2048 and 4096 threads 52.9, 57.8 and 53.5).
+// of 4096 bf16: 49.7 us; with 1024, 2048 and 4096 threads 52.9, 55.1 and 50.4).
 int fwd_blocks(const RowPlan &p, long long rows)
 {
     const long long groups = std::max(1, p.block / p.tpr);
@@ -939,12 +944,12 @@ int fwd_blocks(const RowPlan &p, long long rows)
 }
 
 // Backward: each workgroup adds 2 x cols partial sums to write and to read
-// again, so 512 threads a CU (16384 x 4096 bf16: 83.7 us; with 768 and 1024
-// 92.5 and 102.4); 1024 where a thread holds one pack, too little in flight,
-// and takes at least five rows (31000 x 1500 bf16: 68.6 us instead of 94.0;
-// 3000 x 1500, three rows: 24.9 instead of 18.8; with an element beside the pack
-// 30000 x 300 fp32 26.7 instead of 24.7).  A single workgroup, which needs no sum
-// after it, takes up to two rows a group (7 x 1024 bf16: 8.6 us instead of 9.8).
+// again, so 512 threads a CU (16384 x 4096 bf16: 83.4 us; with 768 and 1024
+// 90.1 and 103.2); 1024 where a thread holds one pack, too little in flight,
+// and takes at least five rows (31000 x 1500 bf16: 68.2 us instead of 94.1;
+// 3000 x 1500, three rows: 24.6 instead of 18.6; with an element beside the pack
+// 30000 x 300 fp32 26.8 instead of 24.7).  A single workgroup, which needs no sum
+// after it, takes up to two rows a group (7 x 1024 bf16: 8.9 us instead of 9.9).
 int bwd_blocks(const RowPlan &p, long long rows)
 {
     const long long groups = std::max(1, p.block / p.tpr);
@@ -958,10 +963,10 @@ int bwd_blocks(const RowPlan &p, long long rows)
 }
 
 // Loads that leave nothing in the caches, for inputs larger than the last-level
-// one holds beside the rest (from 100 MB on: 16384 x 4096 bf16 49.2 us instead
-// of 51.4 forward, 83.5 instead of 86.7 backward; 9000 x 4096 26.7 with them 29.6),
-// of whole cache lines (16009 x 4369 bf16, lines shared by rows: 97.6 with them,
-// 81.2 without).
+// one holds beside the rest (from 100 MB on: 16384 x 4096 bf16 49.3 us instead
+// of 51.4 forward, 83.5 instead of 86.9 backward; 9000 x 4096 26.8, with them 29.6),
+// of whole cache lines (16009 x 4369 bf16, lines shared by rows: 99.3 with them,
+// 83.2 without).
 bool streams(long long rows, long long cols, size_t elem, std::initializer_list<Rows> in)
 {
     bool lines = rows * cols * (long long)elem > 100LL << 20;
@@ -992,7 +997,7 @@ PiecePlan piece_plan(int xtype, long long rows, long long cols, bool forward)
 
 // Chunks of rows of norm_bwd_cols: one up to 64 rows, which then needs no sum
 // over the chunks; else as many as give every CU two workgroups, of 16 rows at
-// least (169 x 25083 f16: 24.1 us, of 64 32.1).
+// least (169 x 25083 f16: 18.5 us, of 64 22.0).
 int row_chunks(int xtype, long long rows, long long cols)
 {
     const int n = pack_of(xtype);
