@@ -327,7 +327,8 @@ def _run_own(state):
     case, d, out = state["case"], state["in"], state["out"]
     op = case["op"]
     if op == "policy":
-        r = m.policy_loss(d["logp"], d["old"], d["advantages"], ref_logp=d.get("ref"),
+        r = m.policy_loss(d["logp"], d["old"], d["advantages"],
+                          by_sequence=case["by"] == "sequence", ref_logp=d.get("ref"),
                           entropy=d.get("entropy"), mask=d.get("mask"), starts=d["starts"],
                           clip_low=_CLIP[0], clip_high=_CLIP[1],
                           dual_clip=_DUAL if case["dual"] else math.inf, kl=case["kl"] or "low",
