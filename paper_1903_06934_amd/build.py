@@ -1,5 +1,5 @@
 """Build libmiconv.so (the HIP kernels and the C ABI), _mitrain.so (the Python
-binding of include/mitrain.h) and libmipeak.so (the benchmark's measured
+binding of include/mitrain.h and include/mistep.h) and libmipeak.so (the benchmark's measured
 reference points) in-tree for gfx950."""
 from __future__ import annotations
 
@@ -17,10 +17,12 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIBRARY = os.path.join(PKG, "libmiconv.so")
 SOURCES = ["api.hip", "conv_kernels.hip", "wino_kernels.hip", "pool_kernels.hip",
-           "train_api.hip", "norm_kernels.hip", "logprob_kernels.hip", "clip_kernels.hip"]
+           "train_api.hip", "norm_kernels.hip", "logprob_kernels.hip", "clip_kernels.hip",
+           "step_api.hip", "dropout_kernels.hip", "residual_kernels.hip", "loss_kernels.hip"]
 PEAK_LIBRARY = os.path.join(PKG, "libmipeak.so")
 PEAK_SOURCES = ["peaks.hip"]
 BINDING = os.path.join(PKG, "_mitrain.so")
+BINDING_SOURCES = ["binding.cpp", "binding_step.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -70,16 +72,20 @@ def _binding(verbose):
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     include = os.path.join(os.path.dirname(torch.__file__), "include")
     tmp = BINDING + ".tmp"
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall",
            "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-I", os.path.join(ROOT, "include"),
            "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
            "-isystem", sysconfig.get_paths()["include"],
-           "-isystem", os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include"),
-           os.path.join(CSRC, "binding.cpp"), "-o", tmp,
-           "-L", lib, "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
-    _run(cmd, verbose)
+           "-isystem", os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include")]
+    with tempfile.TemporaryDirectory() as obj_dir, ThreadPoolExecutor(2) as pool:
+        objs = [os.path.join(obj_dir, s + ".o") for s in BINDING_SOURCES]
+        list(pool.map(lambda so: _run(
+            cmd + ["-c", os.path.join(CSRC, so[0]), "-o", so[1]], verbose),
+            zip(BINDING_SOURCES, objs)))
+        _run(["g++", "-shared"] + objs + ["-o", tmp, "-L", lib, "-lc10", "-lc10_hip",
+                                          "-ltorch_cpu", "-ltorch_python"], verbose)
     return tmp
 
 

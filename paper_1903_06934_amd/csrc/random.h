@@ -1,0 +1,115 @@
+// The random numbers of include/mistep.h on the device.
+#pragma once
+
+#include <stdint.h>
+#include <hip/hip_runtime.h>
+
+#include "step.h"
+
+namespace miconv {
+
+// Philox4x32-10 of the counter {g, step, layer}: ten rounds of two 32 x 32 -> 64
+// bit products, whose low words change places with the other two words.
+__device__ __forceinline__ void philox(uint32_t key0, uint32_t key1, uint32_t step, uint32_t layer,
+                                       unsigned long long g, uint32_t (&w)[4])
+{
+    uint32_t a = (uint32_t)g, b = (uint32_t)(g >> 32), c = step, d = layer;
+#pragma unroll
+    for (int i = 0; i < 10; i++) {
+        const unsigned long long p = (unsigned long long)0xD2511F53u * a;
+        const unsigned long long q = (unsigned long long)0xCD9E8D57u * c;
+        a = (uint32_t)(q >> 32) ^ b ^ key0;
+        c = (uint32_t)(p >> 32) ^ d ^ key1;
+        b = (uint32_t)q;
+        d = (uint32_t)p;
+        key0 += 0x9E3779B9u;
+        key1 += 0xBB67AE85u;
+    }
+    w[0] = a;
+    w[1] = b;
+    w[2] = c;
+    w[3] = d;
+}
+
+// What a kernel holds of its Drop.
+struct Dropper {
+    uint32_t below, key0, key1, step, layer;
+    float scale;
+
+    __device__ __forceinline__ explicit Dropper(const Drop &d)
+        : below(d.below), key0(d.key0), key1(d.key1), step(d.step), layer(d.layer), scale(d.scale)
+    {
+        if (d.step_at && below)
+            step += (uint32_t)*d.step_at;
+    }
+
+    __device__ __forceinline__ void group(unsigned long long g, uint32_t (&w)[4]) const
+    {
+        philox(key0, key1, step, layer, g, w);
+    }
+
+    // The bits of element i of 2 * (words) elements.
+    __device__ __forceinline__ bool kept(uint32_t word, int odd) const
+    {
+        return (odd ? word >> 16 : word & 0xffff) >= below;
+    }
+
+    // The words of elements e .. e + N - 1 (N 4 or 8), which may lie in two groups.
+    template <int N>
+    __device__ __forceinline__ void words(long long e, uint32_t (&out)[N / 2]) const
+    {
+        uint32_t w[8];
+        const int o = (int)(e & 7);
+        {
+            uint32_t g[4];
+            group((unsigned long long)e >> 3, g);
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                w[i] = g[i];
+        }
+        if (N == 8 && o == 0) {
+#pragma unroll
+            for (int i = 0; i < N / 2; i++)
+                out[i] = w[i];
+            return;
+        }
+#pragma unroll
+        for (int i = 4; i < 8; i++)
+            w[i] = 0;
+        if (o + N > 8) {
+            uint32_t g[4];
+            group(((unsigned long long)e >> 3) + 1, g);
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                w[4 + i] = g[i];
+        }
+        // Shifted by o half words: four, two, one.
+        if (o & 4)
+#pragma unroll
+            for (int i = 0; i < 6; i++)
+                w[i] = w[i + 2];
+        if (o & 2)
+#pragma unroll
+            for (int i = 0; i < 5; i++)
+                w[i] = w[i + 1];
+        if (o & 1)
+#pragma unroll
+            for (int i = 0; i < N / 2; i++)
+                w[i] = w[i] >> 16 | w[i + 1] << 16;
+#pragma unroll
+        for (int i = 0; i < N / 2; i++)
+            out[i] = w[i];
+    }
+
+    // Whether element e is kept.
+    __device__ __forceinline__ bool one(long long e) const
+    {
+        uint32_t g[4];
+        group((unsigned long long)e >> 3, g);
+        const int h = (int)(e & 7);
+        const uint32_t w = h & 4 ? (h & 2 ? g[3] : g[2]) : (h & 2 ? g[1] : g[0]);
+        return kept(w, h & 1);
+    }
+};
+
+}  // namespace miconv

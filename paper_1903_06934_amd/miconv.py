@@ -107,6 +107,28 @@ def lib():
         getattr(L, name).restype = _I
     for name in ("layernorm_fwd", "layernorm_bwd", "logprob_fwd", "grad"):
         getattr(L, name + "_workspace_size").restype = _Z
+    # include/mistep.h
+    _D, _U = ctypes.c_double, ctypes.c_uint
+    drop = [_D, ctypes.c_ulonglong, _U, _U, _P]
+    L.dropout_fwd.argtypes = rows + [_P, _L, _P, _L] + drop + [_P, _L, _P]
+    L.dropout_bwd.argtypes = rows + [_P, _L] + drop + [_P, _L, _P]
+    L.residual_norm_fwd_workspace_size.argtypes = rows
+    L.residual_norm_bwd_workspace_size.argtypes = rows
+    L.residual_norm_fwd.argtypes = ([_I] + rows + [_P, _L, _P, _L] + drop +
+                                    [_P, _P, _F, _P, _L, _P, _L, _P, _P, _P, _Z, _P])
+    L.residual_norm_bwd.argtypes = ([_I] + rows + [_P, _L, _P, _L, _P, _P, _P, _P, _L] + drop +
+                                    [_P, _L, _P, _L, _P, _P, _P, _Z, _P])
+    L.policy_loss_workspace_size.argtypes = [_L, _L]
+    L.policy_loss.argtypes = ([_L, _L] + [_P] * 5 + [_I, _P, _P, _D, _D, _D, _I, _D, _D, _I, _D, _D]
+                              + [_P] * 4 + [_Z, _P])
+    L.preference_loss_workspace_size.argtypes = [_L, _L]
+    L.preference_loss.argtypes = ([_L, _L] + [_P] * 4 + [_D, _I, _D, _D, _I, _D] + [_P] * 4 +
+                                  [_Z, _P])
+    for name in ("dropout_fwd", "dropout_bwd", "residual_norm_fwd", "residual_norm_bwd",
+                 "policy_loss", "preference_loss"):
+        getattr(L, name).restype = _I
+    for name in ("residual_norm_fwd", "residual_norm_bwd", "policy_loss", "preference_loss"):
+        getattr(L, name + "_workspace_size").restype = _Z
     _lib = L
     return L
 

@@ -1,0 +1,224 @@
+"""include/mistep.h on the CPU: the library exports what it declares, and every call
+refuses bad arguments before touching a device.  The pointers are fake device addresses
+that are never dereferenced."""
+import os
+import re
+
+import pytest
+import torch
+
+import paper_1903_06934_amd as m
+from test_train_abi import (A, ALIAS, ALIGN, B, BF16, BIG, C, D, E, F16, F32, G, H, L, NULL, S,
+                            SHAPE, TYPE, VALUE, W, WS, inf, launched, nan)
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include",
+                      "mistep.h")
+X = 0xA0000000  # one more tensor
+
+
+def test_exports_every_declared_function(L):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b([a-z_][a-z0-9_]*)\s*\(", text)) - {"defined"}
+    assert names == {"dropout_fwd", "dropout_bwd", "residual_norm_fwd", "residual_norm_bwd",
+                     "residual_norm_fwd_workspace_size", "residual_norm_bwd_workspace_size",
+                     "policy_loss", "policy_loss_workspace_size", "preference_loss",
+                     "preference_loss_workspace_size"}
+    for n in names:
+        assert hasattr(L, n), n
+
+
+def drop(L, xtype=F32, rows=8, cols=64, x=A, ldx=64, res=B, ldr=64, p=0.1, seed=2 ** 64 - 1,
+         layer=2 ** 32 - 1, step=2 ** 32 - 1, at=C, y=D, ldy=64):
+    return L.dropout_fwd(xtype, rows, cols, x, ldx, res, ldr, p, seed, layer, step, at, y, ldy, None)
+
+
+@pytest.mark.parametrize("want,args", [
+    (TYPE, dict(xtype=3)), (SHAPE, dict(rows=-1)), (SHAPE, dict(cols=0)), (SHAPE, dict(ldx=63)),
+    (SHAPE, dict(ldr=63)), (SHAPE, dict(ldy=63)), (SHAPE, dict(rows=1 << 31)),
+    (SHAPE, dict(ldx=1 << 47)), (VALUE, dict(p=-1e-9)), (VALUE, dict(p=1.0001)),
+    (VALUE, dict(p=nan)), (NULL, dict(x=None)), (NULL, dict(y=None)), (NULL, dict(x=None, y=None)),
+    (ALIGN, dict(x=A + 2)), (ALIGN, dict(res=B + 1, xtype=BF16)), (ALIGN, dict(at=C + 4)),
+    (ALIGN, dict(y=D + 2)), (ALIAS, dict(y=A + 4)), (ALIAS, dict(y=B + 256)),
+    (ALIAS, dict(y=A, ldy=65)), (ALIAS, dict(y=C)), (ALIAS, dict(y=A, res=A, ldr=65))], ids=str)
+def test_dropout_fwd_refuses(L, want, args):
+    assert drop(L, **args) == want
+
+
+@pytest.mark.parametrize("args", [
+    dict(), dict(res=None, ldr=0), dict(y=A), dict(y=B), dict(y=A, res=A), dict(res=A),
+    dict(at=None), dict(p=0.0), dict(p=1.0), dict(rows=0, x=None, y=None, res=None),
+    dict(xtype=F16, x=A + 2), dict(ldx=128, ldy=128, y=A + 256)], ids=str)
+def test_dropout_fwd_takes(L, args):
+    assert drop(L, **args) == launched()
+
+
+def drop_bwd(L, xtype=BF16, rows=8, cols=64, dy=A, lddy=64, p=0.1, at=None, dx=B, lddx=64):
+    return L.dropout_bwd(xtype, rows, cols, dy, lddy, p, 1, 0, 0, at, dx, lddx, None)
+
+
+@pytest.mark.parametrize("want,args", [
+    (TYPE, dict(xtype=-1)), (SHAPE, dict(lddy=1)), (SHAPE, dict(lddx=1)), (VALUE, dict(p=2.0)),
+    (NULL, dict(dy=None)), (NULL, dict(dx=None)), (ALIAS, dict(dx=A + 2)),
+    (ALIAS, dict(dx=A, lddx=65)), (ALIAS, dict(at=B))], ids=str)
+def test_dropout_bwd_refuses(L, want, args):
+    assert drop_bwd(L, **args) == want
+
+
+@pytest.mark.parametrize("args", [dict(), dict(dx=A), dict(rows=0, dy=None, dx=None)], ids=str)
+def test_dropout_bwd_takes(L, args):
+    assert drop_bwd(L, **args) == launched()
+
+
+def norm_fwd(L, xtype=F32, wtype=F32, rows=8, cols=64, x=A, ldx=64, res=B, ldr=64, p=0.1, at=None,
+             w=C, b=D, eps=1e-5, total=E, ldt=64, y=G, ldy=64, mean=H, rstd=W, ws=S, n=BIG):
+    return L.residual_norm_fwd(xtype, wtype, rows, cols, x, ldx, res, ldr, p, 1, 2, 3, at, w, b,
+                               eps, total, ldt, y, ldy, mean, rstd, ws, n, None)
+
+
+LONG = dict(cols=1 << 20, ldx=1 << 20, ldr=1 << 20, ldt=1 << 20, ldy=1 << 20, rows=2)
+
+
+@pytest.mark.parametrize("want,args", [
+    (TYPE, dict(xtype=9)), (TYPE, dict(wtype=BF16)), (TYPE, dict(xtype=BF16, wtype=F16)),
+    (SHAPE, dict(cols=0)), (SHAPE, dict(ldx=1)), (SHAPE, dict(ldr=1)), (SHAPE, dict(ldt=1)),
+    (SHAPE, dict(ldy=1)), (VALUE, dict(eps=-1.0)), (VALUE, dict(eps=nan)), (VALUE, dict(p=nan)),
+    (VALUE, dict(p=-0.5)), (NULL, dict(x=None)), (NULL, dict(res=None)), (NULL, dict(total=None)),
+    (NULL, dict(y=None)), (NULL, dict(res=None, total=None)), (ALIGN, dict(w=C + 2)),
+    (ALIGN, dict(total=E + 1)), (ALIAS, dict(total=A)), (ALIAS, dict(y=A)), (ALIAS, dict(y=B)),
+    (ALIAS, dict(y=E)), (ALIAS, dict(total=B, ldt=65)), (ALIAS, dict(mean=W)),
+    (ALIAS, dict(total=B, y=B)), (ALIAS, dict(at=H)), (WS, dict(LONG, n=8)),
+    (WS, dict(LONG, ws=None))], ids=str)
+def test_residual_norm_fwd_refuses(L, want, args):
+    assert norm_fwd(L, **args) == want
+
+
+@pytest.mark.parametrize("args", [
+    dict(), dict(total=B), dict(w=None, b=None, mean=None, rstd=None), dict(at=X),
+    dict(rows=0, x=None, res=None, total=None, y=None), dict(xtype=BF16, wtype=BF16, x=A + 2)],
+    ids=str)
+def test_residual_norm_fwd_takes(L, args):
+    assert norm_fwd(L, **args) == launched()
+
+
+def norm_bwd(L, xtype=F32, wtype=F32, rows=8, cols=64, dy=A, lddy=64, total=B, ldt=64, mean=C,
+             rstd=D, w=E, dt=G, lddt=64, p=0.1, at=None, dr=H, lddr=64, dx=X, lddx=64, dw=W,
+             db=0xB0000000, ws=S, n=BIG):
+    return L.residual_norm_bwd(xtype, wtype, rows, cols, dy, lddy, total, ldt, mean, rstd, w, dt,
+                               lddt, p, 1, 2, 3, at, dr, lddr, dx, lddx, dw, db, ws, n, None)
+
+
+@pytest.mark.parametrize("want,args", [
+    (TYPE, dict(xtype=7)), (TYPE, dict(wtype=F16)), (SHAPE, dict(lddy=1)), (SHAPE, dict(ldt=1)),
+    (SHAPE, dict(lddt=1)), (SHAPE, dict(lddr=1)), (SHAPE, dict(lddx=1)), (VALUE, dict(p=1.5)),
+    (NULL, dict(dy=None)), (NULL, dict(total=None)), (NULL, dict(mean=None)),
+    (NULL, dict(rstd=None)), (NULL, dict(dr=None, dx=None, dw=None, db=None)),
+    (ALIGN, dict(dt=G + 2)), (ALIAS, dict(dr=A)), (ALIAS, dict(dx=G)), (ALIAS, dict(dx=H)),
+    (ALIAS, dict(dr=G, lddr=65)), (ALIAS, dict(dr=G + 4)), (ALIAS, dict(dw=E)),
+    (ALIAS, dict(ws=G)), (WS, dict(n=8)), (WS, dict(ws=None))], ids=str)
+def test_residual_norm_bwd_refuses(L, want, args):
+    assert norm_bwd(L, **args) == want
+
+
+@pytest.mark.parametrize("args", [
+    dict(), dict(dr=G), dict(dt=None, lddt=0), dict(dr=None, lddr=0), dict(dx=None, lddx=0),
+    dict(dr=None, dx=None), dict(dw=None, db=None), dict(w=None),
+    dict(rows=0, dy=None, total=None, mean=None, rstd=None, dt=None, dr=None, dx=None)], ids=str)
+def test_residual_norm_bwd_takes(L, args):
+    assert norm_bwd(L, **args) == launched()
+
+
+def policy(L, tokens=20000, seqs=10, lp=A, lo=B, lr=C, h=D, adv=E, by_seq=0, mask=G, starts=H,
+           low=0.2, high=0.2, dual=3.0, kl=2, kw=0.1, ew=0.1, mean=1, count=0.0, scale=1.0, stats=W,
+           dlp=X, dh=0xB0000000, ws=S, n=BIG):
+    return L.policy_loss(tokens, seqs, lp, lo, lr, h, adv, by_seq, mask, starts, low, high, dual,
+                         kl, kw, ew, mean, count, scale, stats, dlp, dh, ws, n, None)
+
+
+@pytest.mark.parametrize("want,args", [
+    (SHAPE, dict(tokens=-1)), (SHAPE, dict(tokens=1 << 31)), (SHAPE, dict(seqs=-1)),
+    (SHAPE, dict(seqs=1 << 31)), (SHAPE, dict(starts=None)), (VALUE, dict(low=-0.1)),
+    (VALUE, dict(low=1.1)), (VALUE, dict(low=nan)), (VALUE, dict(high=-0.1)),
+    (VALUE, dict(high=nan)), (VALUE, dict(dual=0.9)), (VALUE, dict(dual=nan)), (VALUE, dict(kl=3)),
+    (VALUE, dict(kl=-1)), (VALUE, dict(kw=inf)), (VALUE, dict(kw=1e39)), (VALUE, dict(ew=nan)),
+    (VALUE, dict(mean=3)), (VALUE, dict(mean=-1)), (VALUE, dict(mean=2, count=0.0)),
+    (VALUE, dict(mean=2, count=inf)), (VALUE, dict(mean=2, count=nan)), (VALUE, dict(scale=inf)),
+    (NULL, dict(starts=None, seqs=0)), (NULL, dict(starts=None, seqs=0, mean=0, by_seq=1)),
+    (NULL, dict(lp=None)), (NULL, dict(lo=None)), (NULL, dict(lr=None)), (NULL, dict(h=None)),
+    (NULL, dict(h=None, ew=0.0)), (NULL, dict(adv=None)), (NULL, dict(stats=None)),
+    (ALIGN, dict(lp=A + 2)), (ALIGN, dict(starts=H + 4)), (ALIGN, dict(stats=W + 1)),
+    (ALIAS, dict(dlp=A)), (ALIAS, dict(dh=D)), (ALIAS, dict(dlp=G)), (ALIAS, dict(stats=E)),
+    (ALIAS, dict(dlp=H)), (ALIAS, dict(ws=A)), (WS, dict(n=16)), (WS, dict(ws=None)),
+    (ALIGN, dict(ws=S + 8))], ids=str)
+def test_policy_loss_refuses(L, want, args):
+    assert policy(L, **args) == want
+
+
+@pytest.mark.parametrize("args", [
+    dict(), dict(lr=None, kw=0.0), dict(h=None, ew=0.0, dh=None), dict(mask=None),
+    dict(dlp=None, dh=None), dict(starts=None, seqs=0, mean=0), dict(by_seq=1, adv=E),
+    dict(tokens=0, lp=None, lo=None, lr=None, h=None, adv=None),
+    dict(seqs=0, by_seq=1, adv=None), dict(low=1.0, high=inf, dual=inf), dict(mean=2, count=1.0),
+    dict(tokens=8192, ws=None, n=0), dict(mask=G + 1), dict(kw=-1.0, ew=-1.0, scale=-2.0)], ids=str)
+def test_policy_loss_takes(L, args):
+    assert policy(L, **args) == launched()
+
+
+def prefer(L, tokens=20000, pairs=10, lp=A, lr=B, mask=C, starts=D, beta=0.1, form=0, smooth=0.1,
+           margin=0.0, mean=0, scale=1.0, stats=E, rewards=G, dlp=H, ws=S, n=BIG):
+    return L.preference_loss(tokens, pairs, lp, lr, mask, starts, beta, form, smooth, margin, mean,
+                             scale, stats, rewards, dlp, ws, n, None)
+
+
+@pytest.mark.parametrize("want,args", [
+    (SHAPE, dict(tokens=-1)), (SHAPE, dict(tokens=1 << 31)), (SHAPE, dict(pairs=-1)),
+    (SHAPE, dict(pairs=1 << 30)), (VALUE, dict(beta=0.0)), (VALUE, dict(beta=nan)),
+    (VALUE, dict(beta=inf)), (VALUE, dict(form=3)), (VALUE, dict(form=-1)),
+    (VALUE, dict(smooth=-0.1)), (VALUE, dict(smooth=1.1)), (VALUE, dict(smooth=nan)),
+    (VALUE, dict(margin=inf)), (VALUE, dict(scale=nan)), (NULL, dict(lp=None)),
+    (NULL, dict(starts=None)), (NULL, dict(stats=None)), (ALIGN, dict(lr=B + 2)),
+    (ALIGN, dict(starts=D + 4)), (ALIGN, dict(rewards=G + 2)), (ALIAS, dict(dlp=A)),
+    (ALIAS, dict(dlp=B)), (ALIAS, dict(rewards=E)), (ALIAS, dict(stats=C + 100)),
+    (ALIAS, dict(ws=H)), (WS, dict(n=16)), (WS, dict(ws=None))], ids=str)
+def test_preference_loss_refuses(L, want, args):
+    assert prefer(L, **args) == want
+
+
+@pytest.mark.parametrize("args", [
+    dict(), dict(lr=None), dict(mask=None), dict(rewards=None), dict(dlp=None),
+    dict(tokens=0, lp=None, lr=None, dlp=None), dict(pairs=0), dict(form=2, mean=1, margin=-1.0),
+    dict(tokens=100, ws=None, n=0)], ids=str)
+def test_preference_loss_takes(L, args):
+    assert prefer(L, **args) == launched()
+
+
+def test_workspace_sizes(L):
+    assert L.policy_loss_workspace_size(8192, 8192) == 0
+    assert L.policy_loss_workspace_size(8193, 1) > 0 and L.policy_loss_workspace_size(1, 8193) > 0
+    assert L.preference_loss_workspace_size(8192, 1024) == 0
+    assert L.preference_loss_workspace_size(8193, 1) > 0
+    assert L.preference_loss_workspace_size(1, 1025) > 0
+    for bad in ((-1, 1), (1 << 31, 1), (1, -1), (1, 1 << 31)):
+        assert L.policy_loss_workspace_size(*bad) == 0
+        assert L.preference_loss_workspace_size(*bad) == 0
+    # Each sequence, pair and chunk has its numbers: no more than some bytes a token.
+    assert L.policy_loss_workspace_size((1 << 31) - 1, 1000) < 1 << 25
+    for cols in (64, 8192, 40000):
+        for t in (F32, BF16):
+            assert (L.residual_norm_fwd_workspace_size(t, 100, cols) ==
+                    L.layernorm_fwd_workspace_size(t, 100, cols))
+            assert (L.residual_norm_bwd_workspace_size(t, 100, cols) ==
+                    L.layernorm_bwd_workspace_size(t, 100, cols))
+
+
+def test_binding_refuses(L):
+    """The binding's own checks, on CPU tensors."""
+    x, t, q = torch.zeros(4, 8), torch.zeros(4), torch.zeros(3, dtype=torch.int64)
+    for call in (lambda: m.dropout_fwd(x, 0.1, 1), lambda: m.dropout_bwd(x, 0.1, 1),
+                 lambda: m.residual_norm_fwd(x, x), lambda: m.residual_norm_bwd(x, x, t, t),
+                 lambda: m.residual_norm_workspace(True, x), lambda: m.policy_loss(t, t, t),
+                 lambda: m.preference_loss(t, t, q, 0.1), lambda: m.policy_workspace(t),
+                 lambda: m.preference_workspace(t, q), lambda: m.policy_loss(t, t, t, kl="k"),
+                 lambda: m.policy_loss(t, t, t, mean="rows"),
+                 lambda: m.preference_loss(t, t, q, 0.1, form="f")):
+        with pytest.raises(ValueError):
+            call()
