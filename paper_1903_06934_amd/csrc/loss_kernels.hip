@@ -1,12 +1,15 @@
 // The losses of fine-tuning and their gradients (include/mistep.h): the clipped
 // policy loss of sampled tokens, and the loss of pairs of sequences.
 //
-// Tokens are taken by chunks, whatever the sequences' lengths; of a chunk's
-// sequences each has a team of threads.  A sequence that reaches over several
-// chunks leaves its piece of each in the workspace: `tail` of the chunk it begins
-// in, `head` of those that it continues in, and a later launch adds the pieces in
-// the order of the chunks, so that no result depends on which workgroup ran first.
-// Calls of few tokens run as one workgroup, in one launch.
+// Tokens are taken by chunks, whatever the sequences' lengths, four tokens side by
+// side a thread.  Where sequences begin in a chunk is marked in LDS by a thread a
+// sequence; a scan over the chunk then tells each token where its sequence begins
+// (what belongs to the sequence lies there), or sums the sequences' tokens.  A
+// sequence that reaches over several chunks leaves its piece of each in the
+// workspace: `tail` of the chunk it begins in, `head` of those that it continues in,
+// and the next launch adds the pieces in the order of the chunks, so that no result
+// depends on which workgroup ran first.  Calls of few tokens run as one workgroup,
+// in one launch.
 #include <algorithm>
 
 #include "internal.h"
@@ -17,536 +20,851 @@ namespace miconv {
 
 namespace {
 
-constexpr int kBlock = 256, kChunk = 2048;         // of the calls of many tokens
-constexpr int kOneBlock = 1024, kOneChunk = 8192;  // of those of few
-constexpr int kMaxGroups = 2048;                   // workgroups of a launch, and partial sums
-constexpr int kJoinGroups = 1024;                  // of a launch over the sequences
+constexpr int kEach = 4;  // tokens side by side a thread
+// A workgroup of the calls of many tokens: threads, and packs of kEach tokens a thread,
+// each of the workgroup's packs behind the last one's; and of the calls of few.
+constexpr int kBlock = 256, kPacks = 2, kChunk = kBlock * kPacks * kEach;
+constexpr int kOneBlock = 1024, kOnePacks = 1, kOneChunk = kOneBlock * kOnePacks * kEach;
+constexpr int kMaxGroups = 1024;  // workgroups of a launch over the chunks, and partial sums
+constexpr int kJoinGroups = 1024;  // of a launch over the sequences
 
 typedef Pack<float>::V F4;
 
+// ------------------------------------------------------------------- reductions
+// Of a wave without LDS, as wave_reduce in rows.h; every lane gets the sum.
+template <int CTRL>
+__device__ __forceinline__ double dpp64(double v)
+{
+    const uint2 u = __builtin_bit_cast(uint2, v);
+    uint2 r;
+    r.x = __builtin_amdgcn_mov_dpp((int)u.x, CTRL, 0xf, 0xf, true);
+    r.y = __builtin_amdgcn_mov_dpp((int)u.y, CTRL, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, r);
+}
+
 __device__ __forceinline__ double wave_sum(double v)
 {
-    for (int o = 1; o < 64; o <<= 1)
-        v += __shfl_xor(v, o);
-    return v;
+    v += dpp64<0xb1>(v);
+    v += dpp64<0x4e>(v);
+    v += dpp64<0x141>(v);
+    v += dpp64<0x140>(v);
+    uint2 u = __builtin_bit_cast(uint2, v);
+    auto x = __builtin_amdgcn_permlane16_swap(u.x, u.x, false, false);
+    auto y = __builtin_amdgcn_permlane16_swap(u.y, u.y, false, false);
+    v = __builtin_bit_cast(double, uint2{x[0], y[0]}) + __builtin_bit_cast(double, uint2{x[1], y[1]});
+    u = __builtin_bit_cast(uint2, v);
+    x = __builtin_amdgcn_permlane32_swap(u.x, u.x, false, false);
+    y = __builtin_amdgcn_permlane32_swap(u.y, u.y, false, false);
+    return __builtin_bit_cast(double, uint2{x[0], y[0]}) + __builtin_bit_cast(double, uint2{x[1], y[1]});
 }
 
 __device__ __forceinline__ int wave_sum(int v)
 {
-    for (int o = 1; o < 64; o <<= 1)
-        v += __shfl_xor(v, o);
-    return v;
+    v += __builtin_amdgcn_mov_dpp(v, 0xb1, 0xf, 0xf, true);
+    v += __builtin_amdgcn_mov_dpp(v, 0x4e, 0xf, 0xf, true);
+    v += __builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true);
+    v += __builtin_amdgcn_mov_dpp(v, 0x140, 0xf, 0xf, true);
+    auto x = __builtin_amdgcn_permlane16_swap((unsigned)v, (unsigned)v, false, false);
+    v = (int)(x[0] + x[1]);
+    x = __builtin_amdgcn_permlane32_swap((unsigned)v, (unsigned)v, false, false);
+    return (int)(x[0] + x[1]);
 }
 
-// Sums over a workgroup; lds holds one value a wave.
-template <int BLOCK, class V>
-__device__ __forceinline__ V block_sum(V v, V *lds)
+// The sums of N values over a workgroup, in each thread; lds: N a wave.
+template <int BLOCK, int N, class V>
+__device__ __forceinline__ void block_sums(V (&v)[N], V (*lds)[N])
 {
-    v = wave_sum(v);
-    if ((threadIdx.x & 63) == 0)
-        lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
 #pragma unroll
-    for (int i = 1; i < BLOCK / 64; i++)
-        v += lds[i];
-    __syncthreads();
-    return v;
-}
-
-// How many of n numbers that do not fall are at most v; by a whole wave.
-__device__ __forceinline__ int count_up_to(const long long *p, int n, long long v)
-{
-    const int lane = threadIdx.x & 63;
-    int lo = 0, hi = n;  // those before lo are, those from hi on are not
-    while (lo < hi) {
-        const int step = (int)(((long long)hi - lo + 63) / 64);
-        const long long at = lo + (long long)lane * step;
-        const int k = __popcll(__ballot(at < hi && p[at] <= v));
-        if (!k)
-            break;
-        hi = (int)min((long long)hi, lo + (long long)k * step);
-        lo = (int)(lo + (long long)(k - 1) * step + 1);
+    for (int i = 0; i < N; i++) {
+        v[i] = wave_sum(v[i]);
+        if ((threadIdx.x & 63) == 0)
+            lds[threadIdx.x >> 6][i] = v[i];
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        v[i] = lds[0][i];
+        for (int w = 1; w < BLOCK / 64; w++)
+            v[i] += lds[w][i];
+    }
 }
 
+// The sums of N values over a workgroup, each to one thread's f(i, sum).
+template <int BLOCK, int N, class V, class F>
+__device__ __forceinline__ void block_totals(V (&v)[N], V (*lds)[N], F f)
+{
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        v[i] = wave_sum(v[i]);
+        if ((threadIdx.x & 63) == 0)
+            lds[threadIdx.x >> 6][i] = v[i];
+    }
+    __syncthreads();
+    if (threadIdx.x < N) {
+        V s = lds[0][threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < BLOCK / 64; w++)
+            s += lds[w][threadIdx.x];
+        f((int)threadIdx.x, s);
+    }
+}
+
+// The sum of n numbers (1 at least), by each wave; the loads of eight rounds are issued
+// together.
+template <class V>
+__device__ __forceinline__ V sum_of(const V *p, int n)
+{
+    V v = V(0);
+    for (int i = threadIdx.x & 63; i < n; i += 8 * 64) {
+        V part[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+            part[k] = p[min(i + 64 * k, n - 1)];
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+            v += i + 64 * k < n ? part[k] : V(0);
+    }
+    return wave_sum(v);
+}
+
+// -------------------------------------------------------------------- sequences
 struct Starts {
     const long long *p;
     int tokens;
+
+    __device__ __forceinline__ int cut(uint32_t low, int high) const
+    {
+        return high < 0 ? 0 : high ? tokens : (int)min(low, (uint32_t)tokens);
+    }
     __device__ __forceinline__ int operator()(long long i) const
     {
-        return (int)min(max(p[i], 0LL), (long long)tokens);
+        const long long v = p[i];
+        return cut((uint32_t)v, (int)(v >> 32));
+    }
+    // Where sequence s begins and ends.
+    __device__ __forceinline__ void of(long long s, int &s0, int &s1) const
+    {
+        typedef int V __attribute__((ext_vector_type(4)));
+        typedef V At __attribute__((aligned(8)));
+        const V v = *(const At *)(p + s);
+        s0 = cut((uint32_t)v[0], v[1]);
+        s1 = cut((uint32_t)v[2], v[3]);
     }
 };
 
-// The sequences first <= s < last that have tokens in the chunk [begin, end), and
-// the threads of each one's team: about as many as it has tokens there.
-struct Here {
-    int first, last, width;
+// Of the n numbers at p, which do not fall, those up to v are counted, 64 of them at a
+// time by the lanes of a wave: those before lo are, those from hi on are not.
+struct Search {
+    const long long *p;
+    long long v;
+    int lo, hi;
+
+    __device__ __forceinline__ bool open() const { return lo < hi; }
+    __device__ __forceinline__ int step() const { return (int)(((long long)hi - lo + 63) / 64); }
+    __device__ __forceinline__ bool probe() const
+    {
+        const long long at = lo + (long long)(threadIdx.x & 63) * step();
+        return at < hi && p[at] <= v;
+    }
+    __device__ __forceinline__ void narrow(int k)
+    {
+        const int s = step();
+        if (!k) {
+            hi = lo;
+            return;
+        }
+        hi = (int)min((long long)hi, lo + (long long)k * s);
+        lo = (int)(lo + (long long)(k - 1) * s + 1);
+    }
 };
 
-__device__ __forceinline__ Here sequences_here(const long long *starts, int seqs, int begin, int end)
+// Calls f(s, s0, s1), each in one thread of the workgroup, for the sequences s (the
+// tokens s0 <= t < s1) that have tokens in the chunk begin <= t < end.  Up to kDirect
+// sequences each thread looks at its share of all (one latency); more of them are
+// searched for the chunk's first and last.
+constexpr int kLook = 2, kDirect = 8 * kBlock;
+
+template <int BLOCK, class F>
+__device__ __forceinline__ void for_sequences(const Starts &starts, int seqs, int begin, int end,
+                                              F f)
 {
-    Here h;
-    h.first = count_up_to(starts + 1, seqs, begin);
-    h.last = count_up_to(starts, seqs, (long long)end - 1);
-    h.width = 64;
-    while (h.width > 1 && (long long)h.width / 2 * (h.last - h.first) >= end - begin)
-        h.width /= 2;
-    return h;
+    int first = 0, last = seqs;
+    if (seqs > kDirect) {
+        Search a{starts.p + 1, begin, 0, seqs}, b{starts.p, (long long)end - 1, 0, seqs};
+        while (a.open() || b.open()) {
+            const bool pa = a.open() && a.probe(), pb = b.open() && b.probe();
+            const int ka = __popcll(__ballot(pa)), kb = __popcll(__ballot(pb));
+            if (a.open())
+                a.narrow(ka);
+            if (b.open())
+                b.narrow(kb);
+        }
+        first = a.lo;
+        last = b.lo;
+    }
+    for (long long at = first + (long long)threadIdx.x; at < last; at += kLook * BLOCK) {
+        int s0[kLook], s1[kLook];
+#pragma unroll
+        for (int i = 0; i < kLook; i++)
+            starts.of(min(at + i * BLOCK, (long long)last - 1), s0[i], s1[i]);
+#pragma unroll
+        for (int i = 0; i < kLook; i++)
+            if (at + i * BLOCK < last && s0[i] < s1[i] && s0[i] < end && s1[i] > begin)
+                f(at + i * BLOCK, s0[i], s1[i]);
+    }
 }
 
-// Bytes of the mask for four tokens, of which left (>= 1) are there, one bit each.
-__device__ __forceinline__ unsigned load_mask(const unsigned char *mask, int at, int left)
-{
-    if (!mask)
-        return left >= 4 ? 15u : (1u << left) - 1;
-    unsigned bits = 0;
-    if (left >= 4) {
-        typedef uint32_t At __attribute__((aligned(1)));
-        const uint32_t v = *(const At *)(mask + at);
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-            bits |= (unsigned)((v >> 8 * j & 255) != 0) << j;
-    } else {
-        for (int j = 0; j < left; j++)
-            bits |= (unsigned)(mask[at + j] != 0) << j;
+// What chunks left of a sequence.
+template <class V>
+struct Pieces {
+    V *seq;          // [seqs] of those within a chunk
+    V *head, *tail;  // [chunks]
+
+    __device__ __forceinline__ V *place(long long s, int s0, int s1, int chunk, int begin, int end)
+    {
+        return s0 < begin ? head + chunk : s1 > end ? tail + chunk : seq + s;
     }
+};
+
+// The sum of a sequence's pieces (of the tokens s0 <= t < s1), for the sequence s of
+// each lane that has one, else 0.  Those of up to kFew chunks are added by their lane, of
+// loads that are all issued at once, the others by the wave, one by one.
+constexpr int kFew = 4;
+
+template <class V>
+__device__ __forceinline__ V join(bool has, const Pieces<V> &p, long long s, int s0, int s1)
+{
+    has = has && s0 < s1;
+    const int from = has ? s0 / kChunk : 0, to = has ? (s1 - 1) / kChunk : 0, n = to - from;
+    V part[kFew];
+    part[0] = *(n ? p.tail + from : p.seq + (has ? s : 0));
+#pragma unroll
+    for (int i = 1; i < kFew; i++)
+        part[i] = p.head[min(from + i, to)];
+    V v{};
+    if (has && n < kFew) {
+        v = part[0];
+#pragma unroll
+        for (int i = 1; i < kFew; i++)
+            if (i <= n)
+                v += part[i];
+    }
+    unsigned long long many = __ballot(has && n >= kFew);
+    while (many) {
+        const int lane = __builtin_ctzll(many);
+        many &= many - 1;
+        const int f = __shfl(from, lane), t = __shfl(to, lane);
+        V sum{};
+#pragma unroll 4
+        for (int k = f + (int)(threadIdx.x & 63); k <= t; k += 64)
+            sum += k == f ? p.tail[k] : p.head[k];
+        sum = wave_sum(sum);
+        if ((int)(threadIdx.x & 63) == lane)
+            v = sum;
+    }
+    return v;
+}
+
+// ----------------------------------------------------------------------- tokens
+// A pack of a thread's tokens of the chunk: t0 + j for j < left.
+struct Mine {
+    int t0, left;
+    unsigned mask;  // a bit each: there, and not masked
+};
+
+// rank: of the pack in the chunk.
+__device__ __forceinline__ Mine my_tokens(const unsigned char *mask, int begin, int end, int rank)
+{
+    Mine m;
+    // Past the end the first token may be beyond 32 bits: it is not used.
+    m.left = end - begin - rank * kEach;
+    m.t0 = m.left > 0 ? begin + rank * kEach : begin;
+    m.mask = m.left >= kEach ? (1u << kEach) - 1 : m.left > 0 ? (1u << m.left) - 1 : 0;
+    if (mask && m.left > 0) {
+        unsigned bits = 0;
+        if (m.left >= kEach) {
+            typedef uint32_t At __attribute__((aligned(1)));
+            const uint32_t v = *(const At *)(mask + m.t0);
+#pragma unroll
+            for (int j = 0; j < kEach; j++)
+                bits |= (unsigned)((v >> 8 * j & 255) != 0) << j;
+        } else {
+            for (int j = 0; j < m.left; j++)
+                bits |= (unsigned)(mask[m.t0 + j] != 0) << j;
+        }
+        m.mask = bits;
+    }
+    return m;
+}
+
+// Those of the thread's tokens that lie in from <= t < to.
+__device__ __forceinline__ unsigned inside(const Mine &m, int from, int to)
+{
+    unsigned bits = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; j++)
+        bits |= (unsigned)(m.left > j && m.t0 + j >= from && m.t0 + j < to) << j;
     return bits;
 }
 
-__device__ __forceinline__ F4 load_four(const float *p, int at, int left)
+__device__ __forceinline__ void load_floats(const float *p, const Mine &m, float (&v)[kEach])
 {
-    return load_pack<float>(p + at, left, 0.f);
+    F4 f = F4{};
+    if (m.left > 0)
+        f = load_pack<float>(p + m.t0, m.left, 0.f);
+#pragma unroll
+    for (int j = 0; j < kEach; j++)
+        v[j] = f[j];
 }
 
-// A workgroup's chunks of all of them.
-__device__ __forceinline__ int first_chunk(int chunks, unsigned group)
+__device__ __forceinline__ void store_floats(float *p, const Mine &m, const float (&v)[kEach])
 {
-    return (int)((long long)chunks * group / gridDim.x);
+    if (m.left > 0)
+        store_pack<float>(p + m.t0, m.left, F4{v[0], v[1], v[2], v[3]});
 }
 
-// ------------------------------------------------------------- counts of tokens
-// What the counts of a policy loss are written to and read from.
+static_assert(kEach == Pack<float>::N, "a pack a thread");
+
+// Of a workgroup's BLOCK * PACKS packs of tokens, thread t's are the packs t + h BLOCK;
+// 64 packs side by side are a wave's.
+template <int BLOCK>
+__device__ __forceinline__ int rank_of(int h)
+{
+    return h * BLOCK + (int)threadIdx.x;
+}
+
+// How many tokens of the chunk before each count: by pack, and a bit each.
+template <int BLOCK, int PACKS>
+struct CountTable {
+    static constexpr int ALL = BLOCK * PACKS;
+    int before[ALL];
+    unsigned char bits[ALL];
+    int waves[ALL / 64];
+
+    // To be called by all threads; the caller's barrier follows.
+    __device__ __forceinline__ void scan(int h, unsigned counted)
+    {
+        const int rank = rank_of<BLOCK>(h);
+        int v = 0, n = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; j++) {
+            const unsigned long long b = __ballot(counted >> j & 1);
+            v += __builtin_amdgcn_mbcnt_hi((unsigned)(b >> 32),
+                                           __builtin_amdgcn_mbcnt_lo((unsigned)b, 0));
+            n += __popcll(b);
+        }
+        before[rank] = v;
+        bits[rank] = (unsigned char)counted;
+        if ((threadIdx.x & 63) == 0)
+            waves[rank >> 6] = n;
+    }
+    // Of the chunk's tokens before its at-th (at most all).
+    __device__ __forceinline__ int up_to(int at) const
+    {
+        const int i = at / kEach;
+        int v = 0;
+        for (int w = 0; w < i / 64; w++)
+            v += waves[w];
+        return i < ALL ? v + before[i] + __popc(bits[i] & ((1u << at % kEach) - 1)) : v;
+    }
+};
+
+// Marks in LDS where sequences begin: a byte each of the chunk's tokens.
+template <int BLOCK, int PACKS>
+struct Marks {
+    static constexpr int ALL = BLOCK * PACKS;
+    alignas(4) unsigned char at[ALL * kEach];
+    int waves[ALL / 64];
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int h = 0; h < PACKS; h++)
+            *(uint32_t *)(at + rank_of<BLOCK>(h) * kEach) = 0;
+    }
+    __device__ __forceinline__ unsigned mine(int h) const
+    {
+        const uint32_t v = *(const uint32_t *)(at + rank_of<BLOCK>(h) * kEach);
+        return (v | v >> 7 | v >> 14 | v >> 21) & 15;  // of bytes that are 0 or 1
+    }
+    // Where the sequence of each of the thread's tokens begins in the chunk, -1 where
+    // none has begun.  One barrier.
+    __device__ __forceinline__ void places(int (&place)[PACKS][kEach])
+    {
+        const int lane = threadIdx.x & 63;
+        unsigned marks[PACKS];
+        int last[PACKS];
+        bool within[PACKS];
+#pragma unroll
+        for (int h = 0; h < PACKS; h++) {
+            const int rank = rank_of<BLOCK>(h);
+            marks[h] = mine(h);
+            const int own = rank * kEach + 31 - __builtin_clz(marks[h] | 1);
+            const unsigned long long any = __ballot(marks[h] != 0);
+            const unsigned long long before = any & ((1ULL << lane) - 1);
+            within[h] = before != 0;
+            last[h] = __shfl(own, before ? 63 - __builtin_clzll(before) : 0);
+            if (lane == (any ? 63 - __builtin_clzll(any) : 0))
+                waves[rank >> 6] = any ? own : -1;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < PACKS; h++) {
+            const int rank = rank_of<BLOCK>(h);
+            if (!within[h]) {
+                last[h] = -1;
+                for (int w = (rank >> 6) - 1; w >= 0 && last[h] < 0; w--)
+                    last[h] = waves[w];
+            }
+#pragma unroll
+            for (int j = 0; j < kEach; j++) {
+                last[h] = marks[h] >> j & 1 ? rank * kEach + j : last[h];
+                place[h][j] = last[h];
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ int end_of_chunk(int begin, int tokens)
+{
+    return begin + min(kChunk, tokens - begin);
+}
+
+// ------------------------------------------------------------------ policy loss
+// What a call of many tokens keeps between its launches.
 struct Counts {
-    int *seq;   // [seqs] tokens that count, of sequences within a chunk; later of all
-    int *head, *tail;  // [chunks]
-    int *group;        // [kMaxGroups] of each workgroup's chunks
-    int *some;         // [kJoinGroups] sequences that have any
-    double *part;      // [kMaxGroups][6]
+    double *part;     // [5][groups] each workgroup's sums
+    Pieces<int> n;    // tokens that count; seq later of all sequences
+    int *group;       // [kMaxGroups] tokens that count of each workgroup's chunks
+    int *some;        // [kJoinGroups] sequences that have any
 };
 
 __global__ __launch_bounds__(kBlock) void policy_count(PolicyArgs a, Counts c, int chunks)
 {
-    __shared__ unsigned char bits[kChunk];
-    __shared__ int red[kBlock / 64];
-    const bool by_seq = a.mean == 1;
+    __shared__ CountTable<kBlock, kPacks> table;
+    __shared__ int red[kBlock / 64][1];
     const Starts starts{a.starts, a.tokens};
-    int all = 0;
-    for (int k = first_chunk(chunks, blockIdx.x); k < first_chunk(chunks, blockIdx.x + 1); k++) {
-        const int begin = k * kChunk, end = begin + min(kChunk, a.tokens - begin);
-        const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
-        for (int t = threadIdx.x * 4; t < end - begin; t += kBlock * 4) {
-            const unsigned m = load_mask(a.mask, begin + t, end - begin - t);
+    int all[1] = {0};
+    for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
+        const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
+        Mine m[kPacks];
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const int at = begin + t + j;
-                const bool in = m >> j & 1;
-                all += in && at >= from && at < to;
-                if (by_seq)
-                    bits[t + j] = in;
-            }
+        for (int h = 0; h < kPacks; h++)
+            m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
+        if (a.mean == 1) {
+#pragma unroll
+            for (int h = 0; h < kPacks; h++)
+                table.scan(h, m[h].mask);
+            __syncthreads();
+            for_sequences<kBlock>(starts, a.seqs, begin, end, [&](long long s, int s0, int s1) {
+                *c.n.place(s, s0, s1, k, begin, end) =
+                    table.up_to(min(s1, end) - begin) - table.up_to(max(s0, begin) - begin);
+            });
+            __syncthreads();
+        } else {
+            const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
+#pragma unroll
+            for (int h = 0; h < kPacks; h++)
+                all[0] += __popc(m[h].mask & inside(m[h], from, to));
         }
-        if (!by_seq)
-            continue;
-        __syncthreads();
-        const Here h = sequences_here(a.starts, a.seqs, begin, end);
-        const int lane = threadIdx.x & (h.width - 1);
-        for (long long s = h.first + threadIdx.x / h.width; s < h.last; s += kBlock / h.width) {
-            const int s0 = starts(s), s1 = starts(s + 1);
-            int n = 0;
-            for (int t = max(s0, begin) + lane; t < min(s1, end); t += h.width)
-                n += bits[t - begin];
-            for (int o = 1; o < h.width; o <<= 1)
-                n += __shfl_xor(n, o);
-            if (lane == 0)
-                *(s0 < begin ? c.head + k : s1 > end ? c.tail + k : c.seq + s) = n;
-        }
-        __syncthreads();
     }
-    all = block_sum<kBlock>(all, red);
-    if (threadIdx.x == 0)
-        c.group[blockIdx.x] = all;
+    if (a.mean == 1)
+        return;
+    block_totals<kBlock>(all, red, [&](int, int v) { c.group[blockIdx.x] = v; });
 }
 
-// The sum of a sequence's pieces (of the tokens begin <= t < end) that chunks left;
-// by a whole wave.
-template <class V>
-__device__ __forceinline__ V join_pieces(const V *seq, const V *head, const V *tail, long long s,
-                                         int begin, int end)
-{
-    if (begin >= end)
-        return V(0);
-    const int from = begin / kChunk, to = (end - 1) / kChunk;
-    if (from == to)
-        return seq[s];
-    V v = V(0);
-    for (int k = from + (threadIdx.x & 63); k <= to; k += 64)
-        v += k == from ? tail[k] : head[k];
-    return wave_sum(v);
-}
+// Each sequence's tokens that count, and how many sequences have any.
+constexpr int kJoinBlock = 256;
 
-// A wave a sequence: its tokens that count, and how many sequences have any.
-__global__ __launch_bounds__(kBlock) void policy_join(PolicyArgs a, Counts c)
+__global__ __launch_bounds__(kJoinBlock) void policy_join(PolicyArgs a, Counts c)
 {
-    __shared__ int red[kBlock / 64];
+    __shared__ int red[kJoinBlock / 64][1];
     const Starts starts{a.starts, a.tokens};
-    int some = 0;
-    if (a.mask) {
-        for (long long s = blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6); s < a.seqs;
-             s += gridDim.x * (kBlock / 64)) {
-            const int n = join_pieces(c.seq, c.head, c.tail, s, starts(s), starts(s + 1));
-            if ((threadIdx.x & 63) == 0) {
-                c.seq[s] = n;
-                some += n > 0;
-            }
+    int some[1] = {0};
+    for (long long first = (long long)blockIdx.x * kJoinBlock; first < a.seqs;
+         first += (long long)gridDim.x * kJoinBlock) {
+        const long long s = first + threadIdx.x;
+        const bool has = s < a.seqs;
+        int s0 = 0, s1 = 0;
+        if (has)
+            starts.of(s, s0, s1);
+        int n = max(s1 - s0, 0);
+        if (a.mask) {
+            n = join(has, c.n, s, s0, s1);
+            if (has)
+                c.n.seq[s] = n;
         }
-    } else {
-        for (long long s = (long long)blockIdx.x * kBlock + threadIdx.x; s < a.seqs;
-             s += (long long)gridDim.x * kBlock)
-            some += starts(s + 1) > starts(s);
+        some[0] += n > 0;
     }
-    some = block_sum<kBlock>(some, red);
-    if (threadIdx.x == 0)
-        c.some[blockIdx.x] = some;
+    block_totals<kJoinBlock>(some, red, [&](int, int v) { c.some[blockIdx.x] = v; });
 }
 
-// ------------------------------------------------------------------ policy loss
+// exp(x): 2^h (1 + l ln 2) with h + l = x log2(e), h its rounding to 32 bits and l what
+// that leaves, so that large |x| lose nothing.  Results below 2^-126 are 0.
+__device__ __forceinline__ float exp_of(float x)
+{
+    constexpr float log2e = 0x1.715476p+0f, rest = 0x1.4ae0bep-26f;  // log2(e) = their sum
+    const float h = x * log2e;
+    float l = fmaf(x, log2e, -h);
+    l = fmaf(x, rest, l);
+    const float e = __builtin_amdgcn_exp2f(h);
+    return fabsf(h) < 200.f ? fmaf(e, l * 0x1.62e43p-1f, e) : e;
+}
+
 // exp(x) - 1 - x, and exp(x) - 1; near 0 by the exponential's series, where the
 // difference would lose what matters.
 __device__ __forceinline__ float low_kl(float x, float *expm1)
 {
-    float v;
-    if (fabsf(x) < 1.f) {
-        float p = 1.f / 479001600.f;  // 1 / 12!
-        p = fmaf(p, x, 1.f / 39916800.f);
-        p = fmaf(p, x, 1.f / 3628800.f);
-        p = fmaf(p, x, 1.f / 362880.f);
-        p = fmaf(p, x, 1.f / 40320.f);
-        p = fmaf(p, x, 1.f / 5040.f);
-        p = fmaf(p, x, 1.f / 720.f);
-        p = fmaf(p, x, 1.f / 120.f);
-        p = fmaf(p, x, 1.f / 24.f);
-        p = fmaf(p, x, 1.f / 6.f);
-        p = fmaf(p, x, 0.5f);
-        v = x * x * p;
-        *expm1 = x + v;
-    } else {
-        *expm1 = expf(x) - 1.f;
+    float p = 1.f / 479001600.f;  // 1 / 12!
+    p = fmaf(p, x, 1.f / 39916800.f);
+    p = fmaf(p, x, 1.f / 3628800.f);
+    p = fmaf(p, x, 1.f / 362880.f);
+    p = fmaf(p, x, 1.f / 40320.f);
+    p = fmaf(p, x, 1.f / 5040.f);
+    p = fmaf(p, x, 1.f / 720.f);
+    p = fmaf(p, x, 1.f / 120.f);
+    p = fmaf(p, x, 1.f / 24.f);
+    p = fmaf(p, x, 1.f / 6.f);
+    p = fmaf(p, x, 0.5f);
+    float v = x * x * p;
+    *expm1 = x + v;
+    if (!(fabsf(x) < 1.f)) {
+        *expm1 = exp_of(x) - 1.f;
         v = *expm1 - x;
     }
     return v;
 }
 
+// The borders of the clip in 32 bits, how near to them (2^-22 of each) 32 bits do not
+// tell on which side a log ratio is, and the ratio at them.
+struct Borders {
+    float low, high, dual, near_low, near_high, near_dual, at_low, at_high, at_dual;
+
+    __device__ __forceinline__ explicit Borders(const PolicyArgs &a)
+        : low((float)a.log_low), high((float)a.log_high), dual((float)a.log_dual),
+          near_low(near(low)), near_high(near(high)), near_dual(near(dual)),
+          at_low(a.low), at_high(a.high), at_dual(a.dual)
+    {
+    }
+    static __device__ __forceinline__ float near(float v)
+    {
+        return __builtin_isfinite(v) ? fabsf(v) * 0x1p-22f : -1.f;  // none is near an infinity
+    }
+};
+
 struct Token {
-    float loss, surrogate, kl, ratio, slope;
+    float surrogate, kl, ratio, slope;
     bool clipped;
 };
 
-__device__ __forceinline__ Token token_loss(const PolicyArgs &a, float lp, float lo, float lr,
-                                            float h, float adv)
+// The reference's part: none, the low form, or the others.
+enum class Ref { none, low, other };
+
+template <Ref REF>
+__device__ __forceinline__ Token token_loss(const PolicyArgs &a, const Borders &b, float lp,
+                                            float lo, float lr, float adv)
 {
     Token k;
-    const double d = (double)lp - (double)lo;  // in 64 bits: whether the token is clipped
-    k.ratio = expf((float)d);
-    float bound = k.ratio;
-    k.clipped = false;
-    if (adv > 0.f && d > a.log_high) {
-        k.clipped = true;
-        bound = a.high;
-    } else if (adv < 0.f && d < a.log_low) {
-        k.clipped = true;
-        bound = a.low;
-    } else if (adv < 0.f && d > a.log_dual) {
-        k.clipped = true;
-        bound = a.dual;
+    const float d = lp - lo;  // off by 2^-24 of it
+    k.ratio = exp_of(d);
+    bool high = d > b.high, low = d < b.low, dual = d > b.dual;
+    if (fabsf(d - b.high) <= b.near_high || fabsf(d - b.low) <= b.near_low ||
+        fabsf(d - b.dual) <= b.near_dual) {
+        const double e = (double)lp - (double)lo;
+        high = e > a.log_high;
+        low = e < a.log_low;
+        dual = e > a.log_dual;
     }
-    k.surrogate = -adv * bound;
+    const bool gain = adv > 0.f, loss = adv < 0.f;
+    // A choice of values in registers; of members it would be one of addresses, with a
+    // load a token.
+    const float at_low = b.at_low, at_high = b.at_high, at_dual = b.at_dual;
+    const float bound = gain ? at_high : dual ? at_dual : at_low;
+    k.clipped = (gain && high) || (loss && (low || dual));
+    k.surrogate = -adv * (k.clipped ? bound : k.ratio);
     k.slope = k.clipped ? 0.f : k.surrogate;
-    k.loss = k.surrogate;
     k.kl = 0.f;
-    if (a.ref_logp) {
+    if constexpr (REF != Ref::none) {
         const float x = lr - lp;
         float slope;
-        if (a.kl == 0) {
-            k.kl = -x;
-            slope = 1.f;
-        } else if (a.kl == 1) {
-            k.kl = 0.5f * x * x;
-            slope = -x;
-        } else {
+        if (REF == Ref::low) {
             k.kl = low_kl(x, &slope);
             slope = -slope;
+        } else if (a.kl == 0) {
+            k.kl = -x;
+            slope = 1.f;
+        } else {
+            k.kl = 0.5f * x * x;
+            slope = -x;
         }
-        if (a.kl_weight != 0.f) {
-            k.loss += a.kl_weight * k.kl;
-            k.slope += a.kl_weight * slope;
-        }
+        k.slope = a.kl_weight != 0.f ? fmaf(a.kl_weight, slope, k.slope) : k.slope;
     }
-    if (a.entropy && a.entropy_weight != 0.f)
-        k.loss -= a.entropy_weight * h;
     return k;
 }
 
-// The chunk's tokens a thread holds: two packs of four.
-constexpr int kPacks = 2;
-
 struct Tokens {
-    F4 lp[kPacks], lo[kPacks], lr[kPacks], h[kPacks], adv[kPacks];
-    unsigned mask[kPacks];  // of four: there, and not masked
+    float lp[kEach], lo[kEach], lr[kEach], h[kEach], adv[kEach];
 };
 
-template <int BLOCK>
-__device__ __forceinline__ void load_tokens(const PolicyArgs &a, int begin, int end, Tokens &k)
+template <Ref REF>
+__device__ __forceinline__ void load_tokens(const PolicyArgs &a, const Mine &m, Tokens &k)
 {
 #pragma unroll
-    for (int i = 0; i < kPacks; i++) {
-        const int at = begin + ((int)threadIdx.x + i * BLOCK) * 4, left = end - at;
-        k.mask[i] = 0;
-        k.lp[i] = k.lo[i] = k.lr[i] = k.h[i] = k.adv[i] = F4{};
-        if (left <= 0)
-            continue;
-        k.mask[i] = load_mask(a.mask, at, left);
-        k.lp[i] = load_four(a.logp, at, left);
-        k.lo[i] = load_four(a.old_logp, at, left);
-        if (a.ref_logp)
-            k.lr[i] = load_four(a.ref_logp, at, left);
-        if (a.entropy)
-            k.h[i] = load_four(a.entropy, at, left);
-        if (!a.by_sequence)
-            k.adv[i] = load_four(a.advantages, at, left);
-    }
+    for (int j = 0; j < kEach; j++)
+        k.h[j] = 0.f;
+    load_floats(a.logp, m, k.lp);
+    load_floats(a.old_logp, m, k.lo);
+    if (REF != Ref::none)
+        load_floats(a.ref_logp, m, k.lr);
+    if (a.entropy)
+        load_floats(a.entropy, m, k.h);
+    if (!a.by_sequence)
+        load_floats(a.advantages, m, k.adv);
 }
 
-// The tokens' losses (times their weights within their sequences) to sum, their
-// gradients to memory.  weight, adv: of each token of the chunk in LDS, or null:
-// the tokens from <= t < to have weight 1.  u: what all weights are multiplied by.
-template <int BLOCK>
-__device__ __forceinline__ void chunk_losses(const PolicyArgs &a, const Tokens &k, int begin,
-                                             int end, const float *weight, const float *adv,
-                                             int from, int to, double u, double (&sum)[6])
+// The tokens' surrogates, divergences, entropies, ratios and clips (times their
+// weights within their sequences, if WEIGHTS) to sum, their gradients to memory.
+// counted: the tokens that count; w: their weights; u: what all weights are multiplied by.
+template <bool WEIGHTS, Ref REF>
+__device__ __forceinline__ void token_losses(const PolicyArgs &a, const Mine &m, const Tokens &k,
+                                             unsigned counted, const float (&w)[kEach], double u,
+                                             double (&sum)[5])
 {
     const float factor = (float)(u * a.scale);
+    const Borders borders(a);
+    float g[kEach], gh[kEach], part[5] = {0, 0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < kPacks; i++) {
-        const int at = begin + ((int)threadIdx.x + i * BLOCK) * 4, left = end - at;
-        if (left <= 0)
-            continue;
-        F4 g = F4{}, gh = F4{};
+    for (int j = 0; j < kEach; j++) {
+        const bool in = counted >> j & 1;
+        const Token r = token_loss<REF>(a, borders, k.lp[j], k.lo[j],
+                                        REF == Ref::none ? 0.f : k.lr[j], k.adv[j]);
+        const float d = WEIGHTS ? w[j] : 1.f, f = WEIGHTS ? d * factor : factor;
+        const float v[5] = {r.surrogate, r.kl, k.h[j], r.ratio,
+                            r.clipped ? 1.f : 0.f};
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int t = at + j;
-            if (!(k.mask[i] >> j & 1))
-                continue;
-            const float w = weight ? weight[t - begin] : t >= from && t < to ? 1.f : 0.f;
-            if (w == 0.f)
-                continue;
-            const Token r = token_loss(a, k.lp[i][j], k.lo[i][j], k.lr[i][j], k.h[i][j],
-                                       a.by_sequence ? adv[t - begin] : k.adv[i][j]);
-            sum[0] += (double)w * r.loss;
-            sum[1] += (double)w * r.surrogate;
-            sum[2] += (double)w * r.kl;
-            if (a.entropy)
-                sum[3] += (double)w * k.h[i][j];
-            sum[4] += (double)w * r.ratio;
-            sum[5] += r.clipped ? w : 0.f;
-            g[j] = r.slope * (w * factor);
-            gh[j] = -a.entropy_weight * (w * factor);
-        }
-        if (a.dlogp)
-            store_pack<float>(a.dlogp + at, left, g);
-        if (a.dentropy)
-            store_pack<float>(a.dentropy + at, left, gh);
+        for (int i = 0; i < 5; i++)
+            part[i] += in ? (WEIGHTS ? v[i] * d : v[i]) : 0.f;
+        g[j] = in ? r.slope * f : 0.f;
+        gh[j] = in ? -a.entropy_weight * f : 0.f;
+        __builtin_amdgcn_sched_barrier(0);  // a token at a time: fewer registers, more waves
     }
+#pragma unroll
+    for (int i = 0; i < 5; i++)
+        sum[i] += (double)part[i];
+    if (a.dlogp)
+        store_floats(a.dlogp, m, g);
+    if (a.dentropy)
+        store_floats(a.dentropy, m, gh);
 }
 
-// Sequence s's weight (1 / its tokens that count, or 1) and advantage to its tokens
-// of the chunk; `width` threads.
-__device__ __forceinline__ void fill_tokens(const PolicyArgs &a, long long s, int n, int first,
-                                            int last, int begin, int lane, int width,
-                                            float *weight, float *adv)
+// The results from the sums over all tokens (times their weights): the loss is
+// linear in them.
+__device__ __forceinline__ float policy_result(const PolicyArgs &a, const double *sum, int i)
 {
-    const float w = a.mean == 1 ? (n > 0 ? 1.f / (float)n : 0.f) : 1.f;
-    const float v = a.by_sequence ? a.advantages[s] : 0.f;
-    for (int t = first + lane; t < last; t += width) {
-        weight[t - begin] = w;
-        adv[t - begin] = v;
-    }
+    if (i)
+        return (float)sum[i - 1];
+    double v = sum[0];
+    if (a.ref_logp && a.kl_weight != 0.f)
+        v += (double)a.kl_weight * sum[1];
+    if (a.entropy && a.entropy_weight != 0.f)
+        v -= (double)a.entropy_weight * sum[2];
+    return (float)v;
+}
+
+// What a sequence gives its tokens.
+struct OfSequence {
+    float weight, adv;
+};
+
+__device__ __forceinline__ OfSequence of_sequence(const PolicyArgs &a, long long s, int n)
+{
+    return OfSequence{a.mean == 1 ? 1.f / (float)max(n, 1) : 1.f,
+                      a.by_sequence ? a.advantages[s] : 0.f};
+}
+
+// The tokens' weights and advantages from what lies where their sequences begin.
+template <int BLOCK, int PACKS>
+__device__ __forceinline__ void from_sequences(const PolicyArgs &a, Marks<BLOCK, PACKS> &marks,
+                                               const OfSequence *seq, Tokens (&k)[PACKS],
+                                               float (&w)[PACKS][kEach])
+{
+    int place[PACKS][kEach];
+    marks.places(place);
+#pragma unroll
+    for (int h = 0; h < PACKS; h++)
+#pragma unroll
+        for (int j = 0; j < kEach; j++) {
+            const OfSequence q = seq[max(place[h][j], 0)];
+            w[h][j] = q.weight;
+            if (a.by_sequence)
+                k[h].adv[j] = q.adv;
+        }
 }
 
 // Few tokens: all of the call in one workgroup.  SEQS: the sequences matter.
-template <bool SEQS>
+template <bool SEQS, Ref REF>
 __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
 {
     constexpr int WAVES = kOneBlock / 64;
-    __shared__ float weight[SEQS ? kOneChunk : 1], adv[SEQS ? kOneChunk : 1];
-    __shared__ double red[6][WAVES];
-    __shared__ int counts[2][WAVES];
+    constexpr int PACKS = kOnePacks;
+    __shared__ Marks<SEQS ? kOneBlock : 64, PACKS> marks;
+    __shared__ CountTable<SEQS ? kOneBlock : 64, PACKS> table;
+    __shared__ OfSequence seq[SEQS ? kOneChunk : 1];
+    __shared__ double red[WAVES][5];
+    __shared__ int counts[WAVES][1];
     const Starts starts{a.starts, a.tokens};
-    Tokens k;
-    load_tokens<kOneBlock>(a, 0, a.tokens, k);
+    Mine m[PACKS];
+    Tokens k[PACKS];
+    float w[PACKS][kEach];
+#pragma unroll
+    for (int h = 0; h < PACKS; h++) {
+        m[h] = my_tokens(a.mask, 0, a.tokens, rank_of<kOneBlock>(h));
+        load_tokens<REF>(a, m[h], k[h]);
+#pragma unroll
+        for (int j = 0; j < kEach; j++)
+            w[h][j] = 1.f;
+    }
     const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
-    int all = 0;
+    int n[1] = {0};  // tokens that count, or sequences that have any
 #pragma unroll
-    for (int i = 0; i < kPacks; i++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int t = ((int)threadIdx.x + i * kOneBlock) * 4 + j;
-            const bool in = k.mask[i] >> j & 1;
-            all += in && t >= from && t < to;
-            if (SEQS && t < a.tokens) {
-                weight[t] = 0.f;
-                adv[t] = in ? 1.f : 0.f;  // until the advantages are written
-            }
-        }
+    for (int h = 0; h < PACKS; h++)
+        n[0] += __popc(m[h].mask & inside(m[h], from, to));
     double u = 1.0 / a.count;
-    if (a.mean == 0) {
-        all = block_sum<kOneBlock>(all, counts[0]);
-        u = 1.0 / max(all, 1);
-    }
-    if (SEQS) {
-        int width = 64, some = 0;
-        while (width > 1 && (long long)width / 2 * a.seqs >= a.tokens)
-            width /= 2;
-        const int lane = threadIdx.x & (width - 1);
-        __syncthreads();
-        for (int s = threadIdx.x / width; s < a.seqs; s += kOneBlock / width) {
-            const int s0 = starts(s), s1 = starts(s + 1);
-            int n = 0;
-            if (a.mean == 1) {
-                for (int t = s0 + lane; t < s1; t += width)
-                    n += adv[t] != 0.f;
-                for (int o = 1; o < width; o <<= 1)
-                    n += __shfl_xor(n, o);
-                some += lane == 0 && n > 0;
-            }
-            fill_tokens(a, s, n, s0, s1, 0, lane, width, weight, adv);
-        }
-        if (a.mean == 1) {
-            some = block_sum<kOneBlock>(some, counts[1]);
-            u = 1.0 / max(some, 1);
-        }
-        __syncthreads();
-    }
-    double sum[6] = {0, 0, 0, 0, 0, 0};
-    chunk_losses<kOneBlock>(a, k, 0, a.tokens, SEQS ? weight : nullptr, adv, from, to, u, sum);
+    if constexpr (SEQS) {
+        marks.clear();
 #pragma unroll
-    for (int i = 0; i < 6; i++) {
-        sum[i] = wave_sum(sum[i]);
-        if ((threadIdx.x & 63) == 0)
-            red[i][threadIdx.x >> 6] = sum[i];
+        for (int h = 0; h < PACKS; h++)
+            table.scan(h, m[h].mask);
+        __syncthreads();
+        if (a.mean == 1)
+            n[0] = 0;
+        for_sequences<kOneBlock>(starts, a.seqs, 0, a.tokens, [&](long long s, int s0, int s1) {
+            const int c = table.up_to(s1) - table.up_to(s0);
+            if (a.mean == 1)
+                n[0] += c > 0;
+            marks.at[s0] = 1;
+            seq[s0] = of_sequence(a, s, c);
+        });
     }
-    __syncthreads();
-    if (threadIdx.x < 6) {
-        double v = 0;
-        for (int i = 0; i < WAVES; i++)
-            v += red[threadIdx.x][i];
-        a.stats[threadIdx.x] = (float)(v * u);
+    if (a.mean != 2) {
+        block_sums<kOneBlock>(n, counts);
+        u = 1.0 / max(n[0], 1);
     }
+    if constexpr (SEQS) {
+        __syncthreads();
+        from_sequences(a, marks, seq, k, w);
+    }
+    double sum[5] = {0, 0, 0, 0, 0};
+#pragma unroll
+    for (int h = 0; h < PACKS; h++)
+        token_losses<SEQS, REF>(a, m[h], k[h], m[h].mask & inside(m[h], from, to), w[h], u, sum);
+    block_sums<kOneBlock>(sum, red);
+#pragma unroll
+    for (int i = 0; i < 5; i++)
+        sum[i] *= u;
+    if (threadIdx.x == 0)
+#pragma unroll
+        for (int i = 0; i < 6; i++)
+            a.stats[i] = policy_result(a, sum, i);
 }
 
-// The sum of n (at most a few thousand) counts, by a whole workgroup.
-template <int BLOCK>
-__device__ __forceinline__ long long sum_counts(const int *p, int n, double *lds)
-{
-    double v = 0;  // whole numbers below 2^53
-    for (int i = threadIdx.x; i < n; i += BLOCK)
-        v += p[i];
-    return (long long)block_sum<BLOCK>(v, lds);
-}
-
-// What all weights are multiplied by.
-__device__ __forceinline__ double weight_of_all(const PolicyArgs &a, const Counts &c, int groups,
-                                                int joins, int from, int to, double *lds)
-{
-    if (a.mean == 2)
-        return 1.0 / a.count;
-    long long n;
-    if (a.mean == 1)
-        n = sum_counts<kBlock>(c.some, joins, lds);
-    else
-        n = a.mask ? sum_counts<kBlock>(c.group, groups, lds) : to - from;
-    return 1.0 / (double)max(n, 1LL);
-}
-
-template <bool SEQS>
+template <bool SEQS, Ref REF>
 __global__ __launch_bounds__(kBlock) void policy_main(PolicyArgs a, Counts c, int chunks, int joins)
 {
-    __shared__ float weight[SEQS ? kChunk : 1], adv[SEQS ? kChunk : 1];
-    __shared__ double red[kBlock / 64];
+    __shared__ Marks<SEQS ? kBlock : 64, kPacks> marks;
+    __shared__ OfSequence seq[SEQS ? kChunk : 1];
+    __shared__ double red[kBlock / 64][5], of_all;
     const Starts starts{a.starts, a.tokens};
-    const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
-    const double u = weight_of_all(a, c, gridDim.x, joins, from, to, red);
-    double sum[6] = {0, 0, 0, 0, 0, 0};
-    for (int k = first_chunk(chunks, blockIdx.x); k < first_chunk(chunks, blockIdx.x + 1); k++) {
-        const int begin = k * kChunk, end = begin + min(kChunk, a.tokens - begin);
-        Tokens tokens;
-        load_tokens<kBlock>(a, begin, end, tokens);
-        if (SEQS) {
-            const Here h = sequences_here(a.starts, a.seqs, begin, end);
-            for (int t = threadIdx.x; t < end - begin; t += kBlock)
-                weight[t] = 0.f;
-            __syncthreads();
-            const int lane = threadIdx.x & (h.width - 1);
-            for (long long s = h.first + threadIdx.x / h.width; s < h.last;
-                 s += kBlock / h.width) {
-                const int s0 = starts(s), s1 = starts(s + 1);
-                const int n = a.mean != 1 ? 0 : a.mask ? c.seq[s] : s1 - s0;
-                fill_tokens(a, s, n, max(s0, begin), min(s1, end), begin, lane, h.width, weight,
-                            adv);
-            }
-            __syncthreads();
+    double u = 0.0, sum[5] = {0, 0, 0, 0, 0};
+    int from = 0, to = 0;
+    for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
+        const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
+        Mine m[kPacks];
+        Tokens tokens[kPacks];
+        float w[kPacks][kEach];
+#pragma unroll
+        for (int h = 0; h < kPacks; h++) {
+            m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
+            load_tokens<REF>(a, m[h], tokens[h]);
+#pragma unroll
+            for (int j = 0; j < kEach; j++)
+                w[h][j] = 1.f;
         }
-        chunk_losses<kBlock>(a, tokens, begin, end, SEQS ? weight : nullptr, adv, from, to, u, sum);
+        if constexpr (SEQS) {
+            marks.clear();
+            __syncthreads();
+            for_sequences<kBlock>(starts, a.seqs, begin, end, [&](long long s, int s0, int s1) {
+                const int at = max(s0, begin) - begin;
+                marks.at[at] = 1;
+                seq[at] = of_sequence(a, s, a.mean != 1 ? 1 : a.mask ? c.n.seq[s] : s1 - s0);
+            });
+        }
+        const bool first = k == (int)blockIdx.x;
+        if (first) {
+            from = a.starts ? starts(0) : 0;
+            to = a.starts ? starts(a.seqs) : a.tokens;
+            if (threadIdx.x < 64) {  // what all weights are multiplied by
+                double n = a.count;
+                if (a.mean == 1)
+                    n = max(sum_of(c.some, joins), 1);
+                else if (a.mean == 0)
+                    n = max(a.mask ? sum_of(c.group, (int)gridDim.x) : to - from, 1);
+                of_all = 1.0 / n;
+            }
+        }
+        if (SEQS || first)
+            __syncthreads();
+        u = of_all;
+        if constexpr (SEQS)
+            from_sequences(a, marks, seq, tokens, w);
+#pragma unroll
+        for (int h = 0; h < kPacks; h++)
+            token_losses<SEQS, REF>(a, m[h], tokens[h], m[h].mask & inside(m[h], from, to), w[h], u,
+                                    sum);
         if (SEQS)
             __syncthreads();
     }
-#pragma unroll
-    for (int i = 0; i < 6; i++) {
-        const double v = block_sum<kBlock>(sum[i], red);
-        if (threadIdx.x == 0)
-            c.part[blockIdx.x * 6 + i] = v * u;
-    }
+    block_totals<kBlock>(sum, red, [&](int i, double v) {
+        c.part[(size_t)i * gridDim.x + blockIdx.x] = v * u;
+    });
 }
 
-// Wave i adds the workgroups' sums of the i-th result.
-template <int N>
-__device__ __forceinline__ void add_parts(const double *part, int groups, double u, float *stats)
+__global__ __launch_bounds__(5 * 64) void policy_stats(PolicyArgs a, const double *part, int groups)
 {
+    __shared__ double sum[5];
     const int i = threadIdx.x >> 6;
-    if (i >= N)
-        return;
-    double v = 0;
-    for (int g = threadIdx.x & 63; g < groups; g += 64)
-        v += part[g * N + i];
-    v = wave_sum(v);
+    const double v = sum_of(part + (size_t)i * groups, groups);
     if ((threadIdx.x & 63) == 0)
-        stats[i] = (float)(v * u);
-}
-
-__global__ __launch_bounds__(6 * 64) void policy_stats(const double *part, int groups, float *stats)
-{
-    add_parts<6>(part, groups, 1.0, stats);
+        sum[i] = v;
+    __syncthreads();
+    if (threadIdx.x < 6)
+        a.stats[threadIdx.x] = policy_result(a, sum, (int)threadIdx.x);
 }
 
 // -------------------------------------------------------------- preference loss
+// A sum of log ratios, and of how many tokens.
+struct Piece {
+    double sum;
+    long long n;
+    __device__ __forceinline__ Piece &operator+=(const Piece &o)
+    {
+        sum += o.sum;
+        n += o.n;
+        return *this;
+    }
+};
+
+__device__ __forceinline__ Piece wave_sum(const Piece &p)
+{
+    return Piece{wave_sum(p.sum), wave_sum((int)p.n)};
+}
+
+// What a call of many tokens keeps between its launches.
 struct Pairs {
-    double *seq, *head, *tail;    // sums of log ratios: [2 pairs], [chunks], [chunks]
-    int *count, *chead, *ctail;   // tokens that count, likewise
-    double *slope;                // [pairs] of the loss in x
-    double *part;                 // [kJoinGroups][5]
-    int *some;                    // [kJoinGroups] pairs that have a token
+    Pieces<Piece> sum;  // log ratios and tokens that count; seq later of all sequences
+    double *slope;      // [pairs] of the loss in x
+    double *part;       // [5][joins]
+    int *some;          // [kJoinGroups] pairs that have a token
 };
 
 struct Pair {
@@ -594,177 +912,236 @@ __device__ __forceinline__ float pair_gradient(const PreferenceArgs &a, double s
     return (float)(second ? -v : v);
 }
 
-// Four tokens' log ratios, 0 where they do not count.
-__device__ __forceinline__ F4 load_ratios(const PreferenceArgs &a, int at, int left, unsigned *mask)
+// The tokens' log ratios, 0 where they do not count.
+__device__ __forceinline__ void load_ratios(const PreferenceArgs &a, const Mine &m,
+                                            float (&v)[kEach])
 {
-    *mask = load_mask(a.mask, at, left);
-    const F4 lp = load_four(a.logp, at, left);
-    F4 lr = F4{};
+    float lr[kEach];
+    load_floats(a.logp, m, v);
     if (a.ref_logp)
-        lr = load_four(a.ref_logp, at, left);
-    F4 v;
+        load_floats(a.ref_logp, m, lr);
 #pragma unroll
-    for (int j = 0; j < 4; j++)
-        v[j] = *mask >> j & 1 ? lp[j] - lr[j] : 0.f;
-    return v;
+    for (int j = 0; j < kEach; j++) {
+        v[j] = a.ref_logp ? v[j] - lr[j] : v[j];
+        v[j] = m.mask >> j & 1 ? v[j] : 0.f;
+    }
 }
 
-// The chunk's ratios and masks to LDS.
-template <int BLOCK>
-__device__ __forceinline__ void stage_ratios(const PreferenceArgs &a, int begin, int end, float *v,
-                                             unsigned char *bits)
-{
+// The sums of the chunk's sequences, each at its last token, of the threads' values
+// and the marks where sequences begin.
+template <int BLOCK, int PACKS>
+struct Sums {
+    static constexpr int ALL = BLOCK * PACKS;
+    double at[ALL * kEach];
+    double tail[ALL / 64];             // since the wave's last mark
+    unsigned long long marked[ALL / 64];
+
+    // One barrier; the caller's follows.
+    __device__ __forceinline__ void scan(const Marks<BLOCK, PACKS> &marks,
+                                         const float (&v)[PACKS][kEach])
+    {
+        const int lane = threadIdx.x & 63;
+        double run[PACKS][kEach], before[PACKS];
+        unsigned mine[PACKS];
+        bool within[PACKS];
 #pragma unroll
-    for (int i = 0; i < kPacks; i++) {
-        const int t = ((int)threadIdx.x + i * BLOCK) * 4, left = end - begin - t;
-        if (left <= 0)
-            continue;
-        unsigned m;
-        const F4 r = load_ratios(a, begin + t, left, &m);
+        for (int h = 0; h < PACKS; h++) {
+            const int rank = rank_of<BLOCK>(h);
+            mine[h] = marks.mine(h);
+            double s = 0;
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            v[t + j] = r[j];
-            bits[t + j] = m >> j & 1;
+            for (int j = 0; j < kEach; j++) {
+                s = mine[h] >> j & 1 ? (double)v[h][j] : s + (double)v[h][j];
+                run[h][j] = s;
+            }
+            // A lane takes those before it up to the last that has a mark.
+            const unsigned long long any = __ballot(mine[h] != 0);
+            const unsigned long long here = any & (~0ULL >> (63 - lane));
+            const int last = here ? 63 - __builtin_clzll(here) : -1;
+            double t = s;
+            for (int o = 1; o < 64; o <<= 1) {
+                const double q = __shfl_up(t, o);
+                if (lane >= o && lane - o >= last && last != lane)
+                    t += q;
+            }
+            if (lane == 63) {
+                tail[rank >> 6] = t;
+                marked[rank >> 6] = any;
+            }
+            // What comes before the pack in its first token's sequence.
+            before[h] = __shfl_up(t, 1);
+            if (lane == 0)
+                before[h] = 0;
+            within[h] = any & ((1ULL << lane) - 1);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < PACKS; h++) {
+            const int rank = rank_of<BLOCK>(h);
+            if (!within[h])  // from the waves before, the nearest first
+                for (int w = (rank >> 6) - 1; w >= 0; w--) {
+                    before[h] += tail[w];
+                    if (marked[w])
+                        break;
+                }
+            const bool next = rank + 1 == ALL || marks.at[min(rank + 1, ALL - 1) * kEach];
+#pragma unroll
+            for (int j = 0; j < kEach; j++) {
+                const bool ends = j + 1 < kEach ? mine[h] >> (j + 1) & 1 : next;
+                if (ends)
+                    at[rank * kEach + j] =
+                        mine[h] & ((2u << j) - 1) ? run[h][j] : before[h] + run[h][j];
+            }
         }
     }
-}
+};
 
-// The sum of a sequence's ratios of the chunk, and of its tokens; `width` threads.
-__device__ __forceinline__ double team_sum(const float *v, const unsigned char *bits, int first,
-                                           int last, int lane, int width, int *n)
+// Marks where a sequence begins and ends in the chunk, so that its sum stops there
+// whatever follows.
+template <class M>
+__device__ __forceinline__ void mark_sequence(M &marks, int first, int end)
 {
-    double s = 0;
-    int c = 0;
-    for (int t = first + lane; t < last; t += width) {
-        s += v[t];
-        c += bits[t];
-    }
-    for (int o = 1; o < width; o <<= 1) {
-        s += __shfl_xor(s, o);
-        c += __shfl_xor(c, o);
-    }
-    *n = c;
-    return s;
+    marks.at[first] = 1;
+    if (end < M::ALL * kEach)
+        marks.at[end] = 1;
 }
 
 __global__ __launch_bounds__(kBlock) void preference_sums(PreferenceArgs a, Pairs p, int chunks)
 {
-    __shared__ float v[kChunk];
-    __shared__ unsigned char bits[kChunk];
+    __shared__ Marks<kBlock, kPacks> marks;
+    __shared__ CountTable<kBlock, kPacks> table;
+    __shared__ Sums<kBlock, kPacks> sums;
     const Starts starts{a.starts, a.tokens};
-    for (int k = first_chunk(chunks, blockIdx.x); k < first_chunk(chunks, blockIdx.x + 1); k++) {
-        const int begin = k * kChunk, end = begin + min(kChunk, a.tokens - begin);
-        stage_ratios<kBlock>(a, begin, end, v, bits);
-        const Here h = sequences_here(a.starts, 2 * a.pairs, begin, end);
-        __syncthreads();
-        const int lane = threadIdx.x & (h.width - 1);
-        for (long long s = h.first + threadIdx.x / h.width; s < h.last; s += kBlock / h.width) {
-            const int s0 = starts(s), s1 = starts(s + 1);
-            int n;
-            const double sum = team_sum(v, bits, max(s0, begin) - begin, min(s1, end) - begin,
-                                        lane, h.width, &n);
-            if (lane == 0) {
-                *(s0 < begin ? p.head + k : s1 > end ? p.tail + k : p.seq + s) = sum;
-                *(s0 < begin ? p.chead + k : s1 > end ? p.ctail + k : p.count + s) = n;
-            }
+    for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
+        const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
+        float v[kPacks][kEach];
+#pragma unroll
+        for (int h = 0; h < kPacks; h++) {
+            const Mine m = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
+            load_ratios(a, m, v[h]);
+            table.scan(h, m.mask);
         }
+        marks.clear();
+        __syncthreads();
+        for_sequences<kBlock>(starts, 2 * a.pairs, begin, end, [&](long long, int s0, int s1) {
+            mark_sequence(marks, max(s0, begin) - begin, min(s1, end) - begin);
+        });
+        __syncthreads();
+        sums.scan(marks, v);
+        __syncthreads();
+        for_sequences<kBlock>(starts, 2 * a.pairs, begin, end, [&](long long s, int s0, int s1) {
+            const int b = max(s0, begin) - begin, e = min(s1, end) - begin;
+            *p.sum.place(s, s0, s1, k, begin, end) =
+                Piece{sums.at[e - 1], table.up_to(e) - table.up_to(b)};
+        });
         __syncthreads();
     }
 }
 
-// A wave a pair.
-__global__ __launch_bounds__(kBlock) void preference_pairs(PreferenceArgs a, Pairs p)
+__global__ __launch_bounds__(kJoinBlock) void preference_pairs(PreferenceArgs a, Pairs p)
 {
-    __shared__ double red[kBlock / 64];
+    __shared__ double red[kJoinBlock / 64][6];
     const Starts starts{a.starts, a.tokens};
-    const int lane = threadIdx.x & 63;
-    double sum[5] = {0, 0, 0, 0, 0}, some = 0;
-    for (long long i = blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6); i < a.pairs;
-         i += gridDim.x * (kBlock / 64)) {
+    double sum[6] = {0, 0, 0, 0, 0, 0};  // the results, and how many pairs they are of
+    for (long long first = (long long)blockIdx.x * kJoinBlock; first < a.pairs;
+         first += (long long)gridDim.x * kJoinBlock) {
+        const long long i = first + threadIdx.x;
+        const bool has = i < a.pairs;
+        int s0[2], s1[2];
+        Piece v[2];
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            s0[k] = s1[k] = 0;
+            if (has)
+                starts.of(i + (long long)k * a.pairs, s0[k], s1[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+            v[k] = join(has, p.sum, i + (long long)k * a.pairs, s0[k], s1[k]);
+        if (!has)
+            continue;
         double r[2];
-        int n[2];
 #pragma unroll
         for (int k = 0; k < 2; k++) {
             const long long s = i + (long long)k * a.pairs;
-            const int s0 = starts(s), s1 = starts(s + 1);
-            n[k] = join_pieces(p.count, p.chead, p.ctail, s, s0, s1);
-            r[k] = reward(a, join_pieces(p.seq, p.head, p.tail, s, s0, s1), n[k]);
-            if (lane == 0) {
-                p.count[s] = n[k];
-                if (a.rewards)
-                    a.rewards[s] = (float)r[k];
-            }
+            r[k] = reward(a, v[k].sum, (int)v[k].n);
+            p.sum.seq[s] = v[k];
+            if (a.rewards)
+                a.rewards[s] = (float)r[k];
         }
-        if (lane == 0) {
-            const Pair q = pair_loss(a, r[0], r[1]);
-            p.slope[i] = q.slope;
-            if (n[0] + n[1] > 0) {
-                some += 1;
+        const Pair q = pair_loss(a, r[0], r[1]);
+        p.slope[i] = q.slope;
+        if (v[0].n + v[1].n > 0) {
 #pragma unroll
-                for (int k = 0; k < 5; k++)
-                    sum[k] += q.stats[k];
-            }
+            for (int k = 0; k < 5; k++)
+                sum[k] += q.stats[k];
+            sum[5] += 1;
         }
     }
-#pragma unroll
-    for (int k = 0; k < 5; k++) {
-        const double v = block_sum<kBlock>(sum[k], red);
-        if (threadIdx.x == 0)
-            p.part[blockIdx.x * 5 + k] = v;
-    }
-    some = block_sum<kBlock>(some, red);
-    if (threadIdx.x == 0)
-        p.some[blockIdx.x] = (int)some;
+    block_totals<kJoinBlock>(sum, red, [&](int i, double v) {
+        if (i < 5)
+            p.part[(size_t)i * gridDim.x + blockIdx.x] = v;
+        else
+            p.some[blockIdx.x] = (int)v;
+    });
 }
 
-// The chunk's gradients from LDS to memory.
-template <int BLOCK>
-__device__ __forceinline__ void store_gradients(const PreferenceArgs &a, int begin, int end,
-                                                const float *v)
+// The tokens' gradients from what lies where their sequences begin.
+template <int BLOCK, int PACKS>
+__device__ __forceinline__ void store_gradients(const PreferenceArgs &a, const Mine (&m)[PACKS],
+                                                int from, int to, Marks<BLOCK, PACKS> &marks,
+                                                const float *seq)
 {
+    int place[PACKS][kEach];
+    marks.places(place);
 #pragma unroll
-    for (int i = 0; i < kPacks; i++) {
-        const int t = ((int)threadIdx.x + i * BLOCK) * 4, left = end - begin - t;
-        if (left <= 0)
-            continue;
-        const unsigned m = load_mask(a.mask, begin + t, left);
-        F4 g;
+    for (int h = 0; h < PACKS; h++) {
+        const unsigned counted = m[h].mask & inside(m[h], from, to);
+        float g[kEach];
 #pragma unroll
-        for (int j = 0; j < 4; j++)
-            g[j] = m >> j & 1 ? v[t + j] : 0.f;
-        store_pack<float>(a.dlogp + begin + t, left, g);
+        for (int j = 0; j < kEach; j++) {
+            const float v = seq[max(place[h][j], 0)];
+            g[j] = counted >> j & 1 ? v : 0.f;
+        }
+        store_floats(a.dlogp, m[h], g);
     }
 }
 
-// The gradients; the first workgroup adds the results too.
-__global__ __launch_bounds__(5 * 64) void preference_fill(PreferenceArgs a, Pairs p, int chunks,
+// The gradients; the workgroup behind those of the chunks adds the results.
+__global__ __launch_bounds__(kBlock) void preference_fill(PreferenceArgs a, Pairs p, int chunks,
                                                           int joins)
 {
-    constexpr int BLOCK = 5 * 64;
-    __shared__ float v[kChunk];
-    __shared__ double red[BLOCK / 64];
+    __shared__ Marks<kBlock, kPacks> marks;
+    __shared__ float seq[kChunk];
     const Starts starts{a.starts, a.tokens};
-    const double u = 1.0 / (double)max(sum_counts<BLOCK>(p.some, joins, red), 1LL);
-    if (blockIdx.x == 0)
-        add_parts<5>(p.part, joins, u, a.stats);
-    if (!a.dlogp)
-        return;
-    for (int k = first_chunk(chunks, blockIdx.x); k < first_chunk(chunks, blockIdx.x + 1); k++) {
-        const int begin = k * kChunk, end = begin + min(kChunk, a.tokens - begin);
-        const Here h = sequences_here(a.starts, 2 * a.pairs, begin, end);
-        for (int t = threadIdx.x; t < end - begin; t += BLOCK)
-            v[t] = 0.f;
-        __syncthreads();
-        const int lane = threadIdx.x & (h.width - 1);
-        for (long long s = h.first + threadIdx.x / h.width; s < h.last; s += BLOCK / h.width) {
-            const int first = max(starts(s), begin) - begin, last = min(starts(s + 1), end) - begin;
-            const bool second = s >= a.pairs;
-            const float g = pair_gradient(a, p.slope[second ? s - a.pairs : s], second, p.count[s], u);
-            for (int t = first + lane; t < last; t += h.width)
-                v[t] = g;
+    const double u = 1.0 / max(sum_of(p.some, joins), 1);
+    const unsigned groups = gridDim.x - 1;
+    if (blockIdx.x == groups) {
+        for (int i = threadIdx.x >> 6; i < 5; i += kBlock / 64) {
+            const double v = sum_of(p.part + (size_t)i * joins, joins);
+            if ((threadIdx.x & 63) == 0)
+                a.stats[i] = (float)(v * u);
         }
+        return;
+    }
+    const int from = starts(0), to = starts(2LL * a.pairs);
+    for (int k = blockIdx.x; k < chunks; k += groups) {
+        const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
+        Mine m[kPacks];
+#pragma unroll
+        for (int h = 0; h < kPacks; h++)
+            m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
+        marks.clear();
         __syncthreads();
-        store_gradients<BLOCK>(a, begin, end, v);
+        for_sequences<kBlock>(starts, 2 * a.pairs, begin, end, [&](long long s, int s0, int) {
+            const bool second = s >= a.pairs;
+            const int at = max(s0, begin) - begin;
+            marks.at[at] = 1;
+            seq[at] = pair_gradient(a, p.slope[second ? s - a.pairs : s], second,
+                                    (int)p.sum.seq[s].n, u);
+        });
+        __syncthreads();
+        store_gradients(a, m, from, to, marks, seq);
         __syncthreads();
     }
 }
@@ -773,79 +1150,86 @@ constexpr int kOnePairs = 1024;
 
 __global__ __launch_bounds__(kOneBlock) void preference_one(PreferenceArgs a)
 {
-    constexpr int WAVES = kOneBlock / 64;
-    __shared__ float v[kOneChunk];
-    __shared__ unsigned char bits[kOneChunk];
-    __shared__ double sums[2 * kOnePairs];  // of ratios; then a pair's slope
-    __shared__ int count[2 * kOnePairs];
-    __shared__ double red[WAVES];
+    constexpr int PACKS = kOnePacks;
+    __shared__ Marks<kOneBlock, PACKS> marks;
+    __shared__ CountTable<kOneBlock, PACKS> table;
+    __shared__ Sums<kOneBlock, PACKS> sums;
+    __shared__ float seq[kOneChunk];
+    __shared__ double red[kOneBlock / 64][6];
     const Starts starts{a.starts, a.tokens};
-    const int seqs = 2 * a.pairs;
-    stage_ratios<kOneBlock>(a, 0, a.tokens, v, bits);
-    int width = 64;
-    while (width > 1 && (long long)width / 2 * seqs >= a.tokens)
-        width /= 2;
-    const int lane = threadIdx.x & (width - 1);
-    __syncthreads();
-    for (int s = threadIdx.x / width; s < seqs; s += kOneBlock / width) {
-        int n;
-        const double sum = team_sum(v, bits, starts(s), starts(s + 1), lane, width, &n);
-        if (lane == 0) {
-            sums[s] = sum;
-            count[s] = n;
-        }
+    Mine m[PACKS];
+    float v[PACKS][kEach];
+#pragma unroll
+    for (int h = 0; h < PACKS; h++) {
+        m[h] = my_tokens(a.mask, 0, a.tokens, rank_of<kOneBlock>(h));
+        load_ratios(a, m[h], v[h]);
+        table.scan(h, m[h].mask);
     }
-    __syncthreads();
-    double sum[5] = {0, 0, 0, 0, 0}, some = 0;
+    const int from = starts(0), to = starts(2LL * a.pairs);
+    // A thread a pair.
     const int i = threadIdx.x;
-    if (i < a.pairs) {
-        const int n0 = count[i], n1 = count[a.pairs + i];
-        const double r0 = reward(a, sums[i], n0), r1 = reward(a, sums[a.pairs + i], n1);
-        if (a.rewards) {
-            a.rewards[i] = (float)r0;
-            a.rewards[a.pairs + i] = (float)r1;
+    const bool has = i < a.pairs;
+    int s0[2], s1[2], n[2];
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        s0[k] = s1[k] = 0;
+        if (has)
+            starts.of(i + k * a.pairs, s0[k], s1[k]);
+    }
+    marks.clear();
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+        if (s0[k] < s1[k])
+            mark_sequence(marks, s0[k], s1[k]);
+    __syncthreads();
+    sums.scan(marks, v);
+    __syncthreads();
+    double sum[6] = {0, 0, 0, 0, 0, 0}, slope = 0;
+    if (has) {
+        double r[2];
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const bool some = s0[k] < s1[k];
+            n[k] = some ? table.up_to(s1[k]) - table.up_to(s0[k]) : 0;
+            r[k] = reward(a, some ? sums.at[s1[k] - 1] : 0.0, n[k]);
+            if (a.rewards)
+                a.rewards[i + k * a.pairs] = (float)r[k];
         }
-        const Pair q = pair_loss(a, r0, r1);
-        sums[i] = q.slope;
-        if (n0 + n1 > 0) {
-            some = 1;
+        const Pair q = pair_loss(a, r[0], r[1]);
+        slope = q.slope;
+        if (n[0] + n[1] > 0) {
 #pragma unroll
             for (int k = 0; k < 5; k++)
                 sum[k] = q.stats[k];
+            sum[5] = 1;
         }
     }
-    const double u = 1.0 / max(block_sum<kOneBlock>(some, red), 1.0);
+    block_sums<kOneBlock>(sum, red);
+    const double u = 1.0 / max(sum[5], 1.0);
+    if (threadIdx.x == 0)
 #pragma unroll
-    for (int k = 0; k < 5; k++) {
-        const double s = block_sum<kOneBlock>(sum[k], red);
-        if (threadIdx.x == 0)
-            a.stats[k] = (float)(s * u);
-    }
+        for (int k = 0; k < 5; k++)
+            a.stats[k] = (float)(sum[k] * u);
     if (!a.dlogp)
         return;
-    for (int t = threadIdx.x; t < a.tokens; t += kOneBlock)
-        v[t] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+        if (s0[k] < s1[k])
+            seq[s0[k]] = pair_gradient(a, slope, k == 1, n[k], u);
     __syncthreads();
-    for (int s = threadIdx.x / width; s < seqs; s += kOneBlock / width) {
-        const bool second = s >= a.pairs;
-        const float g = pair_gradient(a, sums[second ? s - a.pairs : s], second, count[s], u);
-        const int last = starts(s + 1);
-        for (int t = starts(s) + lane; t < last; t += width)
-            v[t] = g;
-    }
-    __syncthreads();
-    store_gradients<kOneBlock>(a, 0, a.tokens, v);
+    // Marks at the ends of sequences are the next one's beginning, or of tokens that
+    // are in none.
+    store_gradients(a, m, from, to, marks, seq);
 }
 
 // ---------------------------------------------------------------- launch rules
-static_assert(kPacks * 4 * kBlock == kChunk && kPacks * 4 * kOneBlock == kOneChunk, "chunks");
-static_assert(kPacks * 4 * 5 * 64 >= kChunk, "chunks of preference_fill");
-
 int chunks_of(long long tokens) { return (int)std::max(1LL, (tokens + kChunk - 1) / kChunk); }
 
-int join_groups(long long waves)
+// A thread a sequence or pair.
+int join_groups(long long n)
 {
-    return (int)std::min((waves + kBlock / 64 - 1) / (kBlock / 64), (long long)kJoinGroups);
+    return (int)std::max(1LL, std::min((n + kJoinBlock - 1) / kJoinBlock, (long long)kJoinGroups));
 }
 
 // One workgroup.
@@ -858,6 +1242,8 @@ bool preference_is_small(long long tokens, long long pairs)
 {
     return tokens <= kOneChunk && pairs <= kOnePairs;
 }
+
+static_assert(kOnePairs <= kOneBlock, "a thread a pair");
 
 // Arrays one after the other in the workspace, of 16 bytes' alignment.
 struct Arena {
@@ -877,10 +1263,10 @@ size_t layout(Counts &c, void *ws, long long tokens, long long seqs)
 {
     Arena a{(char *)ws};
     const int chunks = chunks_of(tokens);
-    c.part = a.take<double>(6 * std::min(chunks, kMaxGroups));
-    c.seq = a.take<int>(seqs);
-    c.head = a.take<int>(chunks);
-    c.tail = a.take<int>(chunks);
+    c.part = a.take<double>(5 * std::min(chunks, kMaxGroups));
+    c.n.seq = a.take<int>(seqs);
+    c.n.head = a.take<int>(chunks);
+    c.n.tail = a.take<int>(chunks);
     c.group = a.take<int>(kMaxGroups);
     c.some = a.take<int>(kJoinGroups);
     return a.used;
@@ -890,16 +1276,34 @@ size_t layout(Pairs &p, void *ws, long long tokens, long long pairs)
 {
     Arena a{(char *)ws};
     const int chunks = chunks_of(tokens);
-    p.seq = a.take<double>(2 * pairs);
-    p.head = a.take<double>(chunks);
-    p.tail = a.take<double>(chunks);
+    p.sum.seq = a.take<Piece>(2 * pairs);
+    p.sum.head = a.take<Piece>(chunks);
+    p.sum.tail = a.take<Piece>(chunks);
     p.slope = a.take<double>(pairs);
     p.part = a.take<double>(5 * kJoinGroups);
-    p.count = a.take<int>(2 * pairs);
-    p.chead = a.take<int>(chunks);
-    p.ctail = a.take<int>(chunks);
     p.some = a.take<int>(kJoinGroups);
     return a.used;
+}
+
+template <bool SEQS, Ref REF>
+void policy_tokens(const PolicyArgs &a, const Counts *c, int groups, int joins, hipStream_t stream)
+{
+    if (c)
+        policy_main<SEQS, REF><<<groups, kBlock, 0, stream>>>(a, *c, chunks_of(a.tokens), joins);
+    else
+        policy_one<SEQS, REF><<<1, kOneBlock, 0, stream>>>(a);
+}
+
+// The launch over the tokens: by chunks, or (c null) of one workgroup.
+template <bool SEQS>
+void policy_tokens(const PolicyArgs &a, const Counts *c, int groups, int joins, hipStream_t stream)
+{
+    if (!a.ref_logp)
+        policy_tokens<SEQS, Ref::none>(a, c, groups, joins, stream);
+    else if (a.kl == 2)
+        policy_tokens<SEQS, Ref::low>(a, c, groups, joins, stream);
+    else
+        policy_tokens<SEQS, Ref::other>(a, c, groups, joins, stream);
 }
 
 }  // namespace
@@ -913,28 +1317,21 @@ size_t policy_ws(long long tokens, long long seqs)
 hipError_t launch_policy(const PolicyArgs &a, hipStream_t stream)
 {
     const bool seqs = a.by_sequence || a.mean == 1;
+    const auto tokens = seqs ? policy_tokens<true> : policy_tokens<false>;
     if (policy_is_small(a.tokens, a.seqs)) {
-        if (seqs)
-            policy_one<true><<<1, kOneBlock, 0, stream>>>(a);
-        else
-            policy_one<false><<<1, kOneBlock, 0, stream>>>(a);
+        tokens(a, nullptr, 0, 0, stream);
         return hipGetLastError();
     }
     Counts c;
     layout(c, a.ws, a.tokens, a.seqs);
     const int chunks = chunks_of(a.tokens), groups = std::min(chunks, kMaxGroups);
-    int joins = 0;
+    const int joins = join_groups(a.seqs);
     if (a.mask && a.mean != 2)
         policy_count<<<groups, kBlock, 0, stream>>>(a, c, chunks);
-    if (a.mean == 1) {
-        joins = std::max(1, a.mask ? join_groups(a.seqs) : join_groups((a.seqs + 63LL) / 64));
-        policy_join<<<joins, kBlock, 0, stream>>>(a, c);
-    }
-    if (seqs)
-        policy_main<true><<<groups, kBlock, 0, stream>>>(a, c, chunks, joins);
-    else
-        policy_main<false><<<groups, kBlock, 0, stream>>>(a, c, chunks, joins);
-    policy_stats<<<1, 6 * 64, 0, stream>>>(c.part, groups, a.stats);
+    if (a.mean == 1)
+        policy_join<<<joins, kJoinBlock, 0, stream>>>(a, c);
+    tokens(a, &c, groups, joins, stream);
+    policy_stats<<<1, 5 * 64, 0, stream>>>(a, c.part, groups);
     return hipGetLastError();
 }
 
@@ -953,10 +1350,10 @@ hipError_t launch_preference(const PreferenceArgs &a, hipStream_t stream)
     Pairs p;
     layout(p, a.ws, a.tokens, a.pairs);
     const int chunks = chunks_of(a.tokens), groups = std::min(chunks, kMaxGroups);
-    const int joins = std::max(1, join_groups(a.pairs));
+    const int joins = join_groups(a.pairs);
     preference_sums<<<groups, kBlock, 0, stream>>>(a, p, chunks);
-    preference_pairs<<<joins, kBlock, 0, stream>>>(a, p);
-    preference_fill<<<a.dlogp ? groups : 1, 5 * 64, 0, stream>>>(a, p, chunks, joins);
+    preference_pairs<<<joins, kJoinBlock, 0, stream>>>(a, p);
+    preference_fill<<<(a.dlogp ? groups : 0) + 1, kBlock, 0, stream>>>(a, p, chunks, joins);
     return hipGetLastError();
 }
 

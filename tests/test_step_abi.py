@@ -158,7 +158,7 @@ def test_policy_loss_refuses(L, want, args):
     dict(dlp=None, dh=None), dict(starts=None, seqs=0, mean=0), dict(by_seq=1, adv=E),
     dict(tokens=0, lp=None, lo=None, lr=None, h=None, adv=None),
     dict(seqs=0, by_seq=1, adv=None), dict(low=1.0, high=inf, dual=inf), dict(mean=2, count=1.0),
-    dict(tokens=8192, ws=None, n=0), dict(mask=G + 1), dict(kw=-1.0, ew=-1.0, scale=-2.0)], ids=str)
+    dict(tokens=4096, ws=None, n=0), dict(mask=G + 1), dict(kw=-1.0, ew=-1.0, scale=-2.0)], ids=str)
 def test_policy_loss_takes(L, args):
     assert policy(L, **args) == launched()
 
@@ -192,17 +192,17 @@ def test_preference_loss_takes(L, args):
 
 
 def test_workspace_sizes(L):
-    assert L.policy_loss_workspace_size(8192, 8192) == 0
-    assert L.policy_loss_workspace_size(8193, 1) > 0 and L.policy_loss_workspace_size(1, 8193) > 0
-    assert L.preference_loss_workspace_size(8192, 1024) == 0
-    assert L.preference_loss_workspace_size(8193, 1) > 0
+    assert L.policy_loss_workspace_size(4096, 4096) == 0
+    assert L.policy_loss_workspace_size(4097, 1) > 0 and L.policy_loss_workspace_size(1, 4097) > 0
+    assert L.preference_loss_workspace_size(4096, 1024) == 0
+    assert L.preference_loss_workspace_size(4097, 1) > 0
     assert L.preference_loss_workspace_size(1, 1025) > 0
     for bad in ((-1, 1), (1 << 31, 1), (1, -1), (1, 1 << 31)):
         assert L.policy_loss_workspace_size(*bad) == 0
         assert L.preference_loss_workspace_size(*bad) == 0
     # Each sequence, pair and chunk has its numbers: no more than some bytes a token.
     assert L.policy_loss_workspace_size((1 << 31) - 1, 1000) < 1 << 25
-    for cols in (64, 8192, 40000):
+    for cols in (64, 4096, 40000):
         for t in (F32, BF16):
             assert (L.residual_norm_fwd_workspace_size(t, 100, cols) ==
                     L.layernorm_fwd_workspace_size(t, 100, cols))
