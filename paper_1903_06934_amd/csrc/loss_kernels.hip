@@ -178,41 +178,70 @@ struct Search {
     }
 };
 
-// Calls f(s, s0, s1), each in one thread of the workgroup, for the sequences s (the
-// tokens s0 <= t < s1) that have tokens in the chunk begin <= t < end.  Up to kDirect
-// sequences each thread looks at its share of all (one latency); more of them are
-// searched for the chunk's first and last.
-constexpr int kLook = 2, kDirect = 8 * kBlock;
+// The sequences that have tokens in the chunk begin <= t < end, for all threads of a
+// workgroup to go through.  Up to kDirect sequences each thread looks at its share of all
+// of them; more are searched for the chunk's first and last.  The first kLook of a
+// thread's share are loaded at once, and before the chunk's tokens, so that these
+// latencies overlap.
+constexpr int kLook = 4, kDirect = 8 * kBlock;
 
-template <int BLOCK, class F>
-__device__ __forceinline__ void for_sequences(const Starts &starts, int seqs, int begin, int end,
-                                              F f)
-{
-    int first = 0, last = seqs;
-    if (seqs > kDirect) {
-        Search a{starts.p + 1, begin, 0, seqs}, b{starts.p, (long long)end - 1, 0, seqs};
-        while (a.open() || b.open()) {
-            const bool pa = a.open() && a.probe(), pb = b.open() && b.probe();
-            const int ka = __popcll(__ballot(pa)), kb = __popcll(__ballot(pb));
-            if (a.open())
-                a.narrow(ka);
-            if (b.open())
-                b.narrow(kb);
+template <int BLOCK>
+struct Sequences {
+    Starts starts;
+    int begin, end, first, last;
+    int s0[kLook], s1[kLook];
+
+    __device__ __forceinline__ Sequences(const Starts &st, int seqs, int begin_, int end_)
+        : starts(st), begin(begin_), end(end_), first(0), last(seqs)
+    {
+        if (seqs > kDirect) {
+            Search a{starts.p + 1, begin, 0, seqs}, b{starts.p, (long long)end - 1, 0, seqs};
+            while (a.open() || b.open()) {
+                const bool pa = a.open() && a.probe(), pb = b.open() && b.probe();
+                const int ka = __popcll(__ballot(pa)), kb = __popcll(__ballot(pb));
+                if (a.open())
+                    a.narrow(ka);
+                if (b.open())
+                    b.narrow(kb);
+            }
+            first = a.lo;
+            last = b.lo;
         }
-        first = a.lo;
-        last = b.lo;
+        look((long long)first + threadIdx.x);
     }
-    for (long long at = first + (long long)threadIdx.x; at < last; at += kLook * BLOCK) {
-        int s0[kLook], s1[kLook];
+    __device__ __forceinline__ void look(long long at)
+    {
+        // A place past the last is looked at all the same (starts has one entry more than
+        // there are sequences), so that no load waits behind a branch.
+        const long long most = max(last - 1, 0);
 #pragma unroll
         for (int i = 0; i < kLook; i++)
-            starts.of(min(at + i * BLOCK, (long long)last - 1), s0[i], s1[i]);
+            if (last > 0)
+                starts.of(min(at + i * BLOCK, most), s0[i], s1[i]);
+    }
+    // f(s, s0, s1), in one thread, for each sequence s, the tokens s0 <= t < s1.
+    template <class F>
+    __device__ __forceinline__ void each(F f)
+    {
+        long long at = (long long)first + threadIdx.x;
+        visit(at, f);
+        if (last - first <= kLook * BLOCK)
+            return;
+        for (at += kLook * BLOCK; at < last; at += kLook * BLOCK) {
+            look(at);
+            visit(at, f);
+        }
+        look((long long)first + threadIdx.x);  // for the next time
+    }
+    template <class F>
+    __device__ __forceinline__ void visit(long long at, F f)
+    {
 #pragma unroll
         for (int i = 0; i < kLook; i++)
             if (at + i * BLOCK < last && s0[i] < s1[i] && s0[i] < end && s1[i] > begin)
                 f(at + i * BLOCK, s0[i], s1[i]);
     }
-}
+};
 
 // What chunks left of a sequence.
 template <class V>
@@ -272,6 +301,15 @@ struct Mine {
     unsigned mask;  // a bit each: there, and not masked
 };
 
+// A bit for each of four bytes: whether it is not 0.
+__device__ __forceinline__ unsigned bits_of(uint32_t v)
+{
+    v |= v >> 4;
+    v |= v >> 2;
+    v = (v | v >> 1) & 0x01010101u;
+    return (v | v >> 7 | v >> 14 | v >> 21) & 15;
+}
+
 // rank: of the pack in the chunk.
 __device__ __forceinline__ Mine my_tokens(const unsigned char *mask, int begin, int end, int rank)
 {
@@ -279,32 +317,26 @@ __device__ __forceinline__ Mine my_tokens(const unsigned char *mask, int begin, 
     // Past the end the first token may be beyond 32 bits: it is not used.
     m.left = end - begin - rank * kEach;
     m.t0 = m.left > 0 ? begin + rank * kEach : begin;
-    m.mask = m.left >= kEach ? (1u << kEach) - 1 : m.left > 0 ? (1u << m.left) - 1 : 0;
+    m.mask = (1u << min(max(m.left, 0), kEach)) - 1;
     if (mask && m.left > 0) {
-        unsigned bits = 0;
         if (m.left >= kEach) {
             typedef uint32_t At __attribute__((aligned(1)));
-            const uint32_t v = *(const At *)(mask + m.t0);
-#pragma unroll
-            for (int j = 0; j < kEach; j++)
-                bits |= (unsigned)((v >> 8 * j & 255) != 0) << j;
+            m.mask = bits_of(*(const At *)(mask + m.t0));
         } else {
+            m.mask = 0;
             for (int j = 0; j < m.left; j++)
-                bits |= (unsigned)(mask[m.t0 + j] != 0) << j;
+                m.mask |= (unsigned)(mask[m.t0 + j] != 0) << j;
         }
-        m.mask = bits;
     }
     return m;
 }
 
-// Those of the thread's tokens that lie in from <= t < to.
+// Those of the pack's tokens that lie in from <= t < to.
 __device__ __forceinline__ unsigned inside(const Mine &m, int from, int to)
 {
-    unsigned bits = 0;
-#pragma unroll
-    for (int j = 0; j < kEach; j++)
-        bits |= (unsigned)(m.left > j && m.t0 + j >= from && m.t0 + j < to) << j;
-    return bits;
+    // Tokens past the end are not in the mask.
+    const unsigned before = (1u << min(max(from - m.t0, 0), kEach)) - 1;
+    return ((1u << min(max(to - m.t0, 0), kEach)) - 1) & ~before;
 }
 
 __device__ __forceinline__ void load_floats(const float *p, const Mine &m, float (&v)[kEach])
@@ -448,15 +480,15 @@ __global__ __launch_bounds__(kBlock) void policy_count(PolicyArgs a, Counts c, i
     for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
         const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
         Mine m[kPacks];
-#pragma unroll
-        for (int h = 0; h < kPacks; h++)
-            m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
         if (a.mean == 1) {
+            Sequences<kBlock> q(starts, a.seqs, begin, end);
 #pragma unroll
-            for (int h = 0; h < kPacks; h++)
+            for (int h = 0; h < kPacks; h++) {
+                m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
                 table.scan(h, m[h].mask);
+            }
             __syncthreads();
-            for_sequences<kBlock>(starts, a.seqs, begin, end, [&](long long s, int s0, int s1) {
+            q.each([&](long long s, int s0, int s1) {
                 *c.n.place(s, s0, s1, k, begin, end) =
                     table.up_to(min(s1, end) - begin) - table.up_to(max(s0, begin) - begin);
             });
@@ -464,8 +496,10 @@ __global__ __launch_bounds__(kBlock) void policy_count(PolicyArgs a, Counts c, i
         } else {
             const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
 #pragma unroll
-            for (int h = 0; h < kPacks; h++)
+            for (int h = 0; h < kPacks; h++) {
+                m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
                 all[0] += __popc(m[h].mask & inside(m[h], from, to));
+            }
         }
     }
     if (a.mean == 1)
@@ -535,20 +569,17 @@ __device__ __forceinline__ float low_kl(float x, float *expm1)
     return v;
 }
 
-// The borders of the clip in 32 bits, how near to them (2^-22 of each) 32 bits do not
-// tell on which side a log ratio is, and the ratio at them.
+// The borders of the clip in 32 bits, and the ratio at them.
 struct Borders {
-    float low, high, dual, near_low, near_high, near_dual, at_low, at_high, at_dual;
+    float low, high, dual, at_low, at_high, at_dual;
+    float near;  // how near to a border 32 bits do not tell on which side a log ratio is
 
     __device__ __forceinline__ explicit Borders(const PolicyArgs &a)
-        : low((float)a.log_low), high((float)a.log_high), dual((float)a.log_dual),
-          near_low(near(low)), near_high(near(high)), near_dual(near(dual)),
-          at_low(a.low), at_high(a.high), at_dual(a.dual)
+        : low((float)a.log_low), high((float)a.log_high), dual((float)a.log_dual), at_low(a.low),
+          at_high(a.high), at_dual(a.dual)
     {
-    }
-    static __device__ __forceinline__ float near(float v)
-    {
-        return __builtin_isfinite(v) ? fabsf(v) * 0x1p-22f : -1.f;  // none is near an infinity
+        const auto size = [](float v) { return __builtin_isfinite(v) ? fabsf(v) : 0.f; };
+        near = fmaxf(fmaxf(size(low), size(high)), size(dual)) * 0x1p-22f;
     }
 };
 
@@ -567,21 +598,21 @@ __device__ __forceinline__ Token token_loss(const PolicyArgs &a, const Borders &
     Token k;
     const float d = lp - lo;  // off by 2^-24 of it
     k.ratio = exp_of(d);
-    bool high = d > b.high, low = d < b.low, dual = d > b.dual;
-    if (fabsf(d - b.high) <= b.near_high || fabsf(d - b.low) <= b.near_low ||
-        fabsf(d - b.dual) <= b.near_dual) {
+    // Above: clipped there for a gain, by the dual clip for a loss; below for a loss.
+    const bool gain = adv > 0.f;
+    const float b_high = b.high, b_dual = b.dual, b_low = b.low, at_high = b.at_high,
+                at_dual = b.at_dual;  // a choice of values, not of addresses
+    const float top = gain ? b_high : b_dual, bottom = gain ? -__builtin_inff() : b_low;
+    bool above = d > top, below = d < bottom;
+    if (fabsf(d - top) <= b.near || fabsf(d - bottom) <= b.near) {
         const double e = (double)lp - (double)lo;
-        high = e > a.log_high;
-        low = e < a.log_low;
-        dual = e > a.log_dual;
+        above = gain ? e > a.log_high : e > a.log_dual;
+        below = !gain && e < a.log_low;
     }
-    const bool gain = adv > 0.f, loss = adv < 0.f;
-    // A choice of values in registers; of members it would be one of addresses, with a
-    // load a token.
-    const float at_low = b.at_low, at_high = b.at_high, at_dual = b.at_dual;
-    const float bound = gain ? at_high : dual ? at_dual : at_low;
-    k.clipped = (gain && high) || (loss && (low || dual));
-    k.surrogate = -adv * (k.clipped ? bound : k.ratio);
+    float r = above ? (gain ? at_high : at_dual) : k.ratio;
+    r = below ? b.at_low : r;
+    k.clipped = (above || below) && fabsf(adv) > 0.f;
+    k.surrogate = -adv * r;
     k.slope = k.clipped ? 0.f : k.surrogate;
     k.kl = 0.f;
     if constexpr (REF != Ref::none) {
@@ -624,28 +655,31 @@ __device__ __forceinline__ void load_tokens(const PolicyArgs &a, const Mine &m, 
 
 // The tokens' surrogates, divergences, entropies, ratios and clips (times their
 // weights within their sequences, if WEIGHTS) to sum, their gradients to memory.
-// counted: the tokens that count; w: their weights; u: what all weights are multiplied by.
+// counted: the tokens that count; w: their weights; factor: what those of the gradients
+// are multiplied by.
 template <bool WEIGHTS, Ref REF>
-__device__ __forceinline__ void token_losses(const PolicyArgs &a, const Mine &m, const Tokens &k,
-                                             unsigned counted, const float (&w)[kEach], double u,
+__device__ __forceinline__ void token_losses(const PolicyArgs &a, const Borders &borders,
+                                             const Mine &m, const Tokens &k, unsigned counted,
+                                             const float (&w)[kEach], float factor,
                                              double (&sum)[5])
 {
-    const float factor = (float)(u * a.scale);
-    const Borders borders(a);
     float g[kEach], gh[kEach], part[5] = {0, 0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < kEach; j++) {
+        // A token that does not count is one of nothing but zeros, with no weight.
         const bool in = counted >> j & 1;
-        const Token r = token_loss<REF>(a, borders, k.lp[j], k.lo[j],
-                                        REF == Ref::none ? 0.f : k.lr[j], k.adv[j]);
-        const float d = WEIGHTS ? w[j] : 1.f, f = WEIGHTS ? d * factor : factor;
-        const float v[5] = {r.surrogate, r.kl, k.h[j], r.ratio,
-                            r.clipped ? 1.f : 0.f};
-#pragma unroll
-        for (int i = 0; i < 5; i++)
-            part[i] += in ? (WEIGHTS ? v[i] * d : v[i]) : 0.f;
-        g[j] = in ? r.slope * f : 0.f;
-        gh[j] = in ? -a.entropy_weight * f : 0.f;
+        const auto only = [in](float v) { return in ? v : 0.f; };
+        const Token r = token_loss<REF>(a, borders, only(k.lp[j]), only(k.lo[j]),
+                                        REF == Ref::none ? 0.f : only(k.lr[j]), only(k.adv[j]));
+        const float d = only(WEIGHTS ? w[j] : 1.f), f = d * factor;
+        part[0] = fmaf(r.surrogate, d, part[0]);
+        if (REF != Ref::none)
+            part[1] = fmaf(r.kl, d, part[1]);
+        part[2] = fmaf(only(k.h[j]), d, part[2]);
+        part[3] = fmaf(r.ratio, d, part[3]);
+        part[4] += r.clipped ? d : 0.f;
+        g[j] = r.slope * f;
+        gh[j] = -a.entropy_weight * f;
         __builtin_amdgcn_sched_barrier(0);  // a token at a time: fewer registers, more waves
     }
 #pragma unroll
@@ -713,6 +747,8 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
     __shared__ double red[WAVES][5];
     __shared__ int counts[WAVES][1];
     const Starts starts{a.starts, a.tokens};
+    const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
+    Sequences<kOneBlock> q(starts, SEQS ? a.seqs : 0, 0, a.tokens);
     Mine m[PACKS];
     Tokens k[PACKS];
     float w[PACKS][kEach];
@@ -724,7 +760,6 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
         for (int j = 0; j < kEach; j++)
             w[h][j] = 1.f;
     }
-    const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
     int n[1] = {0};  // tokens that count, or sequences that have any
 #pragma unroll
     for (int h = 0; h < PACKS; h++)
@@ -738,7 +773,7 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
         __syncthreads();
         if (a.mean == 1)
             n[0] = 0;
-        for_sequences<kOneBlock>(starts, a.seqs, 0, a.tokens, [&](long long s, int s0, int s1) {
+        q.each([&](long long s, int s0, int s1) {
             const int c = table.up_to(s1) - table.up_to(s0);
             if (a.mean == 1)
                 n[0] += c > 0;
@@ -754,10 +789,12 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
         __syncthreads();
         from_sequences(a, marks, seq, k, w);
     }
+    const Borders borders(a);
     double sum[5] = {0, 0, 0, 0, 0};
 #pragma unroll
     for (int h = 0; h < PACKS; h++)
-        token_losses<SEQS, REF>(a, m[h], k[h], m[h].mask & inside(m[h], from, to), w[h], u, sum);
+        token_losses<SEQS, REF>(a, borders, m[h], k[h], m[h].mask & inside(m[h], from, to), w[h],
+                                (float)(u * a.scale), sum);
     block_sums<kOneBlock>(sum, red);
 #pragma unroll
     for (int i = 0; i < 5; i++)
@@ -769,16 +806,26 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
 }
 
 template <bool SEQS, Ref REF>
-__global__ __launch_bounds__(kBlock) void policy_main(PolicyArgs a, Counts c, int chunks, int joins)
+__global__ __launch_bounds__(kBlock, 4) void policy_main(PolicyArgs a, Counts c, int chunks, int joins)
 {
     __shared__ Marks<SEQS ? kBlock : 64, kPacks> marks;
     __shared__ OfSequence seq[SEQS ? kChunk : 1];
     __shared__ double red[kBlock / 64][5], of_all;
     const Starts starts{a.starts, a.tokens};
+    const Borders borders(a);
     double u = 0.0, sum[5] = {0, 0, 0, 0, 0};
-    int from = 0, to = 0;
+    const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
+    if (threadIdx.x < 64) {  // what all weights are multiplied by
+        double n = a.count;
+        if (a.mean == 1)
+            n = max(sum_of(c.some, joins), 1);
+        else if (a.mean == 0)
+            n = max(a.mask ? sum_of(c.group, (int)gridDim.x) : to - from, 1);
+        of_all = 1.0 / n;
+    }
     for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
         const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
+        Sequences<kBlock> q(starts, SEQS ? a.seqs : 0, begin, end);
         Mine m[kPacks];
         Tokens tokens[kPacks];
         float w[kPacks][kEach];
@@ -793,34 +840,22 @@ __global__ __launch_bounds__(kBlock) void policy_main(PolicyArgs a, Counts c, in
         if constexpr (SEQS) {
             marks.clear();
             __syncthreads();
-            for_sequences<kBlock>(starts, a.seqs, begin, end, [&](long long s, int s0, int s1) {
+            q.each([&](long long s, int s0, int s1) {
                 const int at = max(s0, begin) - begin;
                 marks.at[at] = 1;
                 seq[at] = of_sequence(a, s, a.mean != 1 ? 1 : a.mask ? c.n.seq[s] : s1 - s0);
             });
         }
-        const bool first = k == (int)blockIdx.x;
-        if (first) {
-            from = a.starts ? starts(0) : 0;
-            to = a.starts ? starts(a.seqs) : a.tokens;
-            if (threadIdx.x < 64) {  // what all weights are multiplied by
-                double n = a.count;
-                if (a.mean == 1)
-                    n = max(sum_of(c.some, joins), 1);
-                else if (a.mean == 0)
-                    n = max(a.mask ? sum_of(c.group, (int)gridDim.x) : to - from, 1);
-                of_all = 1.0 / n;
-            }
-        }
-        if (SEQS || first)
+        if (SEQS || k == (int)blockIdx.x)
             __syncthreads();
         u = of_all;
         if constexpr (SEQS)
             from_sequences(a, marks, seq, tokens, w);
 #pragma unroll
         for (int h = 0; h < kPacks; h++)
-            token_losses<SEQS, REF>(a, m[h], tokens[h], m[h].mask & inside(m[h], from, to), w[h], u,
-                                    sum);
+            token_losses<SEQS, REF>(a, borders, m[h], tokens[h],
+                                    m[h].mask & inside(m[h], from, to), w[h],
+                                    (float)(u * a.scale), sum);
         if (SEQS)
             __syncthreads();
     }
@@ -904,12 +939,12 @@ __device__ __forceinline__ Pair pair_loss(const PreferenceArgs &a, double r0, do
     return p;
 }
 
-// A token's gradient in a sequence of n tokens that count.
-__device__ __forceinline__ float pair_gradient(const PreferenceArgs &a, double slope, bool second,
-                                               int n, double u)
+// A token's gradient in a sequence of n tokens that count, but for the pairs' number.
+__device__ __forceinline__ double pair_gradient(const PreferenceArgs &a, double slope, bool second,
+                                               int n)
 {
-    const double v = slope * a.beta * a.scale * u / (a.length_mean ? max(n, 1) : 1);
-    return (float)(second ? -v : v);
+    const double v = slope * a.beta * a.scale / (a.length_mean ? max(n, 1) : 1);
+    return second ? -v : v;
 }
 
 // The tokens' log ratios, 0 where they do not count.
@@ -1014,6 +1049,7 @@ __global__ __launch_bounds__(kBlock) void preference_sums(PreferenceArgs a, Pair
     const Starts starts{a.starts, a.tokens};
     for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
         const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
+        Sequences<kBlock> q(starts, 2 * a.pairs, begin, end);
         float v[kPacks][kEach];
 #pragma unroll
         for (int h = 0; h < kPacks; h++) {
@@ -1023,13 +1059,13 @@ __global__ __launch_bounds__(kBlock) void preference_sums(PreferenceArgs a, Pair
         }
         marks.clear();
         __syncthreads();
-        for_sequences<kBlock>(starts, 2 * a.pairs, begin, end, [&](long long, int s0, int s1) {
+        q.each([&](long long, int s0, int s1) {
             mark_sequence(marks, max(s0, begin) - begin, min(s1, end) - begin);
         });
         __syncthreads();
         sums.scan(marks, v);
         __syncthreads();
-        for_sequences<kBlock>(starts, 2 * a.pairs, begin, end, [&](long long s, int s0, int s1) {
+        q.each([&](long long s, int s0, int s1) {
             const int b = max(s0, begin) - begin, e = min(s1, end) - begin;
             *p.sum.place(s, s0, s1, k, begin, end) =
                 Piece{sums.at[e - 1], table.up_to(e) - table.up_to(b)};
@@ -1090,7 +1126,7 @@ __global__ __launch_bounds__(kJoinBlock) void preference_pairs(PreferenceArgs a,
 template <int BLOCK, int PACKS>
 __device__ __forceinline__ void store_gradients(const PreferenceArgs &a, const Mine (&m)[PACKS],
                                                 int from, int to, Marks<BLOCK, PACKS> &marks,
-                                                const float *seq)
+                                                const double *seq, double u)
 {
     int place[PACKS][kEach];
     marks.places(place);
@@ -1100,7 +1136,7 @@ __device__ __forceinline__ void store_gradients(const PreferenceArgs &a, const M
         float g[kEach];
 #pragma unroll
         for (int j = 0; j < kEach; j++) {
-            const float v = seq[max(place[h][j], 0)];
+            const float v = (float)(seq[max(place[h][j], 0)] * u);
             g[j] = counted >> j & 1 ? v : 0.f;
         }
         store_floats(a.dlogp, m[h], g);
@@ -1112,11 +1148,14 @@ __global__ __launch_bounds__(kBlock) void preference_fill(PreferenceArgs a, Pair
                                                           int joins)
 {
     __shared__ Marks<kBlock, kPacks> marks;
-    __shared__ float seq[kChunk];
+    __shared__ double seq[kChunk];
     const Starts starts{a.starts, a.tokens};
-    const double u = 1.0 / max(sum_of(p.some, joins), 1);
+    __shared__ double of_all;
     const unsigned groups = gridDim.x - 1;
+    if (threadIdx.x < 64)
+        of_all = 1.0 / max(sum_of(p.some, joins), 1);  // what all pairs are multiplied by
     if (blockIdx.x == groups) {
+        const double u = 1.0 / max(sum_of(p.some, joins), 1);
         for (int i = threadIdx.x >> 6; i < 5; i += kBlock / 64) {
             const double v = sum_of(p.part + (size_t)i * joins, joins);
             if ((threadIdx.x & 63) == 0)
@@ -1127,21 +1166,22 @@ __global__ __launch_bounds__(kBlock) void preference_fill(PreferenceArgs a, Pair
     const int from = starts(0), to = starts(2LL * a.pairs);
     for (int k = blockIdx.x; k < chunks; k += groups) {
         const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
+        Sequences<kBlock> q(starts, 2 * a.pairs, begin, end);
         Mine m[kPacks];
 #pragma unroll
         for (int h = 0; h < kPacks; h++)
             m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
         marks.clear();
         __syncthreads();
-        for_sequences<kBlock>(starts, 2 * a.pairs, begin, end, [&](long long s, int s0, int) {
+        q.each([&](long long s, int s0, int) {
             const bool second = s >= a.pairs;
             const int at = max(s0, begin) - begin;
             marks.at[at] = 1;
             seq[at] = pair_gradient(a, p.slope[second ? s - a.pairs : s], second,
-                                    (int)p.sum.seq[s].n, u);
+                                    (int)p.sum.seq[s].n);
         });
         __syncthreads();
-        store_gradients(a, m, from, to, marks, seq);
+        store_gradients(a, m, from, to, marks, seq, of_all);
         __syncthreads();
     }
 }
@@ -1154,7 +1194,7 @@ __global__ __launch_bounds__(kOneBlock) void preference_one(PreferenceArgs a)
     __shared__ Marks<kOneBlock, PACKS> marks;
     __shared__ CountTable<kOneBlock, PACKS> table;
     __shared__ Sums<kOneBlock, PACKS> sums;
-    __shared__ float seq[kOneChunk];
+    __shared__ double seq[kOneChunk];
     __shared__ double red[kOneBlock / 64][6];
     const Starts starts{a.starts, a.tokens};
     Mine m[PACKS];
@@ -1216,11 +1256,11 @@ __global__ __launch_bounds__(kOneBlock) void preference_one(PreferenceArgs a)
 #pragma unroll
     for (int k = 0; k < 2; k++)
         if (s0[k] < s1[k])
-            seq[s0[k]] = pair_gradient(a, slope, k == 1, n[k], u);
+            seq[s0[k]] = pair_gradient(a, slope, k == 1, n[k]);
     __syncthreads();
     // Marks at the ends of sequences are the next one's beginning, or of tokens that
     // are in none.
-    store_gradients(a, m, from, to, marks, seq);
+    store_gradients(a, m, from, to, marks, seq, u);
 }
 
 // ---------------------------------------------------------------- launch rules
