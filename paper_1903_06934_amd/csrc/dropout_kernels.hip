@@ -2,8 +2,14 @@
 //
 // Element e's 16 random bits are computed where they are used, eight elements at
 // a time (random.h), and nothing of the mask is stored; both directions are one
-// kernel.
+// kernel.  Bound by memory: 16384 x 4096 bf16 43 us (6.2 TB/s; a copy of as many bytes
+// takes 50), onto a residual 64.7; 12544 x 513 fp32 inside wider rows 13.2 (a copy 11.5).
+// The generator's twenty 32 x 32 bit products for eight elements are what else it does:
+// with 32 bits an element there would be twice as many, more than the memory hides.
+// The figures at the rules are of whole calls replayed from a graph on three inputs in
+// turn, both sides of a rule in one run.
 #include <algorithm>
+#include <initializer_list>
 
 #include "internal.h"
 #include "random.h"
@@ -14,7 +20,10 @@ namespace miconv {
 
 namespace {
 
-constexpr int kGroups = 2;  // of eight elements, in flight a thread
+// Packs in flight a thread: of eight 16-bit elements (16384 x 4096 bf16 43.6 us, of two
+// packs 46.4), or of four 32-bit ones (12544 x 513 fp32 13.3 us, of eight packs 18.9).
+template <class T>
+constexpr int kPacksOf = Pack<T>::N == 8 ? 1 : 4;
 
 template <class T>
 __device__ __forceinline__ T dropped(const Dropper &drop, T x, T residual, uint32_t word, int odd)
@@ -23,29 +32,61 @@ __device__ __forceinline__ T dropped(const Dropper &drop, T x, T residual, uint3
     return (T)(v + (float)residual);
 }
 
-// FLAT: the rows lie behind each other in all tensors, as one row of all elements.
-// Otherwise a group's eight elements may lie in several rows.
-template <class T, bool FLAT>
-__global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, long long groups)
+// The words of a thread's packs q[0 .. U).  A group of eight 32-bit elements is two
+// packs, of neighbouring threads: of two packs each the even thread computes the first
+// one's group, the odd one the second one's, and they exchange halves (16384 x 2048 fp32:
+// 47.6 us, with two packs side by side a thread 77.5).  All threads of a wave call it.
+template <class T>
+__device__ __forceinline__ void words_of(const Dropper &drop, const long long (&q)[kPacksOf<T>],
+                                         uint32_t (&w)[kPacksOf<T>][Pack<T>::N / 2])
 {
-    constexpr int N = Pack<T>::N, K = 8 / N;  // packs a group
+    constexpr int U = kPacksOf<T>;
+    if constexpr (Pack<T>::N == 8) {
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            drop.group((unsigned long long)q[u], w[u]);
+    } else {
+        const bool odd = threadIdx.x & 1;
+#pragma unroll
+        for (int u = 0; u < U; u += 2) {
+            uint32_t g[4], got[2];
+            drop.group((unsigned long long)(odd ? q[u + 1] : q[u]) >> 1, g);
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const uint32_t give = odd ? g[i] : g[2 + i];
+                got[i] = __builtin_amdgcn_mov_dpp((int)give, 0xb1, 0xf, 0xf, true);
+                w[u][i] = odd ? got[i] : g[i];
+                w[u + 1][i] = odd ? g[2 + i] : got[i];
+            }
+        }
+    }
+}
+
+// FLAT: the rows lie behind each other in all tensors, as one row of all elements.
+// Otherwise a pack's elements may lie in several rows.
+template <class T, bool FLAT, bool STREAM>
+__global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, long long packs)
+{
+    constexpr int N = Pack<T>::N, U = kPacksOf<T>;
     typedef typename Pack<T>::V V;
+    typedef typename Pack<T>::At At;
     const Dropper drop(a.drop);
     const T *x = (const T *)a.x.p, *res = (const T *)a.residual.p;
     T *y = (T *)a.y.p;
     const long long n = a.rows * a.cols;
     const double inv = 1.0 / (double)a.cols;
-    for (long long first = (long long)blockIdx.x * 256 * kGroups; first < groups;
-         first += (long long)gridDim.x * 256 * kGroups) {
-        V vx[kGroups][K], vr[kGroups][K];
-        long long row[kGroups], col[kGroups];
-        bool whole[kGroups];
+    for (long long first = (long long)blockIdx.x * 256 * U; first < packs;
+         first += (long long)gridDim.x * 256 * U) {
+        V vx[U], vr[U];
+        long long q[U], row[U], col[U];
+        bool whole[U];
 #pragma unroll
-        for (int u = 0; u < kGroups; u++) {
-            const long long g = first + u * 256 + threadIdx.x, e = g * 8;
+        for (int u = 0; u < U; u++) {
+            q[u] = first + u * 256 + threadIdx.x;
+            const long long e = q[u] * N;
             row[u] = 0;
             col[u] = e;
-            if (!FLAT && g < groups) {
+            if (!FLAT && q[u] < packs) {
                 row[u] = (long long)((double)e * inv);  // off by one at most
                 col[u] = e - row[u] * a.cols;
                 if (col[u] < 0) {
@@ -56,70 +97,101 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, long long g
                     col[u] -= a.cols;
                 }
             }
-            whole[u] = g < groups && (FLAT ? e + 8 <= n : col[u] + 8 <= a.cols);
-#pragma unroll
-            for (int k = 0; k < K; k++) {
-                vx[u][k] = vr[u][k] = V{};
-                if (whole[u]) {
-                    vx[u][k] = *(const typename Pack<T>::At *)(x + row[u] * a.x.ld + col[u] + k * N);
-                    if (res)
-                        vr[u][k] = *(const typename Pack<T>::At *)(res + row[u] * a.residual.ld +
-                                                                   col[u] + k * N);
+            whole[u] = q[u] < packs && (FLAT ? e + N <= n : col[u] + N <= a.cols);
+            vx[u] = vr[u] = V{};
+            if (whole[u]) {
+                const At *px = (const At *)(x + row[u] * a.x.ld + col[u]);
+                vx[u] = STREAM ? __builtin_nontemporal_load(px) : *px;
+                if (res) {
+                    const At *pr = (const At *)(res + row[u] * a.residual.ld + col[u]);
+                    vr[u] = STREAM ? __builtin_nontemporal_load(pr) : *pr;
                 }
             }
         }
+        uint32_t w[U][N / 2] = {};
+        if (drop.below)
+            words_of<T>(drop, q, w);
 #pragma unroll
-        for (int u = 0; u < kGroups; u++) {
-            const long long g = first + u * 256 + threadIdx.x;
-            if (g >= groups)
-                continue;
-            uint32_t w[4] = {0, 0, 0, 0};
-            if (drop.below)
-                drop.group((unsigned long long)g, w);
+        for (int u = 0; u < U; u++) {
             if (whole[u]) {
+                V v;
 #pragma unroll
-                for (int k = 0; k < K; k++) {
-                    V v;
-#pragma unroll
-                    for (int j = 0; j < N; j++)
-                        v[j] = dropped<T>(drop, vx[u][k][j], vr[u][k][j], w[(k * N + j) / 2], j & 1);
-                    __builtin_nontemporal_store(
-                        v, (typename Pack<T>::At *)(y + row[u] * a.y.ld + col[u] + k * N));
-                }
+                for (int j = 0; j < N; j++)
+                    v[j] = dropped<T>(drop, vx[u][j], vr[u][j], w[u][j / 2], j & 1);
+                __builtin_nontemporal_store(v, (At *)(y + row[u] * a.y.ld + col[u]));
                 continue;
             }
-            long long r = row[u], c = col[u];
+            // A pack that the row's end cuts, or the last: element by element, all loads
+            // before the stores.
+            const int left = (int)max(0LL, min((long long)N, n - q[u] * N));
+            long long at_x[N], at_r[N], at_y[N], c = col[u];
+            long long px = row[u] * a.x.ld + c, pr = row[u] * a.residual.ld + c,
+                      py = row[u] * a.y.ld + c;
+            T tx[N], tr[N];
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                if (g * 8 + j >= n)
-                    break;
-                if (!FLAT && c == a.cols) {
+            for (int j = 0; j < N; j++) {
+                at_x[j] = px++;
+                at_r[j] = pr++;
+                at_y[j] = py++;
+                if (!FLAT && ++c == a.cols) {
                     c = 0;
-                    r++;
+                    px += a.x.ld - a.cols;
+                    pr += a.residual.ld - a.cols;
+                    py += a.y.ld - a.cols;
                 }
-                const T xj = x[r * a.x.ld + c];
-                const T rj = res ? res[r * a.residual.ld + c] : (T)0.f;
-                y[r * a.y.ld + c] = dropped<T>(drop, xj, rj, w[j / 2], j & 1);
-                c++;
+                tx[j] = tr[j] = (T)0.f;
+                if (j < left)
+                    tx[j] = x[at_x[j]];
             }
+            if (res)
+#pragma unroll
+                for (int j = 0; j < N; j++)
+                    if (j < left)
+                        tr[j] = res[at_r[j]];
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                if (j < left)
+                    y[at_y[j]] = dropped<T>(drop, tx[j], tr[j], w[u][j / 2], j & 1);
         }
     }
+}
+
+// Loads that leave nothing in the caches, for inputs larger than the last-level one
+// holds beside the rest, of whole cache lines (16384 x 4096 bf16 onto a residual 64.7 us,
+// without 68.8; 16384 x 2048 32.2 and 35.5, without a residual 23.2 and 22.9; 30001 x 2049,
+// lines shared by rows, 85.7 and 78.3).
+bool streams(const DropoutArgs &a, size_t elem)
+{
+    bool lines = a.rows * a.cols * (long long)elem * (a.residual.p ? 2 : 1) > 100LL << 20;
+    for (const Rows &r : {a.x, a.residual})
+        lines = lines && (uintptr_t)r.p % 128 == 0 && (!r.p || r.ld * elem % 128 == 0);
+    return lines;
+}
+
+template <class T, bool FLAT>
+void launch(const DropoutArgs &a, long long packs, bool stream_through, hipStream_t stream)
+{
+    const long long each = 256 * kPacksOf<T>;
+    const int n = (int)std::min((packs + each - 1) / each, kMaxBlocks);
+    if (stream_through)
+        dropout_kernel<T, FLAT, true><<<n, 256, 0, stream>>>(a, packs);
+    else
+        dropout_kernel<T, FLAT, false><<<n, 256, 0, stream>>>(a, packs);
 }
 
 template <class T>
 hipError_t launch(const DropoutArgs &a, hipStream_t stream)
 {
-    const long long groups = (a.rows * a.cols + 7) / 8;
-    if (!groups)
+    const long long packs = (a.rows * a.cols + Pack<T>::N - 1) / Pack<T>::N;
+    if (!packs)
         return hipSuccess;
-    const long long each = 256 * kGroups;
-    const int n = (int)std::min((groups + each - 1) / each, kMaxBlocks);
     const bool flat = a.rows <= 1 || (a.x.ld == a.cols && a.y.ld == a.cols &&
                                       (!a.residual.p || a.residual.ld == a.cols));
+    const bool through = streams(a, sizeof(T));
     if (flat)
-        dropout_kernel<T, true><<<n, 256, 0, stream>>>(a, groups);
+        launch<T, true>(a, packs, through, stream);
     else
-        dropout_kernel<T, false><<<n, 256, 0, stream>>>(a, groups);
+        launch<T, false>(a, packs, through, stream);
     return hipGetLastError();
 }
 

@@ -180,7 +180,7 @@ __device__ __forceinline__ void kept_places(const Dropper &drop, long long e, in
 // A row of a branch in registers (raw, x1) becomes that of total, which is stored.
 template <class T, int NV, bool TAIL>
 __device__ __forceinline__ void add_branch(const ResidualFwdArgs &a, long long row, int t, int tpr,
-                                           typename Pack<T>::V (&raw)[NV], float &x1)
+                                           bool stream, typename Pack<T>::V (&raw)[NV], float &x1)
 {
     constexpr int N = Pack<T>::N;
     const int cols = (int)a.cols, last = NV * N * tpr + t;
@@ -193,8 +193,12 @@ __device__ __forceinline__ void add_branch(const ResidualFwdArgs &a, long long r
     for (int i = 0; i < NV; i++) {
         const int c = (t + i * tpr) * N, left = TAIL ? N : cols - c;
         res[i] = typename Pack<T>::V{};
-        if (left > 0)
-            res[i] = load_places<T>(rr + c, left);
+        if (left > 0) {
+            if (stream)
+                res[i] = load_places<T, true>(rr + c, left);
+            else
+                res[i] = load_places<T>(rr + c, left);
+        }
     }
     const float r1 = TAIL && last < cols ? (float)rr[last] : 0.f;
 #pragma unroll
@@ -309,7 +313,7 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(A a, int tpr, bool stream
         }
         float x1 = TAIL && last < cols ? (float)xr[last] : 0.f;
         if constexpr (BRANCH)
-            add_branch<T, NV, TAIL>(a, row, t, tpr, raw, x1);
+            add_branch<T, NV, TAIL>(a, row, t, tpr, stream, raw, x1);
         float s = x1;
 #pragma unroll
         for (int i = 0; i < NV; i++)
@@ -672,8 +676,12 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(A a, int tpr, bool stream
                 for (int i = 0; i < NP; i++) {
                     const int c = (t + i * tpr) * N;
                     const int left = TAIL ? N : cols - c;
-                    if (left > 0)
-                        np[i] = load_places<T>(dtr + c, left);
+                    if (left > 0) {
+                        if (stream)
+                            np[i] = load_places<T, true>(dtr + c, left);
+                        else
+                            np[i] = load_places<T>(dtr + c, left);
+                    }
                 }
                 if (TAIL && last < cols)
                     np1 = dtr[last];
@@ -1219,7 +1227,9 @@ template <class T, class TW, int NV, bool TAIL, bool HOLD, class A>
 void fwd_rows(const A &a, const RowPlan &p, hipStream_t stream)
 {
     const int n = fwd_blocks(p, a.rows);
-    const bool through = streams(a.rows, a.cols, sizeof(T), {a.x});
+    bool through = streams(a.rows, a.cols, sizeof(T), {a.x});
+    if constexpr (is_branch<A>)
+        through = streams(2 * a.rows, a.cols, sizeof(T), {a.x, a.residual});
     if (p.block <= 256)
         norm_fwd_rows<A, T, TW, NV, TAIL, HOLD, 256><<<n, p.block, 0, stream>>>(a, p.tpr, through);
     else
@@ -1274,7 +1284,9 @@ void bwd_rows(const A &a, const RowPlan &p, int n, hipStream_t stream)
 {
     const size_t lds =
         p.block > p.tpr ? (size_t)p.block * (NV * Pack<T>::N + TAIL) * sizeof(float) : 0;
-    const bool through = streams(a.rows, a.cols, sizeof(T), {a.x, a.dy});
+    bool through = streams(a.rows, a.cols, sizeof(T), {a.x, a.dy});
+    if constexpr (is_branch<A>)
+        through = through && (!a.dtotal.p || streams(a.rows, a.cols, sizeof(T), {a.dtotal}));
     if (p.block <= 256)
         norm_bwd_rows<A, T, TW, NV, TAIL, 256><<<n, p.block, lds, stream>>>(a, p.tpr, through);
     else
