@@ -18,6 +18,7 @@
 #pragma once
 
 #include <algorithm>
+#include <atomic>
 #include <initializer_list>
 #include <type_traits>
 
@@ -154,18 +155,28 @@ template <class A>
 constexpr bool is_branch =
     std::is_same<A, ResidualFwdArgs>::value || std::is_same<A, ResidualBwdArgs>::value;
 
-// Whether the N elements of a pack from element e on are kept, in the order of
-// their places (`left` >= 1 of them are in the row).
-template <int N>
-__device__ __forceinline__ void kept_places(const Dropper &drop, long long e, int left,
-                                            bool (&keep)[N])
+template <class A>
+__device__ __forceinline__ Drop drop_of(const A &a)
 {
+    if constexpr (is_branch<A>)
+        return a.drop;
+    else
+        return Drop{};
+}
+
+// The N elements v of a pack from element e on (in the order of their places, `left` >=
+// 1 of them in the row), dropped out.
+template <int N>
+__device__ __forceinline__ void drop_pack(const Dropper &drop, long long e, int left, float (&v)[N])
+{
+    if (!drop.below)
+        return;
     uint32_t w[N / 2];
     drop.words<N>(e, w);
     if (left >= N) {
 #pragma unroll
         for (int j = 0; j < N; j++)
-            keep[j] = drop.kept(w[j / 2], j & 1);
+            v[j] = drop.kept(w[j / 2], j & 1) ? v[j] * drop.scale : 0.f;
         return;
     }
     unsigned bits = 0;
@@ -174,53 +185,58 @@ __device__ __forceinline__ void kept_places(const Dropper &drop, long long e, in
         bits |= (unsigned)drop.kept(w[j / 2], j & 1) << j;
 #pragma unroll
     for (int j = 0; j < N; j++)
-        keep[j] = bits >> max(0, place<N>(j, left)) & 1;
+        v[j] = bits >> max(0, place<N>(j, left)) & 1 ? v[j] * drop.scale : 0.f;
 }
 
 // A row of a branch in registers (raw, x1) becomes that of total, which is stored.
 template <class T, int NV, bool TAIL>
-__device__ __forceinline__ void add_branch(const ResidualFwdArgs &a, long long row, int t, int tpr,
-                                           bool stream, typename Pack<T>::V (&raw)[NV], float &x1)
+__device__ __forceinline__ void add_branch(const ResidualFwdArgs &a, const Dropper &drop,
+                                           long long row, int t, int tpr, bool stream,
+                                           typename Pack<T>::V (&raw)[NV], float &x1)
 {
     constexpr int N = Pack<T>::N;
     const int cols = (int)a.cols, last = NV * N * tpr + t;
-    const Dropper drop(a.drop);
     const T *rr = (const T *)a.residual.p + row * a.residual.ld;
     T *tr = (T *)a.total.p + row * a.total.ld;
     const long long e = row * a.cols;
-    typename Pack<T>::V res[NV];
-#pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const int c = (t + i * tpr) * N, left = TAIL ? N : cols - c;
-        res[i] = typename Pack<T>::V{};
-        if (left > 0) {
-            if (stream)
-                res[i] = load_places<T, true>(rr + c, left);
-            else
-                res[i] = load_places<T>(rr + c, left);
-        }
-    }
     const float r1 = TAIL && last < cols ? (float)rr[last] : 0.f;
+    // The stream's packs two at a time, for registers (3000 x 20480 fp32 235 us, eight at a
+    // time 263; 9000 x 4096 103 and 106).
+    constexpr int F = NV < 2 ? NV : 2;
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const int c = (t + i * tpr) * N, left = TAIL ? N : cols - c;
-        if (left <= 0)
-            continue;
-        bool keep[N];
+    for (int i0 = 0; i0 < NV; i0 += F) {
+        typename Pack<T>::V res[F];
 #pragma unroll
-        for (int j = 0; j < N; j++)
-            keep[j] = true;
-        if (drop.below)
-            kept_places<N>(drop, e + c, left, keep);
+        for (int i = i0; i < i0 + F && i < NV; i++) {
+            const int c = (t + i * tpr) * N, left = TAIL ? N : cols - c;
+            res[i - i0] = typename Pack<T>::V{};
+            if (left > 0) {
+                if (stream)
+                    res[i - i0] = load_places<T, true>(rr + c, left);
+                else
+                    res[i - i0] = load_places<T>(rr + c, left);
+            }
+        }
 #pragma unroll
-        for (int j = 0; j < N; j++)
-            raw[i][j] = (T)((float)res[i][j] + (keep[j] ? (float)raw[i][j] * drop.scale : 0.f));
-        store_places<T>(tr + c, left, raw[i]);
-        if (left < N)  // no element: 0 in the sums
+        for (int i = i0; i < i0 + F && i < NV; i++) {
+            const int c = (t + i * tpr) * N, left = TAIL ? N : cols - c;
+            if (left <= 0)
+                continue;
+            float v[N];
 #pragma unroll
             for (int j = 0; j < N; j++)
-                if (place<N>(j, left) < 0)
-                    raw[i][j] = (T)0.f;
+                v[j] = (float)raw[i][j];
+            drop_pack<N>(drop, e + c, left, v);
+#pragma unroll
+            for (int j = 0; j < N; j++)
+                raw[i][j] = (T)((float)res[i - i0][j] + v[j]);
+            store_places<T>(tr + c, left, raw[i]);
+            if (left < N)  // no element: 0 in the sums
+#pragma unroll
+                for (int j = 0; j < N; j++)
+                    if (place<N>(j, left) < 0)
+                        raw[i][j] = (T)0.f;
+        }
     }
     if (TAIL && last < cols) {
         const bool keep = !drop.below || drop.one(e + last);
@@ -294,6 +310,7 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(A a, int tpr, bool stream
         load_weights<1>(w, last, cols, 1.f, &w1);
         load_weights<1>(b, last, cols, 0.f, &b1);
     }
+    const Dropper drop(drop_of(a));
     int turn = 0;
     for (long long row = (long long)blockIdx.x * groups + threadIdx.x / tpr; row < a.rows;
          row += (long long)gridDim.x * groups) {
@@ -313,7 +330,7 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_rows(A a, int tpr, bool stream
         }
         float x1 = TAIL && last < cols ? (float)xr[last] : 0.f;
         if constexpr (BRANCH)
-            add_branch<T, NV, TAIL>(a, row, t, tpr, stream, raw, x1);
+            add_branch<T, NV, TAIL>(a, drop, row, t, tpr, stream, raw, x1);
         float s = x1;
 #pragma unroll
         for (int i = 0; i < NV; i++)
@@ -561,8 +578,9 @@ __global__ __launch_bounds__(256) void norm_fwd_apply(NormFwdArgs a, long long p
 // A pack of a branch's gradients (in the order of their places) at column c of a
 // row, and one element of them.
 template <class T>
-__device__ __forceinline__ void store_branch(const ResidualBwdArgs &a, long long row, long long c,
-                                             int left, const float (&g)[Pack<T>::N])
+__device__ __forceinline__ void store_branch(const ResidualBwdArgs &a, const Dropper &drop,
+                                             long long row, long long c, int left,
+                                             const float (&g)[Pack<T>::N])
 {
     constexpr int N = Pack<T>::N;
     typename Pack<T>::V v;
@@ -574,28 +592,25 @@ __device__ __forceinline__ void store_branch(const ResidualBwdArgs &a, long long
     }
     if (!a.dx.p)
         return;
-    const Dropper drop(a.drop);
-    bool keep[N];
+    float d[N];
 #pragma unroll
     for (int j = 0; j < N; j++)
-        keep[j] = true;
-    if (drop.below)
-        kept_places<N>(drop, row * a.cols + c, left, keep);
+        d[j] = g[j];
+    drop_pack<N>(drop, row * a.cols + c, left, d);
 #pragma unroll
     for (int j = 0; j < N; j++)
-        v[j] = (T)(keep[j] ? g[j] * drop.scale : 0.f);
+        v[j] = (T)d[j];
     store_places<T>((T *)a.dx.p + row * a.dx.ld + c, left, v);
 }
 
 template <class T>
-__device__ __forceinline__ void store_branch_one(const ResidualBwdArgs &a, long long row,
-                                                 long long c, float g)
+__device__ __forceinline__ void store_branch_one(const ResidualBwdArgs &a, const Dropper &drop,
+                                                 long long row, long long c, float g)
 {
     if (a.dresidual.p)
         ((T *)a.dresidual.p)[row * a.dresidual.ld + c] = (T)g;
     if (!a.dx.p)
         return;
-    const Dropper drop(a.drop);
     const bool keep = !drop.below || drop.one(row * a.cols + c);
     ((T *)a.dx.p)[row * a.dx.ld + c] = (T)(keep ? g * drop.scale : 0.f);
 }
@@ -695,6 +710,7 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(A a, int tpr, bool stream
         rstdr += step;
     };
     load(row);
+    const Dropper drop(drop_of(a));
     int turn = 0;
     for (; row < a.rows; row += step) {  // one row for the workgroup where it meets at the barrier
 #pragma unroll
@@ -765,10 +781,10 @@ __global__ __launch_bounds__(BLOCK) void norm_bwd_rows(A a, int tpr, bool stream
 #pragma unroll
                 for (int j = 0; j < N; j++)
                     g[j] = back(i * N + j, rd[i][j], rx[i][j]) + (float)rp[i][j];
-                store_branch<T>(a, row, c, left, g);
+                store_branch<T>(a, drop, row, c, left, g);
             }
             if (TAIL && last < cols)
-                store_branch_one<T>(a, row, last, back(NV * N, rd1, rx1) + (float)rp1);
+                store_branch_one<T>(a, drop, row, last, back(NV * N, rd1, rx1) + (float)rp1);
             continue;
         }
 #pragma unroll
@@ -953,6 +969,7 @@ __global__ __launch_bounds__(512) void norm_bwd_cols(A a, int splits, long long 
     const long long end = min((long long)(blockIdx.y + 1) * chunk, a.rows);
     const int left = (int)max(0LL, min((long long)N, a.cols - c));
     const float inv_n = 1.f / (float)a.cols;
+    const Dropper drop(drop_of(a));
     float wv[N], sw[N], sb[N];
     load_weights<N>((const TW *)a.w, c, a.cols, 1.f, wv);
 #pragma unroll
@@ -1027,7 +1044,7 @@ __global__ __launch_bounds__(512) void norm_bwd_cols(A a, int splits, long long 
                 }
                 if constexpr (BRANCH) {
                     if (wanted)
-                        store_branch<T>(a, base + r, c, left, g);
+                        store_branch<T>(a, drop, base + r, c, left, g);
                 } else if (a.dx.p)
                     store_places<T>((T *)a.dx.p + (base + r) * a.dx.ld + c, left, v);
             }
@@ -1154,7 +1171,7 @@ RowPlan row_plan(int xtype, long long rows, long long cols, bool forward)
 
 // Workgroups of the register kernels.  Forward: 1536 threads a CU (16384 rows
 // of 4096 bf16: 49.7 us; with 1024, 2048 and 4096 threads 52.9, 55.1 and 50.4).
-int fwd_blocks(const RowPlan &p, long long rows)
+inline int fwd_blocks(const RowPlan &p, long long rows)
 {
     const long long groups = std::max(1, p.block / p.tpr);
     return (int)std::min((rows + groups - 1) / groups, 1536LL / p.block * num_cus());
@@ -1223,10 +1240,40 @@ int row_chunks(int xtype, long long rows, long long cols)
     return rows <= 64 ? 1 : (int)std::max(1LL, std::min(want, rows / 16));
 }
 
+// Workgroups of the forward kernel for branches: as many as the CUs hold at once, which
+// its registers decide, so that none begins late (16384 x 4096 bf16, 1280 threads a CU:
+// 97 us; with 1024 and 1536 106 and 122. 9000 x 4096 fp32, 1024: 106; with 1280 126.
+// 8192 x 5120 bf16 by workgroups of five waves, three a CU 71, four 100).
+template <auto KERNEL>
+int resident_blocks(const RowPlan &p, long long rows)
+{
+    static std::atomic<int> cache[17];  // a CU's, by waves a workgroup; 0: not asked for yet
+    const int waves = p.block / 64;
+    int per_cu = cache[waves].load(std::memory_order_relaxed);
+    if (!per_cu) {
+        // 512 registers a lane of a SIMD, given to its waves by eights; at most 8 waves.
+        hipFuncAttributes f;
+        int most = 4;
+        if (hipFuncGetAttributes(&f, (const void *)KERNEL) == hipSuccess && f.numRegs > 0)
+            most = std::min(8, std::max(1, 512 / ((f.numRegs + 7) / 8 * 8)));
+        // Workgroups that do not divide among the SIMDs evenly leave room for one less.
+        per_cu = std::max(1, 4 * most / waves - (waves > 4 && waves % 4));
+        cache[waves].store(per_cu, std::memory_order_relaxed);
+    }
+    const long long each = std::max(1, p.block / p.tpr);
+    return (int)std::min((rows + each - 1) / each, (long long)per_cu * num_cus());
+}
+
 template <class T, class TW, int NV, bool TAIL, bool HOLD, class A>
 void fwd_rows(const A &a, const RowPlan &p, hipStream_t stream)
 {
-    const int n = fwd_blocks(p, a.rows);
+    int n = 0;
+    if constexpr (is_branch<A>)
+        n = p.block <= 256
+                ? resident_blocks<norm_fwd_rows<A, T, TW, NV, TAIL, HOLD, 256>>(p, a.rows)
+                : resident_blocks<norm_fwd_rows<A, T, TW, NV, TAIL, HOLD, 1024>>(p, a.rows);
+    else
+        n = fwd_blocks(p, a.rows);
     bool through = streams(a.rows, a.cols, sizeof(T), {a.x});
     if constexpr (is_branch<A>)
         through = streams(2 * a.rows, a.cols, sizeof(T), {a.x, a.residual});
