@@ -1,0 +1,357 @@
+"""Dropout, residual branches and the losses of fine-tuning as programs use them: in one
+training step with the library's other layers, captured and replayed, on several
+streams, into given tensors, at sizes past 32 bits."""
+import math
+
+import pytest
+import torch
+
+import step_ref as ref
+import train_ref
+from test_gpu_train import gen, randn
+from train_ref import U, assert_close, half_ulp
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+# ------------------------------------------------------------ one training step
+def model_inputs(rows, width, vocab, seed):
+    g = gen(rows, width, vocab, seed)
+    return {"x": randn(g, rows, width), "res": randn(g, rows, width),
+            "w": 1 + 0.2 * randn(g, width), "b": 0.1 * randn(g, width),
+            "head": randn(g, vocab, width) / math.sqrt(width), "bias": 0.1 * randn(g, vocab),
+            "targets": torch.randint(vocab, (rows,), generator=g)}
+
+
+NUM = dict(p=0.2, seed=2 ** 40 + 5, layer=4)
+
+
+def forward(m, t, step):
+    """A branch's end, the vocabulary's inner product, the log probabilities."""
+    rows, width = t["x"].shape
+    n = m.residual_norm_fwd(t["x"], t["res"], t["w"], t["b"], **NUM, step=step)
+    z = m.conv_fwd(n.y.view(rows, width, 1, 1), t["head"].view(-1, width, 1, 1), t["bias"])
+    z = z.view(rows, -1)
+    return n, z, m.logprob_fwd(z, t["targets"])
+
+
+def backward(m, t, step, n, z, out, dlogp, dentropy=None):
+    """The gradients of all inputs and weights, clipped."""
+    rows, width = t["x"].shape
+    dz = m.logprob_bwd(z, out.stats, t["targets"], dlogp, out.entropy, dentropy)
+    d = dz.view(rows, -1, 1, 1)
+    dhead, dbias = m.conv_bwd_weight(n.y.view(rows, width, 1, 1), d, (1, 1))
+    dy = m.conv_bwd_data(d, t["head"].view(-1, width, 1, 1), (1, 1)).view(rows, width)
+    dx, dres, dw, db = m.residual_norm_bwd(dy, n.total, n.mean, n.rstd, t["w"], **NUM, step=step)
+    grads = {"x": dx, "res": dres, "w": dw, "b": db, "head": dhead.view(-1, width), "bias": dbias}
+    norm = m.grad_clip([grads[k] for k in grads], 1e9)
+    return grads, norm
+
+
+def forward64(t, step):
+    """The same in 64 bits on the CPU, with a history."""
+    rows, width = t["x"].shape
+    t = {k: v.double().requires_grad_() if v.is_floating_point() else v for k, v in t.items()}
+    keep = ref.mask_of(rows, width, NUM["p"], NUM["seed"], NUM["layer"], step)
+    total = t["res"] + torch.where(keep, t["x"] * ref.scale_of(NUM["p"]), torch.zeros(()).double())
+    y = torch.nn.functional.layer_norm(total, (width,), t["w"], t["b"], 1e-5)
+    lp = torch.log_softmax(y @ t["head"].t() + t["bias"], 1)
+    logp = lp.gather(1, t["targets"][:, None])[:, 0]
+    return t, logp, -(lp.exp() * lp).sum(1)
+
+
+def check_step(grads, norm, t, loss):
+    """Against autograd.  The convolution kernels' inner products are within 1e-4 of their
+    magnitudes' sums, which here are below some 30 times the results' scale."""
+    loss.backward()
+    total = math.sqrt(sum(float((t[k].grad ** 2).sum()) for k in grads))
+    assert abs(float(norm) - total) < 1e-3 * total
+    for k, g in grads.items():
+        want = t[k].grad
+        scale = float(want.abs().max())
+        assert_close(g, want, 2e-3 * scale, k)
+
+
+def test_a_step_of_a_policy():
+    import paper_1903_06934_amd as m
+    rows, seqs, step = 300, 6, 17
+    t = model_inputs(rows, 96, 70, 1)
+    g = gen(2)
+    starts = torch.tensor([0, 40, 41, 130, 130, 250, 290])
+    mask = torch.rand(rows, generator=g) > 0.2
+    adv = randn(g, seqs)
+    ht, logp, entropy = forward64(t, step)
+    old = (logp + 0.2 * randn(g, rows)).detach().float()
+    reference = (logp + 0.3 * randn(g, rows)).detach().float()
+
+    d = {k: v.cuda() for k, v in t.items()}
+    n, z, out = forward(m, d, step)
+    assert_close(out.logp, logp.detach(), 1e-3, "logp")
+    loss = m.policy_loss(out.logp, old.cuda(), adv.cuda(), by_sequence=True,
+                         ref_logp=reference.cuda(), entropy=out.entropy, mask=mask.cuda(),
+                         starts=starts.cuda(), kl_weight=0.1, entropy_weight=0.05,
+                         mean="sequences")
+    grads, norm = backward(m, d, step, n, z, out, loss.dlogp, loss.dentropy)
+
+    ratio = torch.exp(logp - old)
+    want = 0.0
+    some = [i for i in range(seqs) if mask[starts[i]:starts[i + 1]].any()]
+    for i in some:
+        at = torch.nonzero(mask[starts[i]:starts[i + 1]])[:, 0] + starts[i]
+        a, r = adv[i].double(), ratio[at]
+        each = -torch.minimum(r * a, r.clamp(0.8, 1.2) * a)
+        x = reference[at].double() - logp[at]
+        each = each + 0.1 * (torch.exp(x) - 1 - x) - 0.05 * entropy[at]
+        want = want + each.mean() / len(some)
+    assert abs(float(loss.loss) - float(want.detach())) < 1e-3
+    check_step(grads, norm, ht, want)
+
+
+def test_a_step_of_preferences():
+    import paper_1903_06934_amd as m
+    rows, pairs, step = 260, 3, 3
+    t = model_inputs(rows, 130, 50, 2)
+    starts = torch.tensor([0, 40, 100, 120, 180, 181, 250])
+    mask = torch.rand(rows, generator=gen(3)) > 0.3
+    ht, logp, _ = forward64(t, step)
+    reference = (logp + 0.05 * randn(gen(4), rows)).detach().float()
+
+    d = {k: v.cuda() for k, v in t.items()}
+    n, z, out = forward(m, d, step)
+    loss = m.preference_loss(out.logp, reference.cuda(), starts.cuda(), 0.5, smoothing=0.1,
+                             mask=mask.cuda())
+    grads, norm = backward(m, d, step, n, z, out, loss.dlogp)
+
+    v = torch.where(mask, logp - reference, torch.zeros(()).double())
+    r = torch.stack([0.5 * v[starts[s]:starts[s + 1]].sum() for s in range(2 * pairs)])
+    x = r[:pairs] - r[pairs:]
+    ls = torch.nn.functional.logsigmoid
+    want = -(0.9 * ls(x) + 0.1 * ls(-x)).mean()
+    assert abs(float(loss.loss) - float(want.detach())) < 1e-3
+    check_step(grads, norm, ht, want)
+
+
+# ------------------------------------------------------------- graphs, streams
+def small_step(m, d, step, ws):
+    """All the operators of a step, into new tensors."""
+    n = m.residual_norm_fwd(d["x"], d["res"], d["w"], p=0.3, seed=5, layer=1, step=step,
+                            ws=ws["fwd"])
+    y = m.dropout_fwd(n.y, 0.5, 5, 2, step)
+    dy = m.dropout_bwd(y, 0.5, 5, 2, step)
+    back = m.residual_norm_bwd(dy, n.total, n.mean, n.rstd, d["w"], d["res"], p=0.3, seed=5,
+                               layer=1, step=step, ws=ws["bwd"])
+    pol = m.policy_loss(d["lp"], d["old"], d["adv"], by_sequence=True, ref_logp=d["ref"],
+                        mask=d["mask"], starts=d["starts"], kl_weight=0.1, mean="sequences",
+                        ws=ws["policy"])
+    pref = m.preference_loss(d["lp"], d["ref"], d["starts"], 0.1, mask=d["mask"], ws=ws["pref"])
+    return [*n, y, dy, *back, pol.stats, pol.dlogp, *pref]
+
+
+def small_inputs(m, rows, cols, tokens, xt, seed=0):
+    g = gen(rows, cols, tokens, seed)
+    lp = -randn(g, tokens).abs()
+    cuts = torch.sort(torch.randint(tokens + 1, (19,), generator=g))[0]
+    d = {"x": randn(g, rows, cols).to(xt), "res": randn(g, rows, cols).to(xt),
+         "w": randn(g, cols), "lp": lp, "old": lp + 0.1 * randn(g, tokens),
+         "ref": lp + 0.1 * randn(g, tokens), "adv": randn(g, 18),
+         "mask": torch.rand(tokens, generator=g) > 0.2, "starts": cuts}
+    d = {k: v.cuda() for k, v in d.items()}
+    ws = {"fwd": m.residual_norm_workspace(False, d["x"]),
+          "bwd": m.residual_norm_workspace(True, d["x"]),
+          "policy": m.policy_workspace(d["lp"], d["starts"]),
+          "pref": m.preference_workspace(d["lp"], d["starts"])}
+    return d, ws
+
+
+@pytest.mark.parametrize("rows,cols,tokens,xt", [(60, 520, 900, BF16), (300, 4099, 30000, F32),
+                                                 (3, 40000, 12345, BF16)])
+def test_replayed_in_graphs(rows, cols, tokens, xt):
+    """Two graphs that share workspaces, replayed in turn with eager work between them;
+    every replay is what an eager call gives on the inputs and at the step it finds."""
+    import paper_1903_06934_amd as m
+    d, ws = small_inputs(m, rows, cols, tokens, xt)
+    fresh = [small_inputs(m, rows, cols, tokens, xt, s)[0] for s in range(1, 4)]
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    small_step(m, d, step, ws)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for _ in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(small_step(m, d, step, ws))
+            step.add_(1)
+    step.zero_()
+    for i, new in enumerate(fresh):
+        for k in d:
+            d[k].copy_(new[k])
+        torch.cuda.synchronize()
+        for graph, out in zip(graphs, outs):
+            now = int(step)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert int(step) == now + 1
+            none = {k: None for k in ws}
+            for a, b in zip(out, small_step(m, d, now, none)):
+                assert torch.equal(a, b), i
+    # Another step has another mask.
+    a = m.dropout_fwd(d["x"], 0.5, 5, 2, step)
+    assert not torch.equal(a, m.dropout_fwd(d["x"], 0.5, 5, 2, step + 1))
+
+
+def test_on_two_streams():
+    """Two steps at once on streams of their own, with workspaces of their own."""
+    import paper_1903_06934_amd as m
+    sets = [small_inputs(m, 500, 4096, 50000, BF16, s) for s in (1, 2)]
+    want = [small_step(m, d, 7, ws) for d, ws in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(5):
+        got = []
+        for (d, ws), s in zip(sets, streams):
+            with torch.cuda.stream(s):
+                got.append(small_step(m, d, 7, ws))
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_given_tensors_count_as_changed():
+    import paper_1903_06934_amd as m
+    d, _ = small_inputs(m, 8, 64, 100, F32)
+    new = lambda *s: torch.empty(s, device="cuda")
+    y, total, dx, dres = new(8, 64), new(8, 64), new(8, 64), new(8, 64)
+    mean, rstd, dw, db = new(8), new(8), new(64), new(64)
+    stats, dlogp, dent, pstats, rewards = new(6), new(100), new(100), new(5), new(18)
+    out = m.residual_norm_fwd(d["x"], d["res"], d["w"], total=total, y=y, mean=mean, rstd=rstd)
+    assert out.total is total and out.y is y and out.mean is mean and out.rstd is rstd
+    back = m.residual_norm_bwd(y, total, mean, rstd, d["w"], p=0.5, seed=1, dx=dx, dresidual=dres,
+                               dw=dw, db=db)
+    assert back[0] is dx and back[1] is dres and back[2] is dw and back[3] is db
+    r = m.policy_loss(d["lp"], d["old"], d["lp"], entropy=d["ref"], stats=stats, dlogp=dlogp,
+                      dentropy=dent)
+    assert r.stats is stats and r.dlogp is dlogp and r.dentropy is dent
+    r = m.preference_loss(d["lp"], None, d["starts"], 0.1, stats=pstats, rewards=rewards)
+    assert r.stats is pstats and r.rewards is rewards
+    for t in (y, total, dx, dres, mean, rstd, dw, db, stats, dlogp, dent, pstats, rewards):
+        assert t._version == 1
+    m.dropout_fwd(d["x"], 0.5, 1, y=y)
+    m.dropout_bwd(y, 0.5, 1, dx=y)
+    assert y._version == 3
+    x = torch.ones(4, 64, device="cuda", requires_grad=True)
+    assert m.dropout_fwd(x, 0.5, 1).grad_fn is None
+
+
+# ----------------------------------------------------------------- large sizes
+def test_dropout_past_32_bits():
+    """Element indices past 2^32 and, where their groups' numbers are too, past 2^35."""
+    import paper_1903_06934_amd as m
+    for rows, cols, shift in ((9, (1 << 29) - 1, 0), (66, (1 << 29) - 3, 0)):
+        n = rows * cols
+        x = torch.ones(n, dtype=F16, device="cuda")
+        m.dropout_fwd(x.view(rows, cols), 0.25, 11, 3, 4, y=x.view(rows, cols))
+        for first in (0, (1 << 32) - 64, cols * 8 - 30, (1 << 35) - 100, n - 1000):
+            if first + 1000 > n:
+                first = n - 1000
+            keep = ref.kept(range(first, first + 1000), 0.25, 11, 3, 4)
+            got = x[first:first + 1000].cpu()
+            assert torch.equal(got != 0, keep), first
+            assert bool((got[keep] == torch.tensor(ref.scale_of(0.25)).half()).all())
+        del x
+        torch.cuda.empty_cache()
+
+
+def test_strided_dropout_past_32_bits():
+    """Rows whose beginnings in memory, and whose elements' indices, are past 2^32."""
+    import paper_1903_06934_amd as m
+    rows, cols, ld = 1_100_003, 4001, 4104
+    wide = torch.zeros(rows * ld, dtype=BF16, device="cuda")
+    x = wide.view(rows, ld)[:, 5:5 + cols]
+    x.fill_(1.0)
+    y = m.dropout_fwd(x, 0.5, 12, y=x)
+    for r in (0, 1, 1_046_528, 1_073_474, rows - 1):
+        keep = ref.kept(range(r * cols, (r + 1) * cols), 0.5, 12)
+        assert torch.equal(y[r].cpu() != 0, keep), r
+    assert not wide.view(rows, ld)[:, :5].any() and not wide.view(rows, ld)[:, 5 + cols:].any()
+
+
+def test_residual_norm_past_32_bits():
+    import paper_1903_06934_amd as m
+    rows, cols = 1_050_003, 4104
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(rows, cols, generator=g, device="cuda", dtype=BF16)
+    res = torch.randn(rows, cols, generator=g, device="cuda", dtype=BF16)
+    out = m.residual_norm_fwd(x, res, p=0.5, seed=3)
+    dx, dr, dw, db = m.residual_norm_bwd(x, out.total, out.mean, out.rstd, dtotal=res, p=0.5, seed=3)
+    for r in (0, 523_266, 1_046_529, rows - 1):
+        keep = ref.kept(range(r * cols, (r + 1) * cols), 0.5, 3)[None]
+        xr, sr = x[r:r + 1].cpu(), res[r:r + 1].cpu()
+        want, size = ref.dropout(xr, keep, 0.5, sr)
+        assert_close(out.total[r:r + 1], want, U * size + half_ulp(want, BF16) * 1.01, "total")
+        total = out.total[r:r + 1].cpu()
+        ry, _, _, nsize, _ = train_ref.layernorm_fwd(total)
+        assert_close(out.y[r:r + 1], ry, 110 * U * nsize + half_ulp(ry, BF16) * 1.01, "y")
+        (dn, nsize), _, _ = train_ref.layernorm_bwd(xr, total, out.mean[r:r + 1].cpu(),
+                                                    out.rstd[r:r + 1].cpu())
+        rg = dn + sr.double()
+        off = 55 * U * nsize + U * rg.abs()
+        assert_close(dr[r:r + 1], rg, off + half_ulp(rg, BF16) * 1.01, "dresidual")
+        rx, _ = ref.dropout(rg, keep, 0.5)
+        assert_close(dx[r:r + 1], rx, 2 * off + 2 * U * rx.abs() + half_ulp(rx, BF16) * 1.01, "dx")
+
+
+def test_losses_of_as_many_tokens_as_there_can_be():
+    """2^31 - 1 tokens, a long sequence, empty ones and a short one at the end."""
+    import paper_1903_06934_amd as m
+    n = (1 << 31) - 1
+    starts = torch.tensor([3, n - 700, n - 700, n - 700, n - 5], device="cuda")
+    lp = torch.zeros(n, device="cuda")
+    mask = torch.ones(n, dtype=torch.bool, device="cuda")
+    mask[:1000] = False
+    count = [n - 700 - 1000, 695]
+    r = m.policy_loss(lp, lp, torch.tensor([2.0, 7.0, 7.0, -3.0], device="cuda"),
+                      by_sequence=True, mask=mask, starts=starts, mean="sequences")
+    # Every ratio is 1: a sequence's mean surrogate is its advantage, its tokens' slope that
+    # over their number.
+    assert r.stats.tolist() == [0.5, 0.5, 0.0, 0.0, 1.0, 0.0]
+    for i, want in ((999, 0.0), (1000, -1.0 / count[0]), (n - 701, -1.0 / count[0]),
+                    (n - 700, 1.5 / count[1]), (n - 6, 1.5 / count[1]), (n - 5, 0.0), (n - 1, 0.0)):
+        assert abs(float(r.dlogp[i]) - want) <= 4 * U * abs(want), i
+    lp.fill_(2.0 ** -20)
+    q = m.preference_loss(lp, None, starts, 0.25, mask=mask, length_mean=False, dlogp=r.dlogp)
+    # Pair 0: sequences 0 and 2 (empty), pair 1: 1 (empty) and 3.
+    want = torch.tensor([count[0], 0, 0, count[1]], dtype=torch.float64) * 2.0 ** -22
+    assert_close(q.rewards, want, 2 * U * want, "rewards")
+    for i, gap, sign, k in ((1000, want[0], -1, 0), (n - 701, want[0], -1, 0),
+                            (n - 700, -want[3], 1, 1), (n - 6, -want[3], 1, 1)):
+        slope = sign * 0.25 / (1 + math.exp(gap)) / 2
+        # Pair 0's slope is exp(-512): half of the smallest number of 32 bits is what
+        # rounding it to them may cost.
+        assert abs(float(r.dlogp[i]) - slope) <= 1e-6 * abs(slope) + 2.0 ** -150, i
+    assert r.dlogp[n - 5:].abs().max() == 0 and r.dlogp[:1000].abs().max() == 0
+
+
+def test_many_sequences():
+    """A million sequences: more than the chunks look at one by one."""
+    import paper_1903_06934_amd as m
+    n, seqs = 3_000_017, 1_000_000
+    g = torch.Generator(device="cuda").manual_seed(2)
+    starts = torch.sort(torch.randint(n + 1, (seqs + 1,), generator=g, device="cuda"))[0]
+    lp = -torch.rand(n, generator=g, device="cuda")
+    adv = torch.randn(seqs, generator=g, device="cuda")
+    r = m.policy_loss(lp, lp, adv, by_sequence=True, starts=starts, mean="sequences")
+    length = (starts[1:] - starts[:-1]).double()
+    some = length > 0
+    want = -(adv.double() * some).sum() / some.sum()
+    # Sums of single products and weights, each rounded once or twice, in 64 bits.
+    assert abs(float(r.loss) - float(want)) < 4 * U * float(adv.abs().double().mean())
+    seq = torch.searchsorted(starts[1:], torch.arange(n, device="cuda"), right=True)
+    inside = (seq < seqs) & (torch.arange(n, device="cuda") >= starts[0])
+    seq = seq.clamp(max=seqs - 1)
+    g64 = torch.where(inside, -adv.double()[seq] / length[seq] / some.sum(), 0.0)
+    assert bool(((r.dlogp.double() - g64).abs() <= 5 * U * g64.abs()).all())
+    q = m.preference_loss(lp, None, starts, 0.5)
+    total = torch.cat([torch.zeros(1, device="cuda").double(), torch.cumsum(lp.double(), 0)])
+    rew = 0.5 * (total[starts[1:]] - total[starts[:-1]])
+    assert bool(((q.rewards.double() - rew).abs() <= 2 * U * rew.abs() + 1e-9).all())
