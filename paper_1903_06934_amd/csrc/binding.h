@@ -133,14 +133,17 @@ inline void written(const Maybe &m)
         written(*m);
 }
 
-// Small float results side by side in one buffer: its allocation takes the host
-// longer than the views.  Only floats: tensors of several types in one storage
-// cannot be saved together.
+// Small results of one type (floats, if it is not said) side by side in one buffer: its
+// allocation takes the host longer than the views.  Only of one type: tensors of several
+// types in one storage cannot be saved together.
 struct Results {
     Tensor floats;
     int64_t used = 0;
 
-    Results(int64_t n, const Tensor &x) : floats(empty({n}, x, at::kFloat)) {}
+    Results(int64_t n, const Tensor &x, at::ScalarType type = at::kFloat)
+        : floats(empty({n}, x, type))
+    {
+    }
 
     Tensor next(at::IntArrayRef sizes)
     {

@@ -83,6 +83,10 @@ Tensor dropout_backward(const Tensor &dy, double p, uint64_t seed, uint32_t laye
 }
 
 // ------------------------------------------------------------ residual branches
+// Of so many bytes each, two results share an allocation (four rows of 2048 16-bit
+// elements: 16 KiB).  Larger ones do not: one would keep the other's memory.
+constexpr size_t kSmall = 64 << 10;
+
 Maybe norm_workspace(bool backward, const Tensor &x)
 {
     Rows r;
@@ -101,8 +105,15 @@ norm_forward(const Tensor &x, const Tensor &residual, const Maybe &w, const Mayb
     const int64_t ldr = like(residual, "residual", x, r);
     const at::ScalarType wt = w ? w->scalar_type() : b ? b->scalar_type() : x.scalar_type();
     const void *wp = vector(w, "w", r.cols, wt), *bp = vector(b, "b", r.cols, wt);
-    const Tensor total = total_ ? *total_ : empty(x.sizes(), x, x.scalar_type());
-    const Tensor y = y_ ? *y_ : empty(x.sizes(), x, x.scalar_type());
+    Tensor total, y;
+    if (!total_ && !y_ && x.nbytes() <= kSmall) {
+        Results out(2 * x.numel(), x, x.scalar_type());
+        total = out.next(x.sizes());
+        y = out.next(x.sizes());
+    } else {
+        total = total_ ? *total_ : empty(x.sizes(), x, x.scalar_type());
+        y = y_ ? *y_ : empty(x.sizes(), x, x.scalar_type());
+    }
     const int64_t ldt = like(total, "total", x, r), ldy = like(y, "y", x, r);
     Tensor mean, rstd;
     if (mean_ && rstd_) {
@@ -122,8 +133,8 @@ norm_forward(const Tensor &x, const Tensor &residual, const Maybe &w, const Mayb
                            vector<float>(rstd, "rstd", r.rows, at::kFloat), s.p, s.bytes,
                            stream()),
          "residual_norm_fwd");
-    for (const Tensor *t : {&total, &y, (const Tensor *)&mean, (const Tensor *)&rstd})
-        written(*t);
+    for (const Tensor &t : {total, y, mean, rstd})
+        written(t);
     return {total, y, mean, rstd};
 }
 

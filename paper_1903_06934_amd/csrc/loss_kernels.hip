@@ -89,13 +89,16 @@ __device__ __forceinline__ void block_sums(V (&v)[N], V (*lds)[N])
     }
 }
 
-// The sums of N values over a workgroup, each to one thread's f(i, sum).
+// The sums of N values over a workgroup, each to one thread's f(i, sum).  some: whether
+// the thread's may be other than 0.
 template <int BLOCK, int N, class V, class F>
-__device__ __forceinline__ void block_totals(V (&v)[N], V (*lds)[N], F f)
+__device__ __forceinline__ void block_totals(V (&v)[N], V (*lds)[N], F f, bool some = true)
 {
+    const bool any = __ballot(some) != 0;
 #pragma unroll
     for (int i = 0; i < N; i++) {
-        v[i] = wave_sum(v[i]);
+        if (any)
+            v[i] = wave_sum(v[i]);
         if ((threadIdx.x & 63) == 0)
             lds[threadIdx.x >> 6][i] = v[i];
     }
@@ -744,7 +747,7 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
     __shared__ Marks<SEQS ? kOneBlock : 64, PACKS> marks;
     __shared__ CountTable<SEQS ? kOneBlock : 64, PACKS> table;
     __shared__ OfSequence seq[SEQS ? kOneChunk : 1];
-    __shared__ double red[WAVES][5];
+    __shared__ double red[WAVES][5], total[5];
     __shared__ int counts[WAVES][1];
     const Starts starts{a.starts, a.tokens};
     const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
@@ -764,6 +767,7 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
 #pragma unroll
     for (int h = 0; h < PACKS; h++)
         n[0] += __popc(m[h].mask & inside(m[h], from, to));
+    const bool counted = n[0] > 0;
     double u = 1.0 / a.count;
     if constexpr (SEQS) {
         marks.clear();
@@ -795,14 +799,10 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
     for (int h = 0; h < PACKS; h++)
         token_losses<SEQS, REF>(a, borders, m[h], k[h], m[h].mask & inside(m[h], from, to), w[h],
                                 (float)(u * a.scale), sum);
-    block_sums<kOneBlock>(sum, red);
-#pragma unroll
-    for (int i = 0; i < 5; i++)
-        sum[i] *= u;
-    if (threadIdx.x == 0)
-#pragma unroll
-        for (int i = 0; i < 6; i++)
-            a.stats[i] = policy_result(a, sum, i);
+    block_totals<kOneBlock>(sum, red, [&](int i, double v) { total[i] = v * u; }, counted);
+    // The same wave has written them.
+    if (threadIdx.x < 6)
+        a.stats[threadIdx.x] = policy_result(a, total, (int)threadIdx.x);
 }
 
 template <bool SEQS, Ref REF>
@@ -1196,6 +1196,7 @@ __global__ __launch_bounds__(kOneBlock) void preference_one(PreferenceArgs a)
     __shared__ Sums<kOneBlock, PACKS> sums;
     __shared__ double seq[kOneChunk];
     __shared__ double red[kOneBlock / 64][6];
+    __shared__ int counts[kOneBlock / 64];
     const Starts starts{a.starts, a.tokens};
     Mine m[PACKS];
     float v[PACKS][kEach];
@@ -1245,12 +1246,20 @@ __global__ __launch_bounds__(kOneBlock) void preference_one(PreferenceArgs a)
             sum[5] = 1;
         }
     }
-    block_sums<kOneBlock>(sum, red);
-    const double u = 1.0 / max(sum[5], 1.0);
-    if (threadIdx.x == 0)
+    // How many pairs have a token.
+    const int given = __popcll(__ballot(sum[5] > 0));
+    if ((threadIdx.x & 63) == 0)
+        counts[threadIdx.x >> 6] = given;
+    __syncthreads();
+    int all = 0;
 #pragma unroll
-        for (int k = 0; k < 5; k++)
-            a.stats[k] = (float)(sum[k] * u);
+    for (int w = 0; w < kOneBlock / 64; w++)
+        all += counts[w];
+    const double u = 1.0 / max(all, 1);
+    block_totals<kOneBlock>(sum, red, [&](int k, double v) {
+        if (k < 5)
+            a.stats[k] = (float)(v * u);
+    }, has);
     if (!a.dlogp)
         return;
 #pragma unroll
