@@ -182,22 +182,23 @@ struct Search {
 };
 
 // The sequences that have tokens in the chunk begin <= t < end, for all threads of a
-// workgroup to go through.  Up to kDirect sequences each thread looks at its share of all
-// of them; more are searched for the chunk's first and last.  The first kLook of a
-// thread's share are loaded at once, and before the chunk's tokens, so that these
-// latencies overlap.
-constexpr int kLook = 4, kDirect = 8 * kBlock;
+// workgroup to go through.  Each thread looks at LOOK of them, loaded at once and before
+// the chunk's tokens, so that these latencies overlap; if there are more, they are
+// searched for the chunk's first and last before (2 000 003 tokens: 1024 pairs with LOOK 8
+// 21.3 us, with 4 and a search 23.0; 1024 sequences of a policy 26.2 and 24.6, as 8 take
+// the registers of a fourth workgroup a CU).
+constexpr int kPolicyLook = 4, kPairsLook = 8;
 
-template <int BLOCK>
+template <int BLOCK, int LOOK>
 struct Sequences {
     Starts starts;
     int begin, end, first, last;
-    int s0[kLook], s1[kLook];
+    int s0[LOOK], s1[LOOK];
 
     __device__ __forceinline__ Sequences(const Starts &st, int seqs, int begin_, int end_)
         : starts(st), begin(begin_), end(end_), first(0), last(seqs)
     {
-        if (seqs > kDirect) {
+        if (seqs > LOOK * BLOCK) {
             Search a{starts.p + 1, begin, 0, seqs}, b{starts.p, (long long)end - 1, 0, seqs};
             while (a.open() || b.open()) {
                 const bool pa = a.open() && a.probe(), pb = b.open() && b.probe();
@@ -218,7 +219,7 @@ struct Sequences {
         // there are sequences), so that no load waits behind a branch.
         const long long most = max(last - 1, 0);
 #pragma unroll
-        for (int i = 0; i < kLook; i++)
+        for (int i = 0; i < LOOK; i++)
             if (last > 0)
                 starts.of(min(at + i * BLOCK, most), s0[i], s1[i]);
     }
@@ -228,9 +229,9 @@ struct Sequences {
     {
         long long at = (long long)first + threadIdx.x;
         visit(at, f);
-        if (last - first <= kLook * BLOCK)
+        if (last - first <= LOOK * BLOCK)
             return;
-        for (at += kLook * BLOCK; at < last; at += kLook * BLOCK) {
+        for (at += LOOK * BLOCK; at < last; at += LOOK * BLOCK) {
             look(at);
             visit(at, f);
         }
@@ -240,7 +241,7 @@ struct Sequences {
     __device__ __forceinline__ void visit(long long at, F f)
     {
 #pragma unroll
-        for (int i = 0; i < kLook; i++)
+        for (int i = 0; i < LOOK; i++)
             if (at + i * BLOCK < last && s0[i] < s1[i] && s0[i] < end && s1[i] > begin)
                 f(at + i * BLOCK, s0[i], s1[i]);
     }
@@ -484,7 +485,7 @@ __global__ __launch_bounds__(kBlock) void policy_count(PolicyArgs a, Counts c, i
         const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
         Mine m[kPacks];
         if (a.mean == 1) {
-            Sequences<kBlock> q(starts, a.seqs, begin, end);
+            Sequences<kBlock, kPolicyLook> q(starts, a.seqs, begin, end);
 #pragma unroll
             for (int h = 0; h < kPacks; h++) {
                 m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
@@ -751,7 +752,7 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
     __shared__ int counts[WAVES][1];
     const Starts starts{a.starts, a.tokens};
     const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
-    Sequences<kOneBlock> q(starts, SEQS ? a.seqs : 0, 0, a.tokens);
+    Sequences<kOneBlock, kPolicyLook> q(starts, SEQS ? a.seqs : 0, 0, a.tokens);
     Mine m[PACKS];
     Tokens k[PACKS];
     float w[PACKS][kEach];
@@ -825,7 +826,7 @@ __global__ __launch_bounds__(kBlock, 4) void policy_main(PolicyArgs a, Counts c,
     }
     for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
         const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
-        Sequences<kBlock> q(starts, SEQS ? a.seqs : 0, begin, end);
+        Sequences<kBlock, kPolicyLook> q(starts, SEQS ? a.seqs : 0, begin, end);
         Mine m[kPacks];
         Tokens tokens[kPacks];
         float w[kPacks][kEach];
@@ -1049,7 +1050,7 @@ __global__ __launch_bounds__(kBlock) void preference_sums(PreferenceArgs a, Pair
     const Starts starts{a.starts, a.tokens};
     for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
         const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
-        Sequences<kBlock> q(starts, 2 * a.pairs, begin, end);
+        Sequences<kBlock, kPairsLook> q(starts, 2 * a.pairs, begin, end);
         float v[kPacks][kEach];
 #pragma unroll
         for (int h = 0; h < kPacks; h++) {
@@ -1166,7 +1167,7 @@ __global__ __launch_bounds__(kBlock) void preference_fill(PreferenceArgs a, Pair
     const int from = starts(0), to = starts(2LL * a.pairs);
     for (int k = blockIdx.x; k < chunks; k += groups) {
         const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
-        Sequences<kBlock> q(starts, 2 * a.pairs, begin, end);
+        Sequences<kBlock, kPairsLook> q(starts, 2 * a.pairs, begin, end);
         Mine m[kPacks];
 #pragma unroll
         for (int h = 0; h < kPacks; h++)
