@@ -127,8 +127,9 @@ int residual_norm_bwd(int xtype, int wtype, long long rows, long long cols, cons
  * by_sequence nor MISTEP_MEAN_SEQUENCES is allowed (MICONV_ERR_NULL).  ref_logp
  * may be NULL if kl_weight is 0, entropy if entropy_weight is and dentropy is NULL.
  * MICONV_ERR_VALUE: clip_low outside [0, 1], clip_high below 0, dual_clip below 1
- * (infinite ones do not clip), weights that are not finite, count not above 0 or
- * not finite (read for its mean only), a form or mean that is not listed.
+ * (infinite ones do not clip), weights that are not finite, a form or mean that is not
+ * listed; for MISTEP_MEAN_COUNT, which alone reads it, a count that is not above 0 and
+ * finite, or whose 1 / count or scale / count is beyond 32 bits.
  */
 #define MISTEP_KL_LINEAR 0
 #define MISTEP_KL_SQUARE 1

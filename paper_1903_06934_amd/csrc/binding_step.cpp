@@ -42,10 +42,16 @@ struct Numbers {
 
     Numbers(uint64_t seed_, uint32_t layer_, const py::object &s) : seed(seed_), layer(layer_)
     {
-        if (THPVariable_Check(s.ptr()))
+        if (THPVariable_Check(s.ptr())) {
             step_at = vector<long long>(THPVariable_Unpack(s.ptr()), "step", 1, at::kLong);
-        else
-            step = (unsigned)py::cast<uint64_t>(s);
+        } else {
+            if (!PyIndex_Check(s.ptr()))
+                refuse("step", " must be a whole number, or a device tensor of one");
+            const auto n = py::reinterpret_steal<py::object>(PyNumber_Index(s.ptr()));
+            if (!n)
+                throw py::error_already_set();
+            step = (unsigned)PyLong_AsUnsignedLongLongMask(n.ptr());  // modulo 2^32
+        }
     }
 };
 

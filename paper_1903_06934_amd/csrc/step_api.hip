@@ -190,7 +190,9 @@ int policy_loss(long long tokens, long long seqs, const float *logp, const float
     if (!(clip_low >= 0 && clip_low <= 1) || !(clip_high >= 0) || !(dual_clip >= 1) ||
         kl < MISTEP_KL_LINEAR || kl > MISTEP_KL_LOW || !in_floats(kl_weight) ||
         !in_floats(entropy_weight) || mean < MISTEP_MEAN_TOKENS || mean > MISTEP_MEAN_COUNT ||
-        (mean == MISTEP_MEAN_COUNT && !(count > 0 && isfinite(count))) || !in_floats(scale))
+        (mean == MISTEP_MEAN_COUNT &&
+         !(count > 0 && isfinite(count) && in_floats(1 / count) && in_floats(scale / count))) ||
+        !in_floats(scale))
         return MICONV_ERR_VALUE;
     if (!starts && (by_sequence || mean == MISTEP_MEAN_SEQUENCES))
         return MICONV_ERR_NULL;

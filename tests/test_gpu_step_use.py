@@ -243,6 +243,94 @@ def test_given_tensors_count_as_changed():
     assert m.dropout_fwd(x, 0.5, 1).grad_fn is None
 
 
+def test_first_call_in_a_graph():
+    """A shape that no call had before is captured at its first."""
+    import paper_1903_06934_amd as m
+    x = torch.randn(77, 330, device="cuda", dtype=F16)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = m.residual_norm_fwd(x, x, p=0.5, seed=1)
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(out, m.residual_norm_fwd(x, x, p=0.5, seed=1)):
+        assert torch.equal(a, b)
+
+
+def test_one_gradient_of_a_branch_alone():
+    """The C call with either of dx and dresidual left out gives the other the same bits."""
+    import paper_1903_06934_amd as m
+    L = m.lib()
+    stream = torch.cuda.current_stream().cuda_stream
+    for rows, cols in ((40, 264), (9, 20000)):
+        d, _ = small_inputs(m, rows, cols, 100, F32)
+        out = m.residual_norm_fwd(d["x"], d["res"], d["w"], p=0.4, seed=8)
+        want = m.residual_norm_bwd(d["x"], out.total, out.mean, out.rstd, d["w"], d["res"], p=0.4,
+                                   seed=8, with_weight=False, with_bias=False)
+        ws = m.residual_norm_workspace(True, d["x"])
+        for k in range(2):
+            got = torch.empty_like(d["x"])
+            p = [None, None]
+            p[k] = got.data_ptr()
+            st = L.residual_norm_bwd(0, 0, rows, cols, d["x"].data_ptr(), cols,
+                                     out.total.data_ptr(), cols, out.mean.data_ptr(),
+                                     out.rstd.data_ptr(), d["w"].data_ptr(), d["res"].data_ptr(),
+                                     cols, 0.4, 8, 0, 0, None, p[1], cols, p[0], cols, None, None,
+                                     ws.data_ptr(), ws.numel(), stream)
+            assert st == 0 and torch.equal(got, want[k])
+
+
+def test_columns_of_one_matrix():
+    """A branch, the stream and the results as columns of one wider matrix."""
+    import paper_1903_06934_amd as m
+    wide = torch.randn(50, 4 * 72 + 8, device="cuda")
+    x, res, total, y = (wide[:, 72 * i:72 * (i + 1)] for i in range(4))
+    keep = wide[:, 288:].clone()
+    want = m.residual_norm_fwd(x.clone(), res.clone(), p=0.3, seed=4)
+    out = m.residual_norm_fwd(x, res, p=0.3, seed=4, total=total, y=y)
+    assert torch.equal(out.total, want.total) and torch.equal(out.y, want.y)
+    m.dropout_fwd(x, 0.3, 4, residual=res, y=y)
+    assert torch.equal(y, want.total) and torch.equal(wide[:, 288:], keep)
+
+
+def test_refuses_on_the_gpu():
+    import paper_1903_06934_amd as m
+    x = torch.zeros(4, 8, device="cuda")
+    half, other = x.half(), torch.zeros(4, 9, device="cuda")
+    t = torch.zeros(32, device="cuda")
+    q = torch.tensor([0, 8, 32], device="cuda")
+    for call in (lambda: m.dropout_fwd(x, 0.1, 1, residual=half),
+                 lambda: m.dropout_fwd(x, 0.1, 1, y=other), lambda: m.dropout_fwd(x, 0.1, 1, step=0.5),
+                 lambda: m.dropout_fwd(x.int(), 0.1, 1), lambda: m.dropout_bwd(x.t(), 0.1, 1),
+                 lambda: m.residual_norm_fwd(x, half), lambda: m.residual_norm_fwd(x, other),
+                 lambda: m.residual_norm_fwd(x, x, w=t), lambda: m.residual_norm_fwd(x, x, total=half),
+                 lambda: m.residual_norm_bwd(x, half, t[:4], t[:4]),
+                 lambda: m.residual_norm_bwd(x, x, t[:3], t[:4]),
+                 lambda: m.residual_norm_bwd(x, x, t[:4], t[:4], dtotal=half),
+                 lambda: m.policy_loss(t, t, t, mask=t), lambda: m.policy_loss(t, t, t[:2]),
+                 lambda: m.policy_loss(t, t, t, by_sequence=True, starts=q),
+                 lambda: m.policy_loss(t, t, t, stats=t[:5]),
+                 lambda: m.policy_loss(t, t, t, ref_logp=t.bfloat16()),
+                 lambda: m.preference_loss(t, t, q[:2], 0.1),
+                 lambda: m.preference_loss(t, t, q, 0.1, rewards=t[:3])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: m.dropout_fwd(x, 1.5, 1), lambda: m.dropout_fwd(x, float("nan"), 1),
+                 lambda: m.dropout_fwd(x[:3], 0.5, 1, y=x[1:]),
+                 lambda: m.residual_norm_fwd(x, x, total=x, y=x),
+                 lambda: m.residual_norm_fwd(x, x, eps=-1.0),
+                 lambda: m.policy_loss(t, t, t, clip_low=2.0), lambda: m.policy_loss(t, t, t, mean=0.0),
+                 lambda: m.policy_loss(t, t, t, kl_weight=1.0),
+                 lambda: m.policy_loss(t, t, t, entropy_weight=1.0),
+                 lambda: m.policy_loss(t, t, t, dlogp=t), lambda: m.policy_loss(t, t, t, mean="sequences"),
+                 lambda: m.preference_loss(t, t, q, 0.0), lambda: m.preference_loss(t, t, q, 0.1, dlogp=t)):
+        with pytest.raises(m.MiconvError):
+            call()
+    for call in (lambda: m.dropout_fwd(x, 0.5, -1), lambda: m.dropout_fwd(x, 0.5, 1 << 64),
+                 lambda: m.dropout_fwd(x, 0.5, 1, 1 << 32)):
+        with pytest.raises(TypeError):
+            call()
+
+
 # ----------------------------------------------------------------- large sizes
 def test_dropout_past_32_bits():
     """Element indices past 2^32 and, where their groups' numbers are too, past 2^35."""

@@ -141,7 +141,8 @@ def policy(L, tokens=20000, seqs=10, lp=A, lo=B, lr=C, h=D, adv=E, by_seq=0, mas
     (VALUE, dict(high=nan)), (VALUE, dict(dual=0.9)), (VALUE, dict(dual=nan)), (VALUE, dict(kl=3)),
     (VALUE, dict(kl=-1)), (VALUE, dict(kw=inf)), (VALUE, dict(kw=1e39)), (VALUE, dict(ew=nan)),
     (VALUE, dict(mean=3)), (VALUE, dict(mean=-1)), (VALUE, dict(mean=2, count=0.0)),
-    (VALUE, dict(mean=2, count=inf)), (VALUE, dict(mean=2, count=nan)), (VALUE, dict(scale=inf)),
+    (VALUE, dict(mean=2, count=inf)), (VALUE, dict(mean=2, count=1e-300)),
+    (VALUE, dict(mean=2, count=1e-10, scale=1e30)), (VALUE, dict(mean=2, count=nan)), (VALUE, dict(scale=inf)),
     (NULL, dict(starts=None, seqs=0)), (NULL, dict(starts=None, seqs=0, mean=0, by_seq=1)),
     (NULL, dict(lp=None)), (NULL, dict(lo=None)), (NULL, dict(lr=None)), (NULL, dict(h=None)),
     (NULL, dict(h=None, ew=0.0)), (NULL, dict(adv=None)), (NULL, dict(stats=None)),
@@ -212,6 +213,9 @@ def test_workspace_sizes(L):
 
 def test_binding_refuses(L):
     """The binding's own checks, on CPU tensors."""
+    # The type of a step is looked at before its device; any whole number is one.
+    with pytest.raises(ValueError, match="x must be"):
+        m.dropout_fwd(torch.zeros(4, 8), 0.1, 1, 0, -1)
     x, t, q = torch.zeros(4, 8), torch.zeros(4), torch.zeros(3, dtype=torch.int64)
     for call in (lambda: m.dropout_fwd(x, 0.1, 1), lambda: m.dropout_bwd(x, 0.1, 1),
                  lambda: m.residual_norm_fwd(x, x), lambda: m.residual_norm_bwd(x, x, t, t),
