@@ -3,7 +3,7 @@
 // Element e's 16 random bits are computed where they are used, eight elements at
 // a time (random.h), and nothing of the mask is stored; both directions are one
 // kernel.  Bound by memory: 16384 x 4096 bf16 43 us (6.2 TB/s; a copy of as many bytes
-// takes 50), onto a residual 64.7; 12544 x 513 fp32 inside wider rows 13.2 (a copy 11.5).
+// takes 50), onto a residual 64.7; 12544 x 513 fp32 inside wider rows 12.1 (a copy 11.5).
 // The generator's twenty 32 x 32 bit products for eight elements are what else it does:
 // with 32 bits an element there would be twice as many, more than the memory hides.
 // The figures at the rules are of whole calls replayed from a graph on three inputs in
@@ -21,9 +21,10 @@ namespace miconv {
 namespace {
 
 // Packs in flight a thread: of eight 16-bit elements (16384 x 4096 bf16 43.6 us, of two
-// packs 46.4), or of four 32-bit ones (12544 x 513 fp32 13.3 us, of eight packs 18.9).
+// packs 46.4), or of four 32-bit ones (12544 x 513 fp32 12.1 us, of four packs 13.6; 128 x
+// 4096 2.8 and 3.5).
 template <class T>
-constexpr int kPacksOf = Pack<T>::N == 8 ? 1 : 4;
+constexpr int kPacksOf = Pack<T>::N == 8 ? 1 : 2;
 
 template <class T>
 __device__ __forceinline__ T dropped(const Dropper &drop, T x, T residual, uint32_t word, int odd)
@@ -35,7 +36,7 @@ __device__ __forceinline__ T dropped(const Dropper &drop, T x, T residual, uint3
 // The words of a thread's packs q[0 .. U).  A group of eight 32-bit elements is two
 // packs, of neighbouring threads: of two packs each the even thread computes the first
 // one's group, the odd one the second one's, and they exchange halves (16384 x 2048 fp32:
-// 47.6 us, with two packs side by side a thread 77.5).  All threads of a wave call it.
+// 43.9 us, with two packs side by side a thread 77.5).  All threads of a wave call it.
 template <class T>
 __device__ __forceinline__ void words_of(const Dropper &drop, const long long (&q)[kPacksOf<T>],
                                          uint32_t (&w)[kPacksOf<T>][Pack<T>::N / 2])
@@ -49,14 +50,17 @@ __device__ __forceinline__ void words_of(const Dropper &drop, const long long (&
         const bool odd = threadIdx.x & 1;
 #pragma unroll
         for (int u = 0; u < U; u += 2) {
-            uint32_t g[4], got[2];
-            drop.group((unsigned long long)(odd ? q[u + 1] : q[u]) >> 1, g);
+            // Values, not places in arrays, to choose from: places go through memory.
+            const long long first = q[u], second = q[u + 1];
+            uint32_t g[4];
+            drop.group((unsigned long long)(odd ? second : first) >> 1, g);
 #pragma unroll
             for (int i = 0; i < 2; i++) {
-                const uint32_t give = odd ? g[i] : g[2 + i];
-                got[i] = __builtin_amdgcn_mov_dpp((int)give, 0xb1, 0xf, 0xf, true);
-                w[u][i] = odd ? got[i] : g[i];
-                w[u + 1][i] = odd ? g[2 + i] : got[i];
+                const uint32_t low = g[i], high = g[2 + i];
+                const uint32_t got = __builtin_amdgcn_mov_dpp((int)(odd ? low : high), 0xb1, 0xf,
+                                                              0xf, true);
+                w[u][i] = odd ? got : low;
+                w[u + 1][i] = odd ? high : got;
             }
         }
     }
