@@ -98,8 +98,10 @@ int residual_norm_bwd(int xtype, int wtype, long long rows, long long cols, cons
  * token counts where it is not 0 and the token is in a sequence.  What the other
  * tensors hold of a token that does not count is not used (it may be NaN), and
  * its gradients are 0.  0 <= tokens, seqs < 2^31 (else MICONV_ERR_SHAPE).
- * Sums are held in 64 bits.  The gradients are those of the loss, times scale
- * (finite, else MICONV_ERR_VALUE); they are NULL where they are not wanted.
+ * Sums are held in 64 bits, but for those of at most eight tokens side by side in
+ * the policy loss: these are held in 32 bits, and infinite beyond them.  The
+ * gradients are those of the loss, times scale (finite, else MICONV_ERR_VALUE);
+ * they are NULL where they are not wanted.
  */
 
 /*

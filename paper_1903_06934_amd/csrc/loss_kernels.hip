@@ -1,8 +1,8 @@
 // The losses of fine-tuning and their gradients (include/mistep.h): the clipped
 // policy loss of sampled tokens, and the loss of pairs of sequences.
 //
-// Tokens are taken by chunks, whatever the sequences' lengths, four tokens side by
-// side a thread.  Where sequences begin in a chunk is marked in LDS by a thread a
+// Tokens are taken by chunks, whatever the sequences' lengths, four or eight of them
+// side by side a thread.  Where sequences begin in a chunk is marked in LDS by a thread a
 // sequence; a scan over the chunk then tells each token where its sequence begins
 // (what belongs to the sequence lies there), or sums the sequences' tokens.  A
 // sequence that reaches over several chunks leaves its piece of each in the
@@ -20,11 +20,30 @@ namespace miconv {
 
 namespace {
 
-constexpr int kEach = 4;  // tokens side by side a thread
-// A workgroup of the calls of many tokens: threads, and packs of kEach tokens a thread,
-// each of the workgroup's packs behind the last one's; and of the calls of few.
-constexpr int kBlock = 256, kPacks = 2, kChunk = kBlock * kPacks * kEach;
-constexpr int kOneBlock = 1024, kOnePacks = 1, kOneChunk = kOneBlock * kOnePacks * kEach;
+// A workgroup's share of the tokens, a chunk: BLOCK threads, PACKS packs of EACH tokens a
+// thread, the packs t + h BLOCK of thread t; 64 packs side by side are a wave's.
+template <int B, int P, int E>
+struct Tile {
+    static constexpr int BLOCK = B, PACKS = P, EACH = E, ALL = B * P, SIZE = ALL * E;
+
+    // Of the thread's h-th pack among all.
+    static __device__ __forceinline__ int rank(int h) { return h * B + (int)threadIdx.x; }
+};
+
+// Calls of many tokens.  The scans over a chunk cost as much for eight tokens a thread as
+// for four, but eight tokens of a policy at once take too many registers (2 000 003
+// tokens: pairs 20.1 us, by packs of four 21.1; policy 33.0 by packs of eight, 24.7 by two
+// of four).
+constexpr int kChunk = 2048;
+typedef Tile<256, 1, 8> Wide;
+typedef Tile<256, 2, 4> Narrow;
+static_assert(Wide::SIZE == kChunk && Narrow::SIZE == kChunk, "one chunk for all launches");
+// Calls of few, in one workgroup: up to 4096 tokens, and up to 8192 (4000 tokens: policy
+// 5.7 us, pairs 7.8, by the larger 7.7 and 9.0; 8000 tokens 11.1 and 9.3, by chunks 15.2 and
+// 13.4).
+typedef Tile<1024, 1, 4> SmallPolicy;
+typedef Tile<512, 1, 8> SmallPairs;
+typedef Tile<1024, 1, 8> Small;
 constexpr int kMaxGroups = 1024;  // workgroups of a launch over the chunks, and partial sums
 constexpr int kJoinGroups = 1024;  // of a launch over the sequences
 
@@ -315,17 +334,23 @@ __device__ __forceinline__ unsigned bits_of(uint32_t v)
 }
 
 // rank: of the pack in the chunk.
+template <class S>
 __device__ __forceinline__ Mine my_tokens(const unsigned char *mask, int begin, int end, int rank)
 {
     Mine m;
     // Past the end the first token may be beyond 32 bits: it is not used.
-    m.left = end - begin - rank * kEach;
-    m.t0 = m.left > 0 ? begin + rank * kEach : begin;
-    m.mask = (1u << min(max(m.left, 0), kEach)) - 1;
+    m.left = end - begin - rank * S::EACH;
+    m.t0 = m.left > 0 ? begin + rank * S::EACH : begin;
+    m.mask = (1u << min(max(m.left, 0), S::EACH)) - 1;
     if (mask && m.left > 0) {
-        if (m.left >= kEach) {
-            typedef uint32_t At __attribute__((aligned(1)));
-            m.mask = bits_of(*(const At *)(mask + m.t0));
+        if (m.left >= S::EACH) {
+            typedef uint32_t V __attribute__((ext_vector_type(S::EACH / 4)));
+            typedef V At __attribute__((aligned(1)));
+            // Four bytes, or eight.
+            const V v = *(const At *)(mask + m.t0);
+            m.mask = bits_of(v[0]);
+            if constexpr (S::EACH == 8)
+                m.mask |= bits_of(v[1]) << 4;
         } else {
             m.mask = 0;
             for (int j = 0; j < m.left; j++)
@@ -336,43 +361,41 @@ __device__ __forceinline__ Mine my_tokens(const unsigned char *mask, int begin, 
 }
 
 // Those of the pack's tokens that lie in from <= t < to.
+template <class S>
 __device__ __forceinline__ unsigned inside(const Mine &m, int from, int to)
 {
     // Tokens past the end are not in the mask.
-    const unsigned before = (1u << min(max(from - m.t0, 0), kEach)) - 1;
-    return ((1u << min(max(to - m.t0, 0), kEach)) - 1) & ~before;
+    const unsigned before = (1u << min(max(from - m.t0, 0), S::EACH)) - 1;
+    return ((1u << min(max(to - m.t0, 0), S::EACH)) - 1) & ~before;
 }
 
-__device__ __forceinline__ void load_floats(const float *p, const Mine &m, float (&v)[kEach])
+template <int E>
+__device__ __forceinline__ void load_floats(const float *p, const Mine &m, float (&v)[E])
 {
-    F4 f = F4{};
-    if (m.left > 0)
-        f = load_pack<float>(p + m.t0, m.left, 0.f);
 #pragma unroll
-    for (int j = 0; j < kEach; j++)
-        v[j] = f[j];
+    for (int i = 0; i < E; i += 4) {
+        F4 f = F4{};
+        if (m.left > i)
+            f = load_pack<float>(p + m.t0 + i, m.left - i, 0.f);
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            v[i + j] = f[j];
+    }
 }
 
-__device__ __forceinline__ void store_floats(float *p, const Mine &m, const float (&v)[kEach])
+template <int E>
+__device__ __forceinline__ void store_floats(float *p, const Mine &m, const float (&v)[E])
 {
-    if (m.left > 0)
-        store_pack<float>(p + m.t0, m.left, F4{v[0], v[1], v[2], v[3]});
-}
-
-static_assert(kEach == Pack<float>::N, "a pack a thread");
-
-// Of a workgroup's BLOCK * PACKS packs of tokens, thread t's are the packs t + h BLOCK;
-// 64 packs side by side are a wave's.
-template <int BLOCK>
-__device__ __forceinline__ int rank_of(int h)
-{
-    return h * BLOCK + (int)threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < E; i += 4)
+        if (m.left > i)
+            store_pack<float>(p + m.t0 + i, m.left - i, F4{v[i], v[i + 1], v[i + 2], v[i + 3]});
 }
 
 // How many tokens of the chunk before each count: by pack, and a bit each.
-template <int BLOCK, int PACKS>
+template <class S>
 struct CountTable {
-    static constexpr int ALL = BLOCK * PACKS;
+    static constexpr int ALL = S::ALL;
     int before[ALL];
     unsigned char bits[ALL];
     int waves[ALL / 64];
@@ -380,10 +403,10 @@ struct CountTable {
     // To be called by all threads; the caller's barrier follows.
     __device__ __forceinline__ void scan(int h, unsigned counted)
     {
-        const int rank = rank_of<BLOCK>(h);
+        const int rank = S::rank(h);
         int v = 0, n = 0;
 #pragma unroll
-        for (int j = 0; j < kEach; j++) {
+        for (int j = 0; j < S::EACH; j++) {
             const unsigned long long b = __ballot(counted >> j & 1);
             v += __builtin_amdgcn_mbcnt_hi((unsigned)(b >> 32),
                                            __builtin_amdgcn_mbcnt_lo((unsigned)b, 0));
@@ -397,45 +420,51 @@ struct CountTable {
     // Of the chunk's tokens before its at-th (at most all).
     __device__ __forceinline__ int up_to(int at) const
     {
-        const int i = at / kEach;
+        const int i = at / S::EACH;
         int v = 0;
         for (int w = 0; w < i / 64; w++)
             v += waves[w];
-        return i < ALL ? v + before[i] + __popc(bits[i] & ((1u << at % kEach) - 1)) : v;
+        return i < ALL ? v + before[i] + __popc(bits[i] & ((1u << at % S::EACH) - 1)) : v;
     }
 };
 
 // Marks in LDS where sequences begin: a byte each of the chunk's tokens.
-template <int BLOCK, int PACKS>
+template <class S>
 struct Marks {
-    static constexpr int ALL = BLOCK * PACKS;
-    alignas(4) unsigned char at[ALL * kEach];
+    static constexpr int ALL = S::ALL, SIZE = S::SIZE;
+    alignas(8) unsigned char at[SIZE];
     int waves[ALL / 64];
 
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
-        for (int h = 0; h < PACKS; h++)
-            *(uint32_t *)(at + rank_of<BLOCK>(h) * kEach) = 0;
+        for (int h = 0; h < S::PACKS; h++)
+            for (int i = 0; i < S::EACH; i += 4)
+                *(uint32_t *)(at + S::rank(h) * S::EACH + i) = 0;
     }
     __device__ __forceinline__ unsigned mine(int h) const
     {
-        const uint32_t v = *(const uint32_t *)(at + rank_of<BLOCK>(h) * kEach);
-        return (v | v >> 7 | v >> 14 | v >> 21) & 15;  // of bytes that are 0 or 1
+        unsigned bits = 0;
+#pragma unroll
+        for (int i = 0; i < S::EACH; i += 4) {
+            const uint32_t b = *(const uint32_t *)(at + S::rank(h) * S::EACH + i);
+            bits |= ((b | b >> 7 | b >> 14 | b >> 21) & 15) << i;  // of bytes that are 0 or 1
+        }
+        return bits;
     }
     // Where the sequence of each of the thread's tokens begins in the chunk, -1 where
     // none has begun.  One barrier.
-    __device__ __forceinline__ void places(int (&place)[PACKS][kEach])
+    __device__ __forceinline__ void places(int (&place)[S::PACKS][S::EACH])
     {
         const int lane = threadIdx.x & 63;
-        unsigned marks[PACKS];
-        int last[PACKS];
-        bool within[PACKS];
+        unsigned marks[S::PACKS];
+        int last[S::PACKS];
+        bool within[S::PACKS];
 #pragma unroll
-        for (int h = 0; h < PACKS; h++) {
-            const int rank = rank_of<BLOCK>(h);
+        for (int h = 0; h < S::PACKS; h++) {
+            const int rank = S::rank(h);
             marks[h] = mine(h);
-            const int own = rank * kEach + 31 - __builtin_clz(marks[h] | 1);
+            const int own = rank * S::EACH + 31 - __builtin_clz(marks[h] | 1);
             const unsigned long long any = __ballot(marks[h] != 0);
             const unsigned long long before = any & ((1ULL << lane) - 1);
             within[h] = before != 0;
@@ -445,16 +474,16 @@ struct Marks {
         }
         __syncthreads();
 #pragma unroll
-        for (int h = 0; h < PACKS; h++) {
-            const int rank = rank_of<BLOCK>(h);
+        for (int h = 0; h < S::PACKS; h++) {
+            const int rank = S::rank(h);
             if (!within[h]) {
                 last[h] = -1;
                 for (int w = (rank >> 6) - 1; w >= 0 && last[h] < 0; w--)
                     last[h] = waves[w];
             }
 #pragma unroll
-            for (int j = 0; j < kEach; j++) {
-                last[h] = marks[h] >> j & 1 ? rank * kEach + j : last[h];
+            for (int j = 0; j < S::EACH; j++) {
+                last[h] = marks[h] >> j & 1 ? rank * S::EACH + j : last[h];
                 place[h][j] = last[h];
             }
         }
@@ -475,20 +504,21 @@ struct Counts {
     int *some;        // [kJoinGroups] sequences that have any
 };
 
-__global__ __launch_bounds__(kBlock) void policy_count(PolicyArgs a, Counts c, int chunks)
+__global__ __launch_bounds__(Narrow::BLOCK) void policy_count(PolicyArgs a, Counts c, int chunks)
 {
-    __shared__ CountTable<kBlock, kPacks> table;
-    __shared__ int red[kBlock / 64][1];
+    typedef Narrow S;
+    __shared__ CountTable<S> table;
+    __shared__ int red[S::BLOCK / 64][1];
     const Starts starts{a.starts, a.tokens};
     int all[1] = {0};
     for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
-        const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
-        Mine m[kPacks];
+        const int begin = k * S::SIZE, end = end_of_chunk(begin, a.tokens);
+        Mine m[S::PACKS];
         if (a.mean == 1) {
-            Sequences<kBlock, kPolicyLook> q(starts, a.seqs, begin, end);
+            Sequences<S::BLOCK, kPolicyLook> q(starts, a.seqs, begin, end);
 #pragma unroll
-            for (int h = 0; h < kPacks; h++) {
-                m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
+            for (int h = 0; h < S::PACKS; h++) {
+                m[h] = my_tokens<S>(a.mask, begin, end, S::rank(h));
                 table.scan(h, m[h].mask);
             }
             __syncthreads();
@@ -500,15 +530,15 @@ __global__ __launch_bounds__(kBlock) void policy_count(PolicyArgs a, Counts c, i
         } else {
             const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
 #pragma unroll
-            for (int h = 0; h < kPacks; h++) {
-                m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
-                all[0] += __popc(m[h].mask & inside(m[h], from, to));
+            for (int h = 0; h < S::PACKS; h++) {
+                m[h] = my_tokens<S>(a.mask, begin, end, S::rank(h));
+                all[0] += __popc(m[h].mask & inside<S>(m[h], from, to));
             }
         }
     }
     if (a.mean == 1)
         return;
-    block_totals<kBlock>(all, red, [&](int, int v) { c.group[blockIdx.x] = v; });
+    block_totals<S::BLOCK>(all, red, [&](int, int v) { c.group[blockIdx.x] = v; });
 }
 
 // Each sequence's tokens that count, and how many sequences have any.
@@ -637,15 +667,16 @@ __device__ __forceinline__ Token token_loss(const PolicyArgs &a, const Borders &
     return k;
 }
 
+template <int E>
 struct Tokens {
-    float lp[kEach], lo[kEach], lr[kEach], h[kEach], adv[kEach];
+    float lp[E], lo[E], lr[E], h[E], adv[E];
 };
 
-template <Ref REF>
-__device__ __forceinline__ void load_tokens(const PolicyArgs &a, const Mine &m, Tokens &k)
+template <Ref REF, int E>
+__device__ __forceinline__ void load_tokens(const PolicyArgs &a, const Mine &m, Tokens<E> &k)
 {
 #pragma unroll
-    for (int j = 0; j < kEach; j++)
+    for (int j = 0; j < E; j++)
         k.h[j] = 0.f;
     load_floats(a.logp, m, k.lp);
     load_floats(a.old_logp, m, k.lo);
@@ -661,16 +692,17 @@ __device__ __forceinline__ void load_tokens(const PolicyArgs &a, const Mine &m, 
 // weights within their sequences, if WEIGHTS) to sum, their gradients to memory.
 // counted: the tokens that count; w: their weights; factor: what those of the gradients
 // are multiplied by.
-template <bool WEIGHTS, Ref REF>
+template <bool WEIGHTS, Ref REF, int E>
 __device__ __forceinline__ void token_losses(const PolicyArgs &a, const Borders &borders,
-                                             const Mine &m, const Tokens &k, unsigned counted,
-                                             const float (&w)[kEach], float factor,
+                                             const Mine &m, const Tokens<E> &k, unsigned counted,
+                                             const float (&w)[E], float factor,
                                              double (&sum)[5])
 {
-    float g[kEach], gh[kEach], part[5] = {0, 0, 0, 0, 0};
+    float g[E], gh[E], part[5] = {0, 0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < kEach; j++) {
-        // A token that does not count is one of nothing but zeros, with no weight.
+    for (int j = 0; j < E; j++) {
+        // A token that does not count is one of nothing but zeros, with no weight.  The
+        // few tokens are added in 32 bits: their terms' own roundings are as large.
         const bool in = counted >> j & 1;
         const auto only = [in](float v) { return in ? v : 0.f; };
         const Token r = token_loss<REF>(a, borders, only(k.lp[j]), only(k.lo[j]),
@@ -721,17 +753,17 @@ __device__ __forceinline__ OfSequence of_sequence(const PolicyArgs &a, long long
 }
 
 // The tokens' weights and advantages from what lies where their sequences begin.
-template <int BLOCK, int PACKS>
-__device__ __forceinline__ void from_sequences(const PolicyArgs &a, Marks<BLOCK, PACKS> &marks,
-                                               const OfSequence *seq, Tokens (&k)[PACKS],
-                                               float (&w)[PACKS][kEach])
+template <class S>
+__device__ __forceinline__ void from_sequences(const PolicyArgs &a, Marks<S> &marks,
+                                               const OfSequence *seq, Tokens<S::EACH> (&k)[S::PACKS],
+                                               float (&w)[S::PACKS][S::EACH])
 {
-    int place[PACKS][kEach];
+    int place[S::PACKS][S::EACH];
     marks.places(place);
 #pragma unroll
-    for (int h = 0; h < PACKS; h++)
+    for (int h = 0; h < S::PACKS; h++)
 #pragma unroll
-        for (int j = 0; j < kEach; j++) {
+        for (int j = 0; j < S::EACH; j++) {
             const OfSequence q = seq[max(place[h][j], 0)];
             w[h][j] = q.weight;
             if (a.by_sequence)
@@ -740,40 +772,39 @@ __device__ __forceinline__ void from_sequences(const PolicyArgs &a, Marks<BLOCK,
 }
 
 // Few tokens: all of the call in one workgroup.  SEQS: the sequences matter.
-template <bool SEQS, Ref REF>
-__global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
+template <class S, bool SEQS, Ref REF>
+__global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
 {
-    constexpr int WAVES = kOneBlock / 64;
-    constexpr int PACKS = kOnePacks;
-    __shared__ Marks<SEQS ? kOneBlock : 64, PACKS> marks;
-    __shared__ CountTable<SEQS ? kOneBlock : 64, PACKS> table;
-    __shared__ OfSequence seq[SEQS ? kOneChunk : 1];
+    constexpr int WAVES = S::BLOCK / 64;
+    __shared__ Marks<std::conditional_t<SEQS, S, Tile<64, 1, 4>>> marks;
+    __shared__ CountTable<std::conditional_t<SEQS, S, Tile<64, 1, 4>>> table;
+    __shared__ OfSequence seq[SEQS ? S::SIZE : 1];
     __shared__ double red[WAVES][5], total[5];
     __shared__ int counts[WAVES][1];
     const Starts starts{a.starts, a.tokens};
     const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
-    Sequences<kOneBlock, kPolicyLook> q(starts, SEQS ? a.seqs : 0, 0, a.tokens);
-    Mine m[PACKS];
-    Tokens k[PACKS];
-    float w[PACKS][kEach];
+    Sequences<S::BLOCK, kPolicyLook> q(starts, SEQS ? a.seqs : 0, 0, a.tokens);
+    Mine m[S::PACKS];
+    Tokens<S::EACH> k[S::PACKS];
+    float w[S::PACKS][S::EACH];
 #pragma unroll
-    for (int h = 0; h < PACKS; h++) {
-        m[h] = my_tokens(a.mask, 0, a.tokens, rank_of<kOneBlock>(h));
+    for (int h = 0; h < S::PACKS; h++) {
+        m[h] = my_tokens<S>(a.mask, 0, a.tokens, S::rank(h));
         load_tokens<REF>(a, m[h], k[h]);
 #pragma unroll
-        for (int j = 0; j < kEach; j++)
+        for (int j = 0; j < S::EACH; j++)
             w[h][j] = 1.f;
     }
     int n[1] = {0};  // tokens that count, or sequences that have any
 #pragma unroll
-    for (int h = 0; h < PACKS; h++)
-        n[0] += __popc(m[h].mask & inside(m[h], from, to));
+    for (int h = 0; h < S::PACKS; h++)
+        n[0] += __popc(m[h].mask & inside<S>(m[h], from, to));
     const bool counted = n[0] > 0;
     double u = 1.0 / a.count;
     if constexpr (SEQS) {
         marks.clear();
 #pragma unroll
-        for (int h = 0; h < PACKS; h++)
+        for (int h = 0; h < S::PACKS; h++)
             table.scan(h, m[h].mask);
         __syncthreads();
         if (a.mean == 1)
@@ -787,7 +818,7 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
         });
     }
     if (a.mean != 2) {
-        block_sums<kOneBlock>(n, counts);
+        block_sums<S::BLOCK>(n, counts);
         u = 1.0 / max(n[0], 1);
     }
     if constexpr (SEQS) {
@@ -797,21 +828,23 @@ __global__ __launch_bounds__(kOneBlock) void policy_one(PolicyArgs a)
     const Borders borders(a);
     double sum[5] = {0, 0, 0, 0, 0};
 #pragma unroll
-    for (int h = 0; h < PACKS; h++)
-        token_losses<SEQS, REF>(a, borders, m[h], k[h], m[h].mask & inside(m[h], from, to), w[h],
+    for (int h = 0; h < S::PACKS; h++)
+        token_losses<SEQS, REF, S::EACH>(a, borders, m[h], k[h], m[h].mask & inside<S>(m[h], from, to), w[h],
                                 (float)(u * a.scale), sum);
-    block_totals<kOneBlock>(sum, red, [&](int i, double v) { total[i] = v * u; }, counted);
+    block_totals<S::BLOCK>(sum, red, [&](int i, double v) { total[i] = v * u; }, counted);
     // The same wave has written them.
     if (threadIdx.x < 6)
         a.stats[threadIdx.x] = policy_result(a, total, (int)threadIdx.x);
 }
 
 template <bool SEQS, Ref REF>
-__global__ __launch_bounds__(kBlock, 4) void policy_main(PolicyArgs a, Counts c, int chunks, int joins)
+__global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Counts c, int chunks,
+                                                             int joins)
 {
-    __shared__ Marks<SEQS ? kBlock : 64, kPacks> marks;
-    __shared__ OfSequence seq[SEQS ? kChunk : 1];
-    __shared__ double red[kBlock / 64][5], of_all;
+    typedef Narrow S;
+    __shared__ Marks<std::conditional_t<SEQS, S, Tile<64, 1, 4>>> marks;
+    __shared__ OfSequence seq[SEQS ? S::SIZE : 1];
+    __shared__ double red[S::BLOCK / 64][5], of_all;
     const Starts starts{a.starts, a.tokens};
     const Borders borders(a);
     double u = 0.0, sum[5] = {0, 0, 0, 0, 0};
@@ -825,17 +858,17 @@ __global__ __launch_bounds__(kBlock, 4) void policy_main(PolicyArgs a, Counts c,
         of_all = 1.0 / n;
     }
     for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
-        const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
-        Sequences<kBlock, kPolicyLook> q(starts, SEQS ? a.seqs : 0, begin, end);
-        Mine m[kPacks];
-        Tokens tokens[kPacks];
-        float w[kPacks][kEach];
+        const int begin = k * S::SIZE, end = end_of_chunk(begin, a.tokens);
+        Sequences<S::BLOCK, kPolicyLook> q(starts, SEQS ? a.seqs : 0, begin, end);
+        Mine m[S::PACKS];
+        Tokens<S::EACH> tokens[S::PACKS];
+        float w[S::PACKS][S::EACH];
 #pragma unroll
-        for (int h = 0; h < kPacks; h++) {
-            m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
+        for (int h = 0; h < S::PACKS; h++) {
+            m[h] = my_tokens<S>(a.mask, begin, end, S::rank(h));
             load_tokens<REF>(a, m[h], tokens[h]);
 #pragma unroll
-            for (int j = 0; j < kEach; j++)
+            for (int j = 0; j < S::EACH; j++)
                 w[h][j] = 1.f;
         }
         if constexpr (SEQS) {
@@ -853,14 +886,14 @@ __global__ __launch_bounds__(kBlock, 4) void policy_main(PolicyArgs a, Counts c,
         if constexpr (SEQS)
             from_sequences(a, marks, seq, tokens, w);
 #pragma unroll
-        for (int h = 0; h < kPacks; h++)
-            token_losses<SEQS, REF>(a, borders, m[h], tokens[h],
-                                    m[h].mask & inside(m[h], from, to), w[h],
+        for (int h = 0; h < S::PACKS; h++)
+            token_losses<SEQS, REF, S::EACH>(a, borders, m[h], tokens[h],
+                                    m[h].mask & inside<S>(m[h], from, to), w[h],
                                     (float)(u * a.scale), sum);
         if (SEQS)
             __syncthreads();
     }
-    block_totals<kBlock>(sum, red, [&](int i, double v) {
+    block_totals<S::BLOCK>(sum, red, [&](int i, double v) {
         c.part[(size_t)i * gridDim.x + blockIdx.x] = v * u;
     });
 }
@@ -949,15 +982,15 @@ __device__ __forceinline__ double pair_gradient(const PreferenceArgs &a, double 
 }
 
 // The tokens' log ratios, 0 where they do not count.
-__device__ __forceinline__ void load_ratios(const PreferenceArgs &a, const Mine &m,
-                                            float (&v)[kEach])
+template <int E>
+__device__ __forceinline__ void load_ratios(const PreferenceArgs &a, const Mine &m, float (&v)[E])
 {
-    float lr[kEach];
+    float lr[E];
     load_floats(a.logp, m, v);
     if (a.ref_logp)
         load_floats(a.ref_logp, m, lr);
 #pragma unroll
-    for (int j = 0; j < kEach; j++) {
+    for (int j = 0; j < E; j++) {
         v[j] = a.ref_logp ? v[j] - lr[j] : v[j];
         v[j] = m.mask >> j & 1 ? v[j] : 0.f;
     }
@@ -965,28 +998,28 @@ __device__ __forceinline__ void load_ratios(const PreferenceArgs &a, const Mine 
 
 // The sums of the chunk's sequences, each at its last token, of the threads' values
 // and the marks where sequences begin.
-template <int BLOCK, int PACKS>
+template <class S>
 struct Sums {
-    static constexpr int ALL = BLOCK * PACKS;
-    double at[ALL * kEach];
+    static constexpr int ALL = S::ALL;
+    double at[S::SIZE];
     double tail[ALL / 64];             // since the wave's last mark
     unsigned long long marked[ALL / 64];
 
     // One barrier; the caller's follows.
-    __device__ __forceinline__ void scan(const Marks<BLOCK, PACKS> &marks,
-                                         const float (&v)[PACKS][kEach])
+    __device__ __forceinline__ void scan(const Marks<S> &marks,
+                                         const float (&v)[S::PACKS][S::EACH])
     {
         const int lane = threadIdx.x & 63;
-        double run[PACKS][kEach], before[PACKS];
-        unsigned mine[PACKS];
-        bool within[PACKS];
+        double run[S::PACKS][S::EACH], before[S::PACKS];
+        unsigned mine[S::PACKS];
+        bool within[S::PACKS];
 #pragma unroll
-        for (int h = 0; h < PACKS; h++) {
-            const int rank = rank_of<BLOCK>(h);
+        for (int h = 0; h < S::PACKS; h++) {
+            const int rank = S::rank(h);
             mine[h] = marks.mine(h);
             double s = 0;
 #pragma unroll
-            for (int j = 0; j < kEach; j++) {
+            for (int j = 0; j < S::EACH; j++) {
                 s = mine[h] >> j & 1 ? (double)v[h][j] : s + (double)v[h][j];
                 run[h][j] = s;
             }
@@ -1012,20 +1045,20 @@ struct Sums {
         }
         __syncthreads();
 #pragma unroll
-        for (int h = 0; h < PACKS; h++) {
-            const int rank = rank_of<BLOCK>(h);
+        for (int h = 0; h < S::PACKS; h++) {
+            const int rank = S::rank(h);
             if (!within[h])  // from the waves before, the nearest first
                 for (int w = (rank >> 6) - 1; w >= 0; w--) {
                     before[h] += tail[w];
                     if (marked[w])
                         break;
                 }
-            const bool next = rank + 1 == ALL || marks.at[min(rank + 1, ALL - 1) * kEach];
+            const bool next = rank + 1 == ALL || marks.at[min(rank + 1, ALL - 1) * S::EACH];
 #pragma unroll
-            for (int j = 0; j < kEach; j++) {
-                const bool ends = j + 1 < kEach ? mine[h] >> (j + 1) & 1 : next;
+            for (int j = 0; j < S::EACH; j++) {
+                const bool ends = j + 1 < S::EACH ? mine[h] >> (j + 1) & 1 : next;
                 if (ends)
-                    at[rank * kEach + j] =
+                    at[rank * S::EACH + j] =
                         mine[h] & ((2u << j) - 1) ? run[h][j] : before[h] + run[h][j];
             }
         }
@@ -1038,23 +1071,24 @@ template <class M>
 __device__ __forceinline__ void mark_sequence(M &marks, int first, int end)
 {
     marks.at[first] = 1;
-    if (end < M::ALL * kEach)
+    if (end < M::SIZE)
         marks.at[end] = 1;
 }
 
-__global__ __launch_bounds__(kBlock) void preference_sums(PreferenceArgs a, Pairs p, int chunks)
+__global__ __launch_bounds__(Wide::BLOCK) void preference_sums(PreferenceArgs a, Pairs p, int chunks)
 {
-    __shared__ Marks<kBlock, kPacks> marks;
-    __shared__ CountTable<kBlock, kPacks> table;
-    __shared__ Sums<kBlock, kPacks> sums;
+    typedef Wide S;
+    __shared__ Marks<S> marks;
+    __shared__ CountTable<S> table;
+    __shared__ Sums<S> sums;
     const Starts starts{a.starts, a.tokens};
     for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
-        const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
-        Sequences<kBlock, kPairsLook> q(starts, 2 * a.pairs, begin, end);
-        float v[kPacks][kEach];
+        const int begin = k * S::SIZE, end = end_of_chunk(begin, a.tokens);
+        Sequences<S::BLOCK, kPairsLook> q(starts, 2 * a.pairs, begin, end);
+        float v[S::PACKS][S::EACH];
 #pragma unroll
-        for (int h = 0; h < kPacks; h++) {
-            const Mine m = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
+        for (int h = 0; h < S::PACKS; h++) {
+            const Mine m = my_tokens<S>(a.mask, begin, end, S::rank(h));
             load_ratios(a, m, v[h]);
             table.scan(h, m.mask);
         }
@@ -1124,19 +1158,19 @@ __global__ __launch_bounds__(kJoinBlock) void preference_pairs(PreferenceArgs a,
 }
 
 // The tokens' gradients from what lies where their sequences begin.
-template <int BLOCK, int PACKS>
-__device__ __forceinline__ void store_gradients(const PreferenceArgs &a, const Mine (&m)[PACKS],
-                                                int from, int to, Marks<BLOCK, PACKS> &marks,
+template <class S>
+__device__ __forceinline__ void store_gradients(const PreferenceArgs &a, const Mine (&m)[S::PACKS],
+                                                int from, int to, Marks<S> &marks,
                                                 const double *seq, double u)
 {
-    int place[PACKS][kEach];
+    int place[S::PACKS][S::EACH];
     marks.places(place);
 #pragma unroll
-    for (int h = 0; h < PACKS; h++) {
-        const unsigned counted = m[h].mask & inside(m[h], from, to);
-        float g[kEach];
+    for (int h = 0; h < S::PACKS; h++) {
+        const unsigned counted = m[h].mask & inside<S>(m[h], from, to);
+        float g[S::EACH];
 #pragma unroll
-        for (int j = 0; j < kEach; j++) {
+        for (int j = 0; j < S::EACH; j++) {
             const float v = (float)(seq[max(place[h][j], 0)] * u);
             g[j] = counted >> j & 1 ? v : 0.f;
         }
@@ -1145,11 +1179,12 @@ __device__ __forceinline__ void store_gradients(const PreferenceArgs &a, const M
 }
 
 // The gradients; the workgroup behind those of the chunks adds the results.
-__global__ __launch_bounds__(kBlock) void preference_fill(PreferenceArgs a, Pairs p, int chunks,
+__global__ __launch_bounds__(Wide::BLOCK) void preference_fill(PreferenceArgs a, Pairs p, int chunks,
                                                           int joins)
 {
-    __shared__ Marks<kBlock, kPacks> marks;
-    __shared__ double seq[kChunk];
+    typedef Wide S;
+    __shared__ Marks<S> marks;
+    __shared__ double seq[S::SIZE];
     const Starts starts{a.starts, a.tokens};
     __shared__ double of_all;
     const unsigned groups = gridDim.x - 1;
@@ -1157,7 +1192,7 @@ __global__ __launch_bounds__(kBlock) void preference_fill(PreferenceArgs a, Pair
         of_all = 1.0 / max(sum_of(p.some, joins), 1);  // what all pairs are multiplied by
     if (blockIdx.x == groups) {
         const double u = 1.0 / max(sum_of(p.some, joins), 1);
-        for (int i = threadIdx.x >> 6; i < 5; i += kBlock / 64) {
+        for (int i = threadIdx.x >> 6; i < 5; i += S::BLOCK / 64) {
             const double v = sum_of(p.part + (size_t)i * joins, joins);
             if ((threadIdx.x & 63) == 0)
                 a.stats[i] = (float)(v * u);
@@ -1166,12 +1201,12 @@ __global__ __launch_bounds__(kBlock) void preference_fill(PreferenceArgs a, Pair
     }
     const int from = starts(0), to = starts(2LL * a.pairs);
     for (int k = blockIdx.x; k < chunks; k += groups) {
-        const int begin = k * kChunk, end = end_of_chunk(begin, a.tokens);
-        Sequences<kBlock, kPairsLook> q(starts, 2 * a.pairs, begin, end);
-        Mine m[kPacks];
+        const int begin = k * S::SIZE, end = end_of_chunk(begin, a.tokens);
+        Sequences<S::BLOCK, kPairsLook> q(starts, 2 * a.pairs, begin, end);
+        Mine m[S::PACKS];
 #pragma unroll
-        for (int h = 0; h < kPacks; h++)
-            m[h] = my_tokens(a.mask, begin, end, rank_of<kBlock>(h));
+        for (int h = 0; h < S::PACKS; h++)
+            m[h] = my_tokens<S>(a.mask, begin, end, S::rank(h));
         marks.clear();
         __syncthreads();
         q.each([&](long long s, int s0, int) {
@@ -1187,23 +1222,21 @@ __global__ __launch_bounds__(kBlock) void preference_fill(PreferenceArgs a, Pair
     }
 }
 
-constexpr int kOnePairs = 1024;
-
-__global__ __launch_bounds__(kOneBlock) void preference_one(PreferenceArgs a)
+template <class S>
+__global__ __launch_bounds__(S::BLOCK) void preference_one(PreferenceArgs a)
 {
-    constexpr int PACKS = kOnePacks;
-    __shared__ Marks<kOneBlock, PACKS> marks;
-    __shared__ CountTable<kOneBlock, PACKS> table;
-    __shared__ Sums<kOneBlock, PACKS> sums;
-    __shared__ double seq[kOneChunk];
-    __shared__ double red[kOneBlock / 64][6];
-    __shared__ int counts[kOneBlock / 64];
+    __shared__ Marks<S> marks;
+    __shared__ CountTable<S> table;
+    __shared__ Sums<S> sums;
+    __shared__ double seq[S::SIZE];
+    __shared__ double red[S::BLOCK / 64][6];
+    __shared__ int counts[S::BLOCK / 64];
     const Starts starts{a.starts, a.tokens};
-    Mine m[PACKS];
-    float v[PACKS][kEach];
+    Mine m[S::PACKS];
+    float v[S::PACKS][S::EACH];
 #pragma unroll
-    for (int h = 0; h < PACKS; h++) {
-        m[h] = my_tokens(a.mask, 0, a.tokens, rank_of<kOneBlock>(h));
+    for (int h = 0; h < S::PACKS; h++) {
+        m[h] = my_tokens<S>(a.mask, 0, a.tokens, S::rank(h));
         load_ratios(a, m[h], v[h]);
         table.scan(h, m[h].mask);
     }
@@ -1254,10 +1287,10 @@ __global__ __launch_bounds__(kOneBlock) void preference_one(PreferenceArgs a)
     __syncthreads();
     int all = 0;
 #pragma unroll
-    for (int w = 0; w < kOneBlock / 64; w++)
+    for (int w = 0; w < S::BLOCK / 64; w++)
         all += counts[w];
     const double u = 1.0 / max(all, 1);
-    block_totals<kOneBlock>(sum, red, [&](int k, double v) {
+    block_totals<S::BLOCK>(sum, red, [&](int k, double v) {
         if (k < 5)
             a.stats[k] = (float)(v * u);
     }, has);
@@ -1285,15 +1318,14 @@ int join_groups(long long n)
 // One workgroup.
 bool policy_is_small(long long tokens, long long seqs)
 {
-    return tokens <= kOneChunk && seqs <= kOneChunk;
+    return tokens <= Small::SIZE && seqs <= Small::SIZE;
 }
 
+// A thread a pair.
 bool preference_is_small(long long tokens, long long pairs)
 {
-    return tokens <= kOneChunk && pairs <= kOnePairs;
+    return tokens <= Small::SIZE && pairs <= Small::BLOCK;
 }
-
-static_assert(kOnePairs <= kOneBlock, "a thread a pair");
 
 // Arrays one after the other in the workspace, of 16 bytes' alignment.
 struct Arena {
@@ -1339,9 +1371,11 @@ template <bool SEQS, Ref REF>
 void policy_tokens(const PolicyArgs &a, const Counts *c, int groups, int joins, hipStream_t stream)
 {
     if (c)
-        policy_main<SEQS, REF><<<groups, kBlock, 0, stream>>>(a, *c, chunks_of(a.tokens), joins);
+        policy_main<SEQS, REF><<<groups, Narrow::BLOCK, 0, stream>>>(a, *c, chunks_of(a.tokens), joins);
+    else if (a.tokens <= SmallPolicy::SIZE)
+        policy_one<SmallPolicy, SEQS, REF><<<1, SmallPolicy::BLOCK, 0, stream>>>(a);
     else
-        policy_one<SEQS, REF><<<1, kOneBlock, 0, stream>>>(a);
+        policy_one<Small, SEQS, REF><<<1, Small::BLOCK, 0, stream>>>(a);
 }
 
 // The launch over the tokens: by chunks, or (c null) of one workgroup.
@@ -1377,7 +1411,7 @@ hipError_t launch_policy(const PolicyArgs &a, hipStream_t stream)
     const int chunks = chunks_of(a.tokens), groups = std::min(chunks, kMaxGroups);
     const int joins = join_groups(a.seqs);
     if (a.mask && a.mean != 2)
-        policy_count<<<groups, kBlock, 0, stream>>>(a, c, chunks);
+        policy_count<<<groups, Narrow::BLOCK, 0, stream>>>(a, c, chunks);
     if (a.mean == 1)
         policy_join<<<joins, kJoinBlock, 0, stream>>>(a, c);
     tokens(a, &c, groups, joins, stream);
@@ -1394,16 +1428,19 @@ size_t preference_ws(long long tokens, long long pairs)
 hipError_t launch_preference(const PreferenceArgs &a, hipStream_t stream)
 {
     if (preference_is_small(a.tokens, a.pairs)) {
-        preference_one<<<1, kOneBlock, 0, stream>>>(a);
+        if (a.tokens <= SmallPairs::SIZE && a.pairs <= SmallPairs::BLOCK)
+            preference_one<SmallPairs><<<1, SmallPairs::BLOCK, 0, stream>>>(a);
+        else
+            preference_one<Small><<<1, Small::BLOCK, 0, stream>>>(a);
         return hipGetLastError();
     }
     Pairs p;
     layout(p, a.ws, a.tokens, a.pairs);
     const int chunks = chunks_of(a.tokens), groups = std::min(chunks, kMaxGroups);
     const int joins = join_groups(a.pairs);
-    preference_sums<<<groups, kBlock, 0, stream>>>(a, p, chunks);
+    preference_sums<<<groups, Wide::BLOCK, 0, stream>>>(a, p, chunks);
     preference_pairs<<<joins, kJoinBlock, 0, stream>>>(a, p);
-    preference_fill<<<(a.dlogp ? groups : 0) + 1, kBlock, 0, stream>>>(a, p, chunks, joins);
+    preference_fill<<<(a.dlogp ? groups : 0) + 1, Wide::BLOCK, 0, stream>>>(a, p, chunks, joins);
     return hipGetLastError();
 }
 

@@ -77,7 +77,10 @@ def policy(logp, old, adv, by_sequence=False, ref=None, entropy=None, mask=None,
     exponential by 2 u, the clip's border and the products by 1 u each; x's rounding moves
     the divergence by its slope; the series' terms and additions cost 8 u of it, and
     from |x| = 1 on, where it is a difference, 4 u of the terms; each sum of the loss, the
-    weight 1 / n, its product and the last rounding 1 u."""
+    weight 1 / n and the last rounding 1 u.  A term joins the sum of at most eight tokens by
+    a fused product and addition in 32 bits, and passes the additions after it: at most
+    8 roundings, each of at most u times the absolute values added so far, so that all of
+    them cost at most 8 u of the terms' absolute values; what comes after is in 64 bits."""
     n = logp.numel()
     counted = torch.zeros(n, dtype=torch.bool)
     weight = torch.zeros(n, dtype=torch.float64)
@@ -134,16 +137,18 @@ def policy(logp, old, adv, by_sequence=False, ref=None, entropy=None, mask=None,
             size_l += abs(kl_weight) * (size_k + 2 * div.abs())
             size_g = size_g + abs(kl_weight) * (size_d + 2 * dslope.abs())
     h = zero
+    added = surrogate.abs() + abs(kl_weight) * div.abs()
     if entropy is not None:
         h = only(entropy)
         if entropy_weight:
             loss -= entropy_weight * h
             size_l += abs(entropy_weight) * 2 * h.abs()
-    parts = [(loss, size_l + 2 * loss.abs()), (surrogate, size_s), (div, size_k), (h, zero),
+            added = added + abs(entropy_weight) * h.abs()
+    parts = [(loss, size_l + 9 * added), (surrogate, size_s), (div, size_k), (h, zero),
              (ratio, ratio * (3 + d.abs())), (clipped.double(), zero)]
     w = lambda v: torch.where(counted, v * weight, zero)
     stats = torch.stack([w(v).sum() for v, _ in parts])
-    bounds = torch.stack([w(s + 2 * v.abs()).sum() for v, s in parts]) * U + U * stats.abs()
+    bounds = torch.stack([w(s + 9 * v.abs()).sum() for v, s in parts]) * U + U * stats.abs()
     g, gh = w(slope) * scale, w(torch.full_like(zero, -entropy_weight)) * scale
     return ((stats, bounds.nan_to_num(0, 0, 0) + 1e-40),
             (g, U * (abs(scale) * w(size_g) + 5 * g.abs()).nan_to_num(0, 0, 0) + 1e-40),

@@ -330,8 +330,8 @@ def check_policy(m, d, *args, **kw):
 
 @pytest.mark.parametrize("masked", [0.0, 0.4])
 @pytest.mark.parametrize("tokens,seqs,tail", [
-    (1, 1, 0), (2, 5, 0), (5, 1, 2), (63, 3, 0), (1000, 7, 13), (4099, 300, 0), (8192, 1, 0),
-    (8192, 8192, 0), (8193, 1, 0), (8193, 40, 5), (300, 9000, 7), (20001, 3, 0), (50003, 600, 77),
+    (1, 1, 0), (2, 5, 0), (5, 1, 2), (63, 3, 0), (1000, 7, 13), (4096, 4096, 0), (4097, 5, 0),
+    (4099, 300, 0), (8192, 1, 0), (8192, 8192, 0), (8193, 1, 0), (8193, 40, 5), (300, 9000, 7), (20001, 3, 0), (50003, 600, 77),
     (70000, 20000, 1)])
 def test_policy(tokens, seqs, tail, masked):
     """Both means, both kinds of advantage, all forms, with and without each part."""
@@ -491,8 +491,8 @@ def check_pairs(m, d, use_ref=True, **kw):
 
 @pytest.mark.parametrize("masked", [0.0, 0.4])
 @pytest.mark.parametrize("tokens,pairs,tail", [
-    (1, 1, 0), (2, 4, 0), (7, 2, 3), (100, 1, 0), (1000, 7, 13), (4099, 150, 0), (8192, 1, 0),
-    (8192, 1024, 0), (8193, 1, 0), (8193, 20, 5), (300, 1500, 7), (20001, 2, 0), (50003, 300, 77),
+    (1, 1, 0), (2, 4, 0), (7, 2, 3), (100, 1, 0), (1000, 7, 13), (4096, 512, 0), (900, 513, 0),
+    (4097, 5, 0), (4099, 150, 0), (8192, 1, 0), (8192, 1024, 0), (8193, 1, 0), (8193, 20, 5), (300, 1500, 7), (20001, 2, 0), (50003, 300, 77),
     (70000, 10000, 1)])
 def test_preference(tokens, pairs, tail, masked):
     import paper_1903_06934_amd as m

@@ -193,10 +193,10 @@ def test_preference_loss_takes(L, args):
 
 
 def test_workspace_sizes(L):
-    assert L.policy_loss_workspace_size(4096, 4096) == 0
-    assert L.policy_loss_workspace_size(4097, 1) > 0 and L.policy_loss_workspace_size(1, 4097) > 0
-    assert L.preference_loss_workspace_size(4096, 1024) == 0
-    assert L.preference_loss_workspace_size(4097, 1) > 0
+    assert L.policy_loss_workspace_size(8192, 8192) == 0
+    assert L.policy_loss_workspace_size(8193, 1) > 0 and L.policy_loss_workspace_size(1, 8193) > 0
+    assert L.preference_loss_workspace_size(8192, 1024) == 0
+    assert L.preference_loss_workspace_size(8193, 1) > 0
     assert L.preference_loss_workspace_size(1, 1025) > 0
     for bad in ((-1, 1), (1 << 31, 1), (1, -1), (1, 1 << 31)):
         assert L.policy_loss_workspace_size(*bad) == 0
