@@ -8,8 +8,12 @@
 
 namespace miconv {
 
-// Philox4x32-10 of the counter {g, step, layer}: ten rounds of two 32 x 32 -> 64
-// bit products, whose low words change places with the other two words.
+// Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2,
+// 3", 2011) of the counter {g, step, layer}: ten rounds of two 32 x 32 -> 64 bit products,
+// whose low words change places with the other two words.  Both halves of a product are
+// one instruction, at a quarter of the rate of others: some 20 of these and 60 others for
+// eight elements, which is half of what a CU can do while the memory moves 16-bit
+// elements in and out.
 __device__ __forceinline__ void philox(uint32_t key0, uint32_t key1, uint32_t step, uint32_t layer,
                                        unsigned long long g, uint32_t (&w)[4])
 {
