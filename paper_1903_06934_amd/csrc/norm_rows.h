@@ -164,15 +164,12 @@ __device__ __forceinline__ Drop drop_of(const A &a)
         return Drop{};
 }
 
-// The N elements v of a pack from element e on (in the order of their places, `left` >=
-// 1 of them in the row), dropped out.
+// The N elements v of a pack (in the order of their places, `left` >= 1 of them in the
+// row), dropped out by its words.
 template <int N>
-__device__ __forceinline__ void drop_pack(const Dropper &drop, long long e, int left, float (&v)[N])
+__device__ __forceinline__ void drop_pack(const Dropper &drop, const uint32_t (&w)[N / 2], int left,
+                                          float (&v)[N])
 {
-    if (!drop.below)
-        return;
-    uint32_t w[N / 2];
-    drop.words<N>(e, w);
     if (left >= N) {
 #pragma unroll
         for (int j = 0; j < N; j++)
@@ -220,13 +217,25 @@ __device__ __forceinline__ void add_branch(const ResidualFwdArgs &a, const Dropp
 #pragma unroll
         for (int i = i0; i < i0 + F && i < NV; i++) {
             const int c = (t + i * tpr) * N, left = TAIL ? N : cols - c;
+            uint32_t words[N / 2] = {};
+            if constexpr (N == 8)
+                if (drop.below) {
+                    if (tpr >= 64)  // a row has whole waves
+                        drop.words_of_wave(e + c, words);
+                    else
+                        drop.words<N>(e + c, words);
+                }
             if (left <= 0)
                 continue;
             float v[N];
 #pragma unroll
             for (int j = 0; j < N; j++)
                 v[j] = (float)raw[i][j];
-            drop_pack<N>(drop, e + c, left, v);
+            if (drop.below) {
+                if (N != 8)
+                    drop.words<N>(e + c, words);
+                drop_pack<N>(drop, words, left, v);
+            }
 #pragma unroll
             for (int j = 0; j < N; j++)
                 raw[i][j] = (T)((float)res[i - i0][j] + v[j]);
@@ -596,7 +605,11 @@ __device__ __forceinline__ void store_branch(const ResidualBwdArgs &a, const Dro
 #pragma unroll
     for (int j = 0; j < N; j++)
         d[j] = g[j];
-    drop_pack<N>(drop, row * a.cols + c, left, d);
+    if (drop.below) {
+        uint32_t words[N / 2];
+        drop.words<N>(row * a.cols + c, words);
+        drop_pack<N>(drop, words, left, d);
+    }
 #pragma unroll
     for (int j = 0; j < N; j++)
         v[j] = (T)d[j];
