@@ -773,7 +773,8 @@ __device__ __forceinline__ OfSequence of_sequence(const PolicyArgs &a, long long
 // The tokens' weights and advantages from what lies where their sequences begin.
 template <class S>
 __device__ __forceinline__ void from_sequences(const PolicyArgs &a, Marks<S> &marks,
-                                               const OfSequence *seq, Tokens<S::EACH> (&k)[S::PACKS],
+                                               const OfSequence *seq,
+                                               Tokens<S::EACH> (&k)[S::PACKS],
                                                float (&w)[S::PACKS][S::EACH])
 {
     int place[S::PACKS][S::EACH];
@@ -848,8 +849,9 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
     double sum[5] = {0, 0, 0, 0, 0};
 #pragma unroll
     for (int h = 0; h < S::PACKS; h++)
-        token_losses<SEQS, REF, S::EACH>(a, borders, m[h], k[h], m[h].mask & inside<S>(m[h], from, to), w[h],
-                                (float)(u * a.scale), sum);
+        token_losses<SEQS, REF, S::EACH>(a, borders, m[h], k[h],
+                                         m[h].mask & inside<S>(m[h], from, to), w[h],
+                                         (float)(u * a.scale), sum);
     block_totals<S::BLOCK>(sum, red, [&](int i, double v) { total[i] = v * u; }, counted);
     // The same wave has written them.
     if (threadIdx.x < 6)
@@ -912,8 +914,8 @@ __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Co
 #pragma unroll
         for (int h = 0; h < S::PACKS; h++)
             token_losses<SEQS, REF, S::EACH>(a, borders, m[h], tokens[h],
-                                    m[h].mask & inside<S>(m[h], from, to), w[h],
-                                    (float)(u * a.scale), sum);
+                                             m[h].mask & inside<S>(m[h], from, to), w[h],
+                                             (float)(u * a.scale), sum);
         if (SEQS)
             __syncthreads();
     }
@@ -1108,7 +1110,8 @@ __device__ __forceinline__ void mark_sequence(M &marks, int first, int end)
 // over the chunk in 64 bits, at whose places the sequences' threads look (2 000 003
 // tokens: 9.2 us for 18 MB; the scan's steps, six of them with 64-bit shuffles, take the
 // most).
-__global__ __launch_bounds__(Wide::BLOCK) void preference_sums(PreferenceArgs a, Pairs p, int chunks)
+__global__ __launch_bounds__(Wide::BLOCK) void preference_sums(PreferenceArgs a, Pairs p,
+                                                                int chunks)
 {
     typedef Wide S;
     __shared__ Marks<S> marks;
@@ -1215,8 +1218,8 @@ __device__ __forceinline__ void store_gradients(const PreferenceArgs &a, const M
 
 // The gradients; the workgroup behind those of the chunks adds the results (2 000 003
 // tokens: 6.5 us for 2 MB of mask and 8 MB written).
-__global__ __launch_bounds__(Wide::BLOCK) void preference_fill(PreferenceArgs a, Pairs p, int chunks,
-                                                          int joins)
+__global__ __launch_bounds__(Wide::BLOCK) void preference_fill(PreferenceArgs a, Pairs p,
+                                                                int chunks, int joins)
 {
     typedef Wide S;
     __shared__ Marks<S> marks;
@@ -1409,7 +1412,8 @@ template <bool SEQS, Ref REF>
 void policy_tokens(const PolicyArgs &a, const Counts *c, int groups, int joins, hipStream_t stream)
 {
     if (c)
-        policy_main<SEQS, REF><<<groups, Narrow::BLOCK, 0, stream>>>(a, *c, chunks_of(a.tokens), joins);
+        policy_main<SEQS, REF>
+            <<<groups, Narrow::BLOCK, 0, stream>>>(a, *c, chunks_of(a.tokens), joins);
     else if (a.tokens <= SmallPolicy::SIZE)
         policy_one<SmallPolicy, SEQS, REF><<<1, SmallPolicy::BLOCK, 0, stream>>>(a);
     else

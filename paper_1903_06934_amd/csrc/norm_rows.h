@@ -198,7 +198,10 @@ __device__ __forceinline__ void add_branch(const ResidualFwdArgs &a, const Dropp
     const long long e = row * a.cols;
     const float r1 = TAIL && last < cols ? (float)rr[last] : 0.f;
     // The stream's packs two at a time, for registers (3000 x 20480 fp32 235 us, eight at a
-    // time 263; 9000 x 4096 103 and 106).
+    // time 263; 9000 x 4096 103 and 106).  Random words of 16-bit elements before the branch
+    // past the row's end, so that they are computed while the loads are awaited (30000 x
+    // 300 f16 27.7 us, behind it 31.6; fp32, whose packs need twice as many words, behind it
+    // 103.6, before 106.3).
     constexpr int F = NV < 2 ? NV : 2;
 #pragma unroll
     for (int i0 = 0; i0 < NV; i0 += F) {
@@ -1254,9 +1257,9 @@ int row_chunks(int xtype, long long rows, long long cols)
 }
 
 // Workgroups of the forward kernel for branches: as many as the CUs hold at once, which
-// its registers decide, so that none begins late (16384 x 4096 bf16, 1280 threads a CU:
-// 97 us; with 1024 and 1536 106 and 122. 9000 x 4096 fp32, 1024: 106; with 1280 126.
-// 8192 x 5120 bf16 by workgroups of five waves, three a CU 71, four 100).
+// its registers decide, so that none begins late (16384 x 4096 bf16, 1280 threads a CU: 95
+// us; with 1024 and 1536 104 and 119. 9000 x 4096 fp32, 1024: 103; with 768 and 1280 109 and
+// 127. 8192 x 5120 bf16 by workgroups of five waves, three a CU 72, two 90, four 99).
 template <auto KERNEL>
 int resident_blocks(const RowPlan &p, long long rows)
 {

@@ -100,7 +100,8 @@ struct Dropper {
     {
         group((unsigned long long)e >> 3, out);
         const unsigned low = __builtin_amdgcn_readfirstlane((unsigned)e);
-        const unsigned high = __builtin_amdgcn_readfirstlane((unsigned)((unsigned long long)e >> 32));
+        const unsigned high =
+            __builtin_amdgcn_readfirstlane((unsigned)((unsigned long long)e >> 32));
         if (low % 8 == 0)
             return;
         uint32_t s[4], w[8];

@@ -5,11 +5,11 @@
 //
 // Forward x and the residual are read, total and y written; backward dy, total and the
 // stream's gradient are read, that of the branch and of the residual written, which are
-// one tensor where nothing is dropped.  Bound by memory (16384 x 4096 bf16: forward 96.7
-// us for 537 MB, 5.6 TB/s, as by launches of their own 64.7 and 47; backward 132 for 671 MB
-// and 34 MB of partial sums, 5.3 TB/s), rows of few elements a thread by the loads they
-// wait for (12544 x 513 fp32 backward 25.7 us, a copy of as many bytes 21), few rows by
-// latencies (4 x 2048 bf16 forward 4.1).
+// one tensor where nothing is dropped.  Bound by memory (16384 x 4096 bf16: forward 94.1
+// us for 537 MB, 5.7 TB/s, the sum and the norm by launches of their own 64.7 and 47;
+// backward 132 for 671 MB and 34 MB of partial sums, 5.3 TB/s), rows of few elements a
+// thread by the loads they wait for (12544 x 513 fp32 backward 25.7 us, a copy of as many
+// bytes 21), few rows by latencies (4 x 2048 bf16 forward 4.0).
 // total is rounded to its type before its statistics are taken, so that the backward
 // pass, which reads it, has the same numbers.
 #include "norm_rows.h"
