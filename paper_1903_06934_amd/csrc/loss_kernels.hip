@@ -15,7 +15,7 @@
 // pair's loss the sums of both its sequences, before the first gradient: that is what
 // the launches are for.  Over the tokens there are two, which read the mask twice and
 // everything else once; the others are over sequences, or join partial sums.  2 000 003
-// tokens move 50 MB for a policy, in 24.7 us, and 26 MB for pairs, in 20.2: the launches
+// tokens move 50 MB for a policy, in 24.1 us, and 26 MB for pairs, in 20.4: the launches
 // over the tokens run at 3 to 4 TB/s (what they read lies in the last-level cache, and
 // each thread has one pack of it), launches and their gaps take the rest.  Up to some
 // 100 000 tokens there is nothing but latency: 3 to 4 us a launch (28 000 tokens in 13 to
@@ -276,6 +276,8 @@ struct Sequences {
     }
 };
 
+__device__ __forceinline__ int from_lane(int v, int lane) { return __shfl(v, lane); }
+
 // What chunks left of a sequence.
 template <class V>
 struct Pieces {
@@ -288,40 +290,45 @@ struct Pieces {
     }
 };
 
-// The sum of a sequence's pieces (of the tokens s0 <= t < s1), for the sequence s of
-// each lane that has one, else 0.  Those of up to kFew chunks are added by their lane, of
-// loads that are all issued at once, the others by the wave, one by one.
+// The sum of the pieces of a sequence (of the tokens s0 <= t < s1), for the sequence s that
+// each group of `lanes` lanes (a power of two) has, else 0; in all its lanes.  Those of up
+// to kFew chunks a lane are added by their group, of loads that are all issued at once,
+// the others by the wave, one by one.
 constexpr int kFew = 4;
 
 template <class V>
-__device__ __forceinline__ V join(bool has, const Pieces<V> &p, long long s, int s0, int s1)
+__device__ __forceinline__ V join(bool has, const Pieces<V> &p, long long s, int s0, int s1,
+                                  int lanes)
 {
+    const int lane = threadIdx.x & 63, own = lane & (lanes - 1);
     has = has && s0 < s1;
     const int from = has ? s0 / kChunk : 0, to = has ? (s1 - 1) / kChunk : 0, n = to - from;
-    V part[kFew];
-    part[0] = *(n ? p.tail + from : p.seq + (has ? s : 0));
+    const bool few = n < kFew * lanes;
+    V part[kFew], v{};
+    part[0] = *(own ? p.head + min(from + own, to) : n ? p.tail + from : p.seq + (has ? s : 0));
 #pragma unroll
     for (int i = 1; i < kFew; i++)
-        part[i] = p.head[min(from + i, to)];
-    V v{};
-    if (has && n < kFew) {
+        part[i] = p.head[min(from + own + i * lanes, to)];
+    if (has && few && own <= n) {
         v = part[0];
 #pragma unroll
         for (int i = 1; i < kFew; i++)
-            if (i <= n)
+            if (own + i * lanes <= n)
                 v += part[i];
     }
-    unsigned long long many = __ballot(has && n >= kFew);
+    for (int o = 1; o < lanes; o <<= 1)
+        v += from_lane(v, lane ^ o);
+    unsigned long long many = __ballot(has && !few && !own);
     while (many) {
-        const int lane = __builtin_ctzll(many);
+        const int at = __builtin_ctzll(many);
         many &= many - 1;
-        const int f = __shfl(from, lane), t = __shfl(to, lane);
+        const int f = __shfl(from, at), t = __shfl(to, at);
         V sum{};
 #pragma unroll 4
-        for (int k = f + (int)(threadIdx.x & 63); k <= t; k += 64)
+        for (int k = f + lane; k <= t; k += 64)
             sum += k == f ? p.tail[k] : p.head[k];
         sum = wave_sum(sum);
-        if ((int)(threadIdx.x & 63) == lane)
+        if ((lane ^ at) < lanes)
             v = sum;
     }
     return v;
@@ -558,25 +565,27 @@ __global__ __launch_bounds__(Narrow::BLOCK) void policy_count(PolicyArgs a, Coun
 // the latency of starts, then of their pieces).
 constexpr int kJoinBlock = 256;
 
-__global__ __launch_bounds__(kJoinBlock) void policy_join(PolicyArgs a, Counts c)
+__global__ __launch_bounds__(kJoinBlock) void policy_join(PolicyArgs a, Counts c, int lanes)
 {
     __shared__ int red[kJoinBlock / 64][1];
     const Starts starts{a.starts, a.tokens};
+    const int each = kJoinBlock / lanes;
+    const bool leads = (threadIdx.x & (lanes - 1)) == 0;
     int some[1] = {0};
-    for (long long first = (long long)blockIdx.x * kJoinBlock; first < a.seqs;
-         first += (long long)gridDim.x * kJoinBlock) {
-        const long long s = first + threadIdx.x;
+    for (long long first = (long long)blockIdx.x * each; first < a.seqs;
+         first += (long long)gridDim.x * each) {
+        const long long s = first + threadIdx.x / lanes;
         const bool has = s < a.seqs;
         int s0 = 0, s1 = 0;
         if (has)
             starts.of(s, s0, s1);
         int n = max(s1 - s0, 0);
         if (a.mask) {
-            n = join(has, c.n, s, s0, s1);
-            if (has)
+            n = join(has, c.n, s, s0, s1, lanes);
+            if (has && leads)
                 c.n.seq[s] = n;
         }
-        some[0] += n > 0;
+        some[0] += leads && n > 0;
     }
     block_totals<kJoinBlock>(some, red, [&](int, int v) { c.some[blockIdx.x] = v; });
 }
@@ -859,8 +868,8 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
 }
 
 // The losses and gradients of a workgroup's chunks (2 000 003 tokens, 1024 sequences: 13.6
-// us for 34 MB read and 16 written, 3.7 TB/s).  About 100 instructions a token, of it two
-// exponentials; by 128 registers four workgroups a CU hide their loads behind each
+// us for 34 MB read and 16 written, 3.7 TB/s).  Some 150 vector instructions a token, of it
+// two exponentials; by 128 registers four workgroups a CU hide their loads behind each
 // other's arithmetic (by 219, two packs' loads and losses at once, two of them: 33 us in
 // all; the few registers that two of the forms spill cost nothing that shows).
 template <bool SEQS, Ref REF>
@@ -953,6 +962,11 @@ struct Piece {
 __device__ __forceinline__ Piece wave_sum(const Piece &p)
 {
     return Piece{wave_sum(p.sum), wave_sum((int)p.n)};
+}
+
+__device__ __forceinline__ Piece from_lane(const Piece &p, int lane)
+{
+    return Piece{__shfl(p.sum, lane), __shfl((int)p.n, lane)};
 }
 
 // What a call of many tokens keeps between its launches.
@@ -1108,8 +1122,7 @@ __device__ __forceinline__ void mark_sequence(M &marks, int first, int end)
 
 // The sums of log ratios and the counts of each sequence, or its pieces: a segmented scan
 // over the chunk in 64 bits, at whose places the sequences' threads look (2 000 003
-// tokens: 9.2 us for 18 MB; the scan's steps, six of them with 64-bit shuffles, take the
-// most).
+// tokens: 9.2 us for 18 MB, 74 vector instructions a token).
 __global__ __launch_bounds__(Wide::BLOCK) void preference_sums(PreferenceArgs a, Pairs p,
                                                                 int chunks)
 {
@@ -1147,14 +1160,16 @@ __global__ __launch_bounds__(Wide::BLOCK) void preference_sums(PreferenceArgs a,
 
 // A thread a pair: its rewards and loss (3.8 us for 1024, the latency of starts, pieces, an
 // exponential and a logarithm in 64 bits).
-__global__ __launch_bounds__(kJoinBlock) void preference_pairs(PreferenceArgs a, Pairs p)
+__global__ __launch_bounds__(kJoinBlock) void preference_pairs(PreferenceArgs a, Pairs p, int lanes)
 {
     __shared__ double red[kJoinBlock / 64][6];
     const Starts starts{a.starts, a.tokens};
     double sum[6] = {0, 0, 0, 0, 0, 0};  // the results, and how many pairs they are of
-    for (long long first = (long long)blockIdx.x * kJoinBlock; first < a.pairs;
-         first += (long long)gridDim.x * kJoinBlock) {
-        const long long i = first + threadIdx.x;
+    const int each = kJoinBlock / lanes;
+    const bool leads = (threadIdx.x & (lanes - 1)) == 0;
+    for (long long first = (long long)blockIdx.x * each; first < a.pairs;
+         first += (long long)gridDim.x * each) {
+        const long long i = first + threadIdx.x / lanes;
         const bool has = i < a.pairs;
         int s0[2], s1[2];
         Piece v[2];
@@ -1166,8 +1181,9 @@ __global__ __launch_bounds__(kJoinBlock) void preference_pairs(PreferenceArgs a,
         }
 #pragma unroll
         for (int k = 0; k < 2; k++)
-            v[k] = join(has, p.sum, i + (long long)k * a.pairs, s0[k], s1[k]);
-        if (!has)
+            v[k] = join(has, p.sum, i + (long long)k * a.pairs, s0[k], s1[k],
+                        lanes);
+        if (!has || !leads)
             continue;
         double r[2];
 #pragma unroll
@@ -1350,10 +1366,21 @@ __global__ __launch_bounds__(S::BLOCK) void preference_one(PreferenceArgs a)
 // ---------------------------------------------------------------- launch rules
 int chunks_of(long long tokens) { return (int)std::max(1LL, (tokens + kChunk - 1) / kChunk); }
 
-// A thread a sequence or pair.
-int join_groups(long long n)
+// Lanes for a sequence: some two for each of its chunks, on an average, up to a wave (2 199
+// 573 tokens of 58 pairs: 22.6 us, with one lane 56.0; 1 015 210 of 174 15.9 and 20.1).
+int join_lanes(int chunks, long long seqs)
 {
-    return (int)std::max(1LL, std::min((n + kJoinBlock - 1) / kJoinBlock, (long long)kJoinGroups));
+    int lanes = 1;
+    while (lanes < 64 && lanes * seqs <= 2LL * chunks)
+        lanes *= 2;
+    return lanes;
+}
+
+// `lanes` lanes a sequence or pair.
+int join_groups(long long n, int lanes)
+{
+    const long long all = n * lanes;
+    return (int)std::max(1LL, std::min((all + kJoinBlock - 1) / kJoinBlock, (long long)kJoinGroups));
 }
 
 // One workgroup.
@@ -1451,11 +1478,11 @@ hipError_t launch_policy(const PolicyArgs &a, hipStream_t stream)
     Counts c;
     layout(c, a.ws, a.tokens, a.seqs);
     const int chunks = chunks_of(a.tokens), groups = std::min(chunks, kMaxGroups);
-    const int joins = join_groups(a.seqs);
+    const int lanes = a.mask ? join_lanes(chunks, a.seqs) : 1, joins = join_groups(a.seqs, lanes);
     if (a.mask && a.mean != 2)
         policy_count<<<groups, Narrow::BLOCK, 0, stream>>>(a, c, chunks);
     if (a.mean == 1)
-        policy_join<<<joins, kJoinBlock, 0, stream>>>(a, c);
+        policy_join<<<joins, kJoinBlock, 0, stream>>>(a, c, lanes);
     tokens(a, &c, groups, joins, stream);
     policy_stats<<<1, 5 * 64, 0, stream>>>(a, c.part, groups);
     return hipGetLastError();
@@ -1479,9 +1506,9 @@ hipError_t launch_preference(const PreferenceArgs &a, hipStream_t stream)
     Pairs p;
     layout(p, a.ws, a.tokens, a.pairs);
     const int chunks = chunks_of(a.tokens), groups = std::min(chunks, kMaxGroups);
-    const int joins = join_groups(a.pairs);
+    const int lanes = join_lanes(chunks, 2LL * a.pairs), joins = join_groups(a.pairs, lanes);
     preference_sums<<<groups, Wide::BLOCK, 0, stream>>>(a, p, chunks);
-    preference_pairs<<<joins, kJoinBlock, 0, stream>>>(a, p);
+    preference_pairs<<<joins, kJoinBlock, 0, stream>>>(a, p, lanes);
     preference_fill<<<(a.dlogp ? groups : 0) + 1, Wide::BLOCK, 0, stream>>>(a, p, chunks, joins);
     return hipGetLastError();
 }

@@ -506,6 +506,23 @@ def test_preference(tokens, pairs, tail, masked):
     check_pairs(m, d, use_ref=False, beta=1.0, smoothing=1.0, length_mean=True)
 
 
+@pytest.mark.parametrize("lengths", [
+    [75001, 0, 75000, 64, 2047, 2048], [250000] + 41 * [1000], 150 * [7] + [250001] + 149 * [300],
+    [8192] * 40, [1, 300000]], ids=lambda v: f"{len(v)}x{max(v)}")
+def test_long_sequences(lengths):
+    """Sequences of many chunks of tokens, alone and among short ones."""
+    import paper_1903_06934_amd as m
+    n, seqs = sum(lengths), len(lengths)
+    starts = torch.tensor([0] + lengths).cumsum(0)
+    d = dict(make_policy(gen(n, seqs, 3), n, seqs, 0, 0.2), starts=starts)
+    check_policy(m, d, True, "low", True, "sequences")
+    d = dict(make_pairs(gen(n, seqs, 4), n, seqs // 2, 0, 0.2), starts=starts)
+    check_pairs(m, d, beta=0.1, smoothing=0.1, length_mean=True)
+    d.pop("mask")
+    d["logp"], d["ref"] = d["logp"].nan_to_num(-1.0), d["ref"].nan_to_num(0, 0, -0.5)
+    check_pairs(m, d, beta=0.002, form="squared")
+
+
 @pytest.mark.parametrize("tokens", [0, 1, 700, 9000])
 def test_preference_nothing_counts(tokens):
     import paper_1903_06934_amd as m
