@@ -14,12 +14,13 @@
 // A weight needs its sequence's (or the call's) number of tokens that count, and a
 // pair's loss the sums of both its sequences, before the first gradient: that is what
 // the launches are for.  Over the tokens there are two, which read the mask twice and
-// everything else once; the others are over sequences, or join partial sums.  2 000 003
+// everything else once; the others are over sequences (unless these are few), or join
+// partial sums.  2 000 003
 // tokens move 50 MB for a policy, in 24.1 us, and 26 MB for pairs, in 20.4: the launches
 // over the tokens run at 3 to 4 TB/s (what they read lies in the last-level cache, and
 // each thread has one pack of it), launches and their gaps take the rest.  Up to some
-// 100 000 tokens there is nothing but latency: 3 to 4 us a launch (28 000 tokens in 13 to
-// 16 us), 5 to 11 for one workgroup's chain of loads, scans, exponentials and sums.
+// 100 000 tokens there is nothing but latency: 3 to 4 us a launch (20 000 to 100 000 tokens in
+// 10 to 16 us), 5 to 11 for one workgroup's chain of loads, scans, exponentials and sums.
 #include <algorithm>
 
 #include "internal.h"
@@ -56,6 +57,8 @@ typedef Tile<512, 1, 8> SmallPairs;
 typedef Tile<1024, 1, 8> Small;
 constexpr int kMaxGroups = 1024;  // workgroups of a launch over the chunks, and partial sums
 constexpr int kJoinGroups = 1024;  // of a launch over the sequences
+constexpr int kOwn = 256;  // sequences or pairs that a workgroup over the tokens joins itself
+static_assert(kOwn <= Wide::BLOCK && kOwn <= Narrow::BLOCK, "a thread each");
 
 typedef Pack<float>::V F4;
 
@@ -561,6 +564,17 @@ __global__ __launch_bounds__(Narrow::BLOCK) void policy_count(PolicyArgs a, Coun
     block_totals<S::BLOCK>(all, red, [&](int, int v) { c.group[blockIdx.x] = v; });
 }
 
+// The tokens that count of the sequence s that a group of lanes has, else 0.
+__device__ __forceinline__ int sequence_tokens(const PolicyArgs &a, const Counts &c,
+                                               const Starts &starts, long long s, bool has,
+                                               int lanes)
+{
+    int s0 = 0, s1 = 0;
+    if (has)
+        starts.of(s, s0, s1);
+    return a.mask ? join(has, c.n, s, s0, s1, lanes) : max(s1 - s0, 0);
+}
+
 // Each sequence's tokens that count, and how many sequences have any (2.8 us for 1024:
 // the latency of starts, then of their pieces).
 constexpr int kJoinBlock = 256;
@@ -576,15 +590,9 @@ __global__ __launch_bounds__(kJoinBlock) void policy_join(PolicyArgs a, Counts c
          first += (long long)gridDim.x * each) {
         const long long s = first + threadIdx.x / lanes;
         const bool has = s < a.seqs;
-        int s0 = 0, s1 = 0;
-        if (has)
-            starts.of(s, s0, s1);
-        int n = max(s1 - s0, 0);
-        if (a.mask) {
-            n = join(has, c.n, s, s0, s1, lanes);
-            if (has && leads)
-                c.n.seq[s] = n;
-        }
+        const int n = sequence_tokens(a, c, starts, s, has, lanes);
+        if (a.mask && has && leads)
+            c.n.seq[s] = n;
         some[0] += leads && n > 0;
     }
     block_totals<kJoinBlock>(some, red, [&](int, int v) { c.some[blockIdx.x] = v; });
@@ -872,11 +880,13 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
 // two exponentials; by 128 registers four workgroups a CU hide their loads behind each
 // other's arithmetic (by 219, two packs' loads and losses at once, two of them: 33 us in
 // all; the few registers that two of the forms spill cost nothing that shows).
-template <bool SEQS, Ref REF>
+// OWN: all sequences are joined here, by `lanes` lanes each.
+template <bool SEQS, bool OWN, Ref REF>
 __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Counts c, int chunks,
-                                                             int joins)
+                                                             int joins, int lanes)
 {
     typedef Narrow S;
+    __shared__ int n_of[OWN ? S::BLOCK : 1], some[S::BLOCK / 64][1];
     __shared__ Marks<std::conditional_t<SEQS, S, Tile<64, 1, 4>>> marks;
     __shared__ OfSequence seq[SEQS ? S::SIZE : 1];
     __shared__ double red[S::BLOCK / 64][5], of_all;
@@ -884,7 +894,18 @@ __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Co
     const Borders borders(a);
     double u = 0.0, sum[5] = {0, 0, 0, 0, 0};
     const int from = a.starts ? starts(0) : 0, to = a.starts ? starts(a.seqs) : a.tokens;
-    if (threadIdx.x < 64) {  // what all weights are multiplied by
+    if constexpr (OWN) {
+        const int s = threadIdx.x / lanes;
+        const bool has = s < a.seqs, leads = (threadIdx.x & (lanes - 1)) == 0;
+        int n[1];
+        n[0] = sequence_tokens(a, c, starts, s, has, lanes);
+        if (leads)
+            n_of[s] = n[0];
+        n[0] = leads && n[0] > 0;
+        block_sums<S::BLOCK>(n, some);
+        if (threadIdx.x == 0)
+            of_all = 1.0 / max(n[0], 1);
+    } else if (threadIdx.x < 64) {  // what all weights are multiplied by
         double n = a.count;
         if (a.mean == 1)
             n = max(sum_of(c.some, joins), 1);
@@ -911,8 +932,13 @@ __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Co
             __syncthreads();
             q.each([&](long long s, int s0, int s1) {
                 const int at = max(s0, begin) - begin;
+                int n = s1 - s0;
+                if constexpr (OWN)
+                    n = n_of[s];
+                else if (a.mean == 1 && a.mask)
+                    n = c.n.seq[s];
                 marks.at[at] = 1;
-                seq[at] = of_sequence(a, s, a.mean != 1 ? 1 : a.mask ? c.n.seq[s] : s1 - s0);
+                seq[at] = of_sequence(a, s, n);
             });
         }
         if (SEQS || k == (int)blockIdx.x)
@@ -1158,6 +1184,36 @@ __global__ __launch_bounds__(Wide::BLOCK) void preference_sums(PreferenceArgs a,
     }
 }
 
+// What a group of lanes gets of its pair.
+struct Joined {
+    Piece v[2];  // of both sequences
+    double r[2];
+    Pair q;
+    bool some;  // has a token
+};
+
+__device__ __forceinline__ Joined join_pair(const PreferenceArgs &a, const Pairs &p,
+                                            const Starts &starts, long long i, bool has, int lanes)
+{
+    Joined o;
+    int s0[2], s1[2];
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        s0[k] = s1[k] = 0;
+        if (has)
+            starts.of(i + (long long)k * a.pairs, s0[k], s1[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+        o.v[k] = join(has, p.sum, i + (long long)k * a.pairs, s0[k], s1[k], lanes);
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+        o.r[k] = reward(a, o.v[k].sum, (int)o.v[k].n);
+    o.q = pair_loss(a, o.r[0], o.r[1]);
+    o.some = o.v[0].n + o.v[1].n > 0;
+    return o;
+}
+
 // A thread a pair: its rewards and loss (3.8 us for 1024, the latency of starts, pieces, an
 // exponential and a logarithm in 64 bits).
 __global__ __launch_bounds__(kJoinBlock) void preference_pairs(PreferenceArgs a, Pairs p, int lanes)
@@ -1171,35 +1227,21 @@ __global__ __launch_bounds__(kJoinBlock) void preference_pairs(PreferenceArgs a,
          first += (long long)gridDim.x * each) {
         const long long i = first + threadIdx.x / lanes;
         const bool has = i < a.pairs;
-        int s0[2], s1[2];
-        Piece v[2];
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            s0[k] = s1[k] = 0;
-            if (has)
-                starts.of(i + (long long)k * a.pairs, s0[k], s1[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < 2; k++)
-            v[k] = join(has, p.sum, i + (long long)k * a.pairs, s0[k], s1[k],
-                        lanes);
+        const Joined o = join_pair(a, p, starts, i, has, lanes);
         if (!has || !leads)
             continue;
-        double r[2];
 #pragma unroll
         for (int k = 0; k < 2; k++) {
             const long long s = i + (long long)k * a.pairs;
-            r[k] = reward(a, v[k].sum, (int)v[k].n);
-            p.sum.seq[s] = v[k];
+            p.sum.seq[s] = o.v[k];
             if (a.rewards)
-                a.rewards[s] = (float)r[k];
+                a.rewards[s] = (float)o.r[k];
         }
-        const Pair q = pair_loss(a, r[0], r[1]);
-        p.slope[i] = q.slope;
-        if (v[0].n + v[1].n > 0) {
+        p.slope[i] = o.q.slope;
+        if (o.some) {
 #pragma unroll
             for (int k = 0; k < 5; k++)
-                sum[k] += q.stats[k];
+                sum[k] += o.q.stats[k];
             sum[5] += 1;
         }
     }
@@ -1234,25 +1276,58 @@ __device__ __forceinline__ void store_gradients(const PreferenceArgs &a, const M
 
 // The gradients; the workgroup behind those of the chunks adds the results (2 000 003
 // tokens: 6.5 us for 2 MB of mask and 8 MB written).
+// OWN: all pairs are joined here, by `lanes` lanes each.
+template <bool OWN>
 __global__ __launch_bounds__(Wide::BLOCK) void preference_fill(PreferenceArgs a, Pairs p,
-                                                                int chunks, int joins)
+                                                                int chunks, int joins, int lanes)
 {
     typedef Wide S;
+    __shared__ double slope_of[OWN ? S::BLOCK : 1], red[S::BLOCK / 64][5];
+    __shared__ int n_of[2][OWN ? S::BLOCK : 1], some[S::BLOCK / 64][1];
     __shared__ Marks<S> marks;
     __shared__ double seq[S::SIZE];
     const Starts starts{a.starts, a.tokens};
     __shared__ double of_all;
     const unsigned groups = gridDim.x - 1;
-    if (threadIdx.x < 64)
-        of_all = 1.0 / max(sum_of(p.some, joins), 1);  // what all pairs are multiplied by
-    if (blockIdx.x == groups) {
-        const double u = 1.0 / max(sum_of(p.some, joins), 1);
-        for (int i = threadIdx.x >> 6; i < 5; i += S::BLOCK / 64) {
-            const double v = sum_of(p.part + (size_t)i * joins, joins);
-            if ((threadIdx.x & 63) == 0)
-                a.stats[i] = (float)(v * u);
+    if constexpr (OWN) {
+        const int i = threadIdx.x / lanes;
+        const bool has = i < a.pairs, leads = (threadIdx.x & (lanes - 1)) == 0;
+        const Joined o = join_pair(a, p, starts, i, has, lanes);
+        const bool counts = has && leads && o.some;
+        if (leads) {
+            slope_of[i] = o.q.slope;
+            n_of[0][i] = (int)o.v[0].n;
+            n_of[1][i] = (int)o.v[1].n;
         }
-        return;
+        int n[1] = {counts};
+        block_sums<S::BLOCK>(n, some);
+        const double u = 1.0 / max(n[0], 1);
+        if (threadIdx.x == 0)
+            of_all = u;
+        if (blockIdx.x == groups) {
+            if (a.rewards && has && leads)
+#pragma unroll
+                for (int k = 0; k < 2; k++)
+                    a.rewards[i + (long long)k * a.pairs] = (float)o.r[k];
+            double sum[5];
+#pragma unroll
+            for (int k = 0; k < 5; k++)
+                sum[k] = counts ? o.q.stats[k] : 0.0;
+            block_totals<S::BLOCK>(sum, red, [&](int k, double v) { a.stats[k] = (float)(v * u); });
+            return;
+        }
+    } else {
+        if (threadIdx.x < 64)
+            of_all = 1.0 / max(sum_of(p.some, joins), 1);  // what all pairs are multiplied by
+        if (blockIdx.x == groups) {
+            const double u = 1.0 / max(sum_of(p.some, joins), 1);
+            for (int i = threadIdx.x >> 6; i < 5; i += S::BLOCK / 64) {
+                const double v = sum_of(p.part + (size_t)i * joins, joins);
+                if ((threadIdx.x & 63) == 0)
+                    a.stats[i] = (float)(v * u);
+            }
+            return;
+        }
     }
     const int from = starts(0), to = starts(2LL * a.pairs);
     for (int k = blockIdx.x; k < chunks; k += groups) {
@@ -1267,9 +1342,18 @@ __global__ __launch_bounds__(Wide::BLOCK) void preference_fill(PreferenceArgs a,
         q.each([&](long long s, int s0, int) {
             const bool second = s >= a.pairs;
             const int at = max(s0, begin) - begin;
+            const long long i = second ? s - a.pairs : s;
+            double slope;
+            int n;
+            if constexpr (OWN) {
+                slope = slope_of[i];
+                n = n_of[second][i];
+            } else {
+                slope = p.slope[i];
+                n = (int)p.sum.seq[s].n;
+            }
             marks.at[at] = 1;
-            seq[at] = pair_gradient(a, p.slope[second ? s - a.pairs : s], second,
-                                    (int)p.sum.seq[s].n);
+            seq[at] = pair_gradient(a, slope, second, n);
         });
         __syncthreads();
         store_gradients(a, m, from, to, marks, seq, of_all);
@@ -1383,6 +1467,19 @@ int join_groups(long long n, int lanes)
     return (int)std::max(1LL, std::min((all + kJoinBlock - 1) / kJoinBlock, (long long)kJoinGroups));
 }
 
+// So few sequences or pairs that every workgroup of the launch over the tokens joins all of
+// them itself, which saves a launch: lanes for each, else 0; at least half of what a launch
+// of their own would give them (158 508 tokens of 199 pairs 11.6 us, with that launch 13.9; 42
+// 011 of a policy's 45 sequences 14.4 and 16.2; 2 468 375 of 79 pairs, by two lanes instead
+// of 16, 41.3 and 24.0).
+int own_lanes(long long n, int lanes)
+{
+    int own = 64;
+    while (own * n > kOwn)
+        own /= 2;
+    return 2 * own < lanes ? 0 : own;
+}
+
 // One workgroup.
 bool policy_is_small(long long tokens, long long seqs)
 {
@@ -1435,12 +1532,13 @@ size_t layout(Pairs &p, void *ws, long long tokens, long long pairs)
     return a.used;
 }
 
-template <bool SEQS, Ref REF>
-void policy_tokens(const PolicyArgs &a, const Counts *c, int groups, int joins, hipStream_t stream)
+template <bool SEQS, bool OWN, Ref REF>
+void policy_tokens(const PolicyArgs &a, const Counts *c, int groups, int joins, int lanes,
+                   hipStream_t stream)
 {
     if (c)
-        policy_main<SEQS, REF>
-            <<<groups, Narrow::BLOCK, 0, stream>>>(a, *c, chunks_of(a.tokens), joins);
+        policy_main<SEQS, OWN, REF>
+            <<<groups, Narrow::BLOCK, 0, stream>>>(a, *c, chunks_of(a.tokens), joins, lanes);
     else if (a.tokens <= SmallPolicy::SIZE)
         policy_one<SmallPolicy, SEQS, REF><<<1, SmallPolicy::BLOCK, 0, stream>>>(a);
     else
@@ -1448,15 +1546,16 @@ void policy_tokens(const PolicyArgs &a, const Counts *c, int groups, int joins, 
 }
 
 // The launch over the tokens: by chunks, or (c null) of one workgroup.
-template <bool SEQS>
-void policy_tokens(const PolicyArgs &a, const Counts *c, int groups, int joins, hipStream_t stream)
+template <bool SEQS, bool OWN>
+void policy_tokens(const PolicyArgs &a, const Counts *c, int groups, int joins, int lanes,
+                   hipStream_t stream)
 {
     if (!a.ref_logp)
-        policy_tokens<SEQS, Ref::none>(a, c, groups, joins, stream);
+        policy_tokens<SEQS, OWN, Ref::none>(a, c, groups, joins, lanes, stream);
     else if (a.kl == 2)
-        policy_tokens<SEQS, Ref::low>(a, c, groups, joins, stream);
+        policy_tokens<SEQS, OWN, Ref::low>(a, c, groups, joins, lanes, stream);
     else
-        policy_tokens<SEQS, Ref::other>(a, c, groups, joins, stream);
+        policy_tokens<SEQS, OWN, Ref::other>(a, c, groups, joins, lanes, stream);
 }
 
 }  // namespace
@@ -1470,20 +1569,23 @@ size_t policy_ws(long long tokens, long long seqs)
 hipError_t launch_policy(const PolicyArgs &a, hipStream_t stream)
 {
     const bool seqs = a.by_sequence || a.mean == 1;
-    const auto tokens = seqs ? policy_tokens<true> : policy_tokens<false>;
     if (policy_is_small(a.tokens, a.seqs)) {
-        tokens(a, nullptr, 0, 0, stream);
+        (seqs ? policy_tokens<true, false>
+              : policy_tokens<false, false>)(a, nullptr, 0, 0, 0, stream);
         return hipGetLastError();
     }
     Counts c;
     layout(c, a.ws, a.tokens, a.seqs);
     const int chunks = chunks_of(a.tokens), groups = std::min(chunks, kMaxGroups);
     const int lanes = a.mask ? join_lanes(chunks, a.seqs) : 1, joins = join_groups(a.seqs, lanes);
+    const int own = a.mean == 1 ? own_lanes(a.seqs, lanes) : 0;
     if (a.mask && a.mean != 2)
         policy_count<<<groups, Narrow::BLOCK, 0, stream>>>(a, c, chunks);
-    if (a.mean == 1)
+    if (a.mean == 1 && !own)
         policy_join<<<joins, kJoinBlock, 0, stream>>>(a, c, lanes);
-    tokens(a, &c, groups, joins, stream);
+    (own    ? policy_tokens<true, true>
+     : seqs ? policy_tokens<true, false>
+            : policy_tokens<false, false>)(a, &c, groups, joins, own, stream);
     policy_stats<<<1, 5 * 64, 0, stream>>>(a, c.part, groups);
     return hipGetLastError();
 }
@@ -1508,8 +1610,14 @@ hipError_t launch_preference(const PreferenceArgs &a, hipStream_t stream)
     const int chunks = chunks_of(a.tokens), groups = std::min(chunks, kMaxGroups);
     const int lanes = join_lanes(chunks, 2LL * a.pairs), joins = join_groups(a.pairs, lanes);
     preference_sums<<<groups, Wide::BLOCK, 0, stream>>>(a, p, chunks);
-    preference_pairs<<<joins, kJoinBlock, 0, stream>>>(a, p, lanes);
-    preference_fill<<<(a.dlogp ? groups : 0) + 1, Wide::BLOCK, 0, stream>>>(a, p, chunks, joins);
+    const int own = own_lanes(a.pairs, lanes);
+    if (!own)
+        preference_pairs<<<joins, kJoinBlock, 0, stream>>>(a, p, lanes);
+    const int n = (a.dlogp ? groups : 0) + 1;
+    if (own)
+        preference_fill<true><<<n, Wide::BLOCK, 0, stream>>>(a, p, chunks, joins, own);
+    else
+        preference_fill<false><<<n, Wide::BLOCK, 0, stream>>>(a, p, chunks, joins, own);
     return hipGetLastError();
 }
 
