@@ -15,12 +15,12 @@
 // pair's loss the sums of both its sequences, before the first gradient: that is what
 // the launches are for.  Over the tokens there are two, which read the mask twice and
 // everything else once; the others are over sequences (unless these are few), or join
-// partial sums.  2 000 003
-// tokens move 50 MB for a policy, in 24.1 us, and 26 MB for pairs, in 20.4: the launches
-// over the tokens run at 3 to 4 TB/s (what they read lies in the last-level cache, and
-// each thread has one pack of it), launches and their gaps take the rest.  Up to some
-// 100 000 tokens there is nothing but latency: 3 to 4 us a launch (20 000 to 100 000 tokens in
-// 10 to 16 us), 5 to 11 for one workgroup's chain of loads, scans, exponentials and sums.
+// partial sums.  2 000 003 tokens move 50 MB for a policy, in 24.1 us, and 26 MB for
+// pairs, in 20.4: the launches over the tokens run at 2 to 4 TB/s (a thread has one pack
+// or two, and waits for them once), launches and their gaps take the rest.  Up to some
+// 100 000 tokens there is nothing but latency: 3 to 4 us a launch (20 000 to 100 000
+// tokens in 10 to 16 us), 5 to 11 for one workgroup's chain of loads, scans, exponentials
+// and sums.
 #include <algorithm>
 
 #include "internal.h"
@@ -525,7 +525,7 @@ struct Counts {
 };
 
 // Which tokens count: of each sequence (mean 1) as its pieces, or of the workgroup's
-// chunks.  Reads the mask alone (2 000 003 tokens: 4.1 us, 1024 sequences); not launched
+// chunks.  Reads the mask alone (2 000 003 tokens: 4.4 us, 1024 sequences); not launched
 // where there is none, or where the caller gives the number.
 __global__ __launch_bounds__(Narrow::BLOCK) void policy_count(PolicyArgs a, Counts c, int chunks)
 {
@@ -575,7 +575,7 @@ __device__ __forceinline__ int sequence_tokens(const PolicyArgs &a, const Counts
     return a.mask ? join(has, c.n, s, s0, s1, lanes) : max(s1 - s0, 0);
 }
 
-// Each sequence's tokens that count, and how many sequences have any (2.8 us for 1024:
+// Each sequence's tokens that count, and how many sequences have any (2.3 us for 1024:
 // the latency of starts, then of their pieces).
 constexpr int kJoinBlock = 256;
 
@@ -875,7 +875,7 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
         a.stats[threadIdx.x] = policy_result(a, total, (int)threadIdx.x);
 }
 
-// The losses and gradients of a workgroup's chunks (2 000 003 tokens, 1024 sequences: 13.6
+// The losses and gradients of a workgroup's chunks (2 000 003 tokens, 1024 sequences: 13.8
 // us for 34 MB read and 16 written, 3.7 TB/s).  Some 150 vector instructions a token, of it
 // two exponentials; by 128 registers four workgroups a CU hide their loads behind each
 // other's arithmetic (by 219, two packs' loads and losses at once, two of them: 33 us in
@@ -1214,7 +1214,7 @@ __device__ __forceinline__ Joined join_pair(const PreferenceArgs &a, const Pairs
     return o;
 }
 
-// A thread a pair: its rewards and loss (3.8 us for 1024, the latency of starts, pieces, an
+// A thread a pair: its rewards and loss (4.0 us for 1024, the latency of starts, pieces, an
 // exponential and a logarithm in 64 bits).
 __global__ __launch_bounds__(kJoinBlock) void preference_pairs(PreferenceArgs a, Pairs p, int lanes)
 {
@@ -1275,7 +1275,7 @@ __device__ __forceinline__ void store_gradients(const PreferenceArgs &a, const M
 }
 
 // The gradients; the workgroup behind those of the chunks adds the results (2 000 003
-// tokens: 6.5 us for 2 MB of mask and 8 MB written).
+// tokens: 6.3 us for 2 MB of mask and 8 MB written).
 // OWN: all pairs are joined here, by `lanes` lanes each.
 template <bool OWN>
 __global__ __launch_bounds__(Wide::BLOCK) void preference_fill(PreferenceArgs a, Pairs p,
