@@ -879,7 +879,7 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
 // us for 34 MB read and 16 written, 3.7 TB/s).  Some 150 vector instructions a token, of it
 // two exponentials; by 128 registers four workgroups a CU hide their loads behind each
 // other's arithmetic (by 219, two packs' loads and losses at once, two of them: 33 us in
-// all; the few registers that two of the forms spill cost nothing that shows).
+// all; two to eight spilled registers in some of the forms are in these figures).
 // OWN: all sequences are joined here, by `lanes` lanes each.
 template <bool SEQS, bool OWN, Ref REF>
 __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Counts c, int chunks,
