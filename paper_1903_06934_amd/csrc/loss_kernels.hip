@@ -599,7 +599,8 @@ __global__ __launch_bounds__(kJoinBlock) void policy_join(PolicyArgs a, Counts c
 }
 
 // exp(x): 2^h (1 + l ln 2) with h + l = x log2(e), h its rounding to 32 bits and l what
-// that leaves, so that large |x| lose nothing.  Results below 2^-126 are 0.
+// that leaves, so that large |x| lose nothing.  Results below 2^-126 are 0; those from
+// 2^128 on are infinite, without the factor: infinity times an l of 0 or below is none.
 __device__ __forceinline__ float exp_of(float x)
 {
     constexpr float log2e = 0x1.715476p+0f, rest = 0x1.4ae0bep-26f;  // log2(e) = their sum
@@ -607,7 +608,7 @@ __device__ __forceinline__ float exp_of(float x)
     float l = fmaf(x, log2e, -h);
     l = fmaf(x, rest, l);
     const float e = __builtin_amdgcn_exp2f(h);
-    return fabsf(h) < 200.f ? fmaf(e, l * 0x1.62e43p-1f, e) : e;
+    return fabsf(h) < 128.f ? fmaf(e, l * 0x1.62e43p-1f, e) : e;
 }
 
 // exp(x) - 1 - x, and exp(x) - 1; near 0 by the exponential's series, where the
