@@ -118,7 +118,8 @@ int residual_norm_bwd(int xtype, int wtype, long long rows, long long cols, cons
  * The token is clipped where a > 0 and d > ln(1 + clip_high), a < 0 and d <
  * ln(1 - clip_low), or a < 0 and d > ln(dual_clip); d is compared in 64 bits.  The
  * surrogate's slope in lp is -ratio a, and 0 where it is clipped.  Exponentials are of 32
- * bits: infinite from 2^128 on, 0 below 2^-126.
+ * bits: infinite from 2^128 on, 0 below 2^-126.  Where a is 0, so are the surrogate and
+ * its slope, for an infinite ratio too.
  * Each token's weight u is, by mean:
  *   MISTEP_MEAN_TOKENS     1 / (tokens that count),
  *   MISTEP_MEAN_SEQUENCES  1 / (those of its sequence) / (sequences that have any),

@@ -681,6 +681,8 @@ __device__ __forceinline__ Token token_loss(const PolicyArgs &a, const Borders &
     }
     float r = above ? (gain ? at_high : at_dual) : k.ratio;
     r = below ? b.at_low : r;
+    // No advantage gives nothing, however large the ratio; NaN stays.
+    r = adv == 0.f && r == __builtin_inff() ? 0.f : r;
     k.clipped = (above || below) && fabsf(adv) > 0.f;
     k.surrogate = -adv * r;
     k.slope = k.clipped ? 0.f : k.surrogate;

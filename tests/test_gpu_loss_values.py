@@ -56,3 +56,34 @@ def test_divergences_past_32_bits(tokens, value):
     (stats, sb), (g, gb), _ = want_policy(d, False, "low", False, 1.0, kl_weight=1.0)
     assert_same(out.stats, stats, sb, "stats")
     assert_same(out.dlogp, g, gb, "dlogp")
+
+
+@pytest.mark.parametrize("tokens", [64, 9000])
+@pytest.mark.parametrize("value", [0.5, 100.0, INF])
+def test_no_advantage(tokens, value):
+    """An advantage of 0, of a token or of its whole sequence, gives 0 to the loss and its
+    gradient however large the ratio is."""
+    import paper_1903_06934_amd as m
+    for by, high in ((False, 0.3), (True, 0.3), (True, INF)):
+        d, i = one_far(tokens, "old", value, 0.0)
+        d["adv"][:5], d["seq_adv"][int(i >= d["starts"][1])] = 0.0, 0.0
+        zero = d["adv"] == 0
+        if by:
+            s = int(i >= d["starts"][1])
+            zero = torch.arange(tokens) >= d["starts"][1] if s else torch.arange(tokens) < d["starts"][1]
+        out = m.policy_loss(d["logp"].cuda(), d["old"].cuda(), d["seq_adv" if by else "adv"].cuda(),
+                            by_sequence=by, starts=d["starts"].cuda(), clip_high=high)
+        # By the definition, with a ratio that the 64-bit form can multiply by 0.
+        d["old"][i] = max(float(d["old"][i]), -100.0)
+        (stats, sb), (g, gb), _ = ref.policy(d["logp"], d["old"], d["seq_adv" if by else "adv"], by,
+                                             starts=d["starts"], high=high)
+        assert_same(out.stats, stats, sb, "stats")
+        assert_same(out.dlogp, g, gb, "dlogp")
+        assert bool((out.dlogp.cpu()[zero] == 0).all())
+
+
+def test_no_advantage_and_no_number():
+    import paper_1903_06934_amd as m
+    lp = torch.tensor([0.0, math.nan, -1.0], device="cuda")
+    out = m.policy_loss(lp, torch.zeros(3, device="cuda"), torch.zeros(3, device="cuda"))
+    assert torch.isnan(out.dlogp).tolist() == [False, True, False] and torch.isnan(out.loss)
