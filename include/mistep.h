@@ -113,7 +113,7 @@ int residual_norm_bwd(int xtype, int wtype, long long rows, long long cols, cons
  *   surrogate = -min(ratio a, clamp(ratio, 1 - clip_low, 1 + clip_high) a),
  *               for a < 0 at most -dual_clip a,
  *   kl, with x = lr - lp:   MISTEP_KL_LINEAR  -x,   _SQUARE  x^2 / 2,
- *                           _LOW  exp(x) - 1 - x   (0 without ref_logp),
+ *                           _LOW  exp(x) - 1 - x   (infinite where x is; 0 without ref_logp),
  *   loss = surrogate + kl_weight kl - entropy_weight h   (h = 0 without entropy).
  * The token is clipped where a > 0 and d > ln(1 + clip_high), a < 0 and d <
  * ln(1 - clip_low), or a < 0 and d > ln(dual_clip); d is compared in 64 bits.  The

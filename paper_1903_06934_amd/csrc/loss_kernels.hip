@@ -630,7 +630,7 @@ __device__ __forceinline__ float low_kl(float x, float *expm1)
     *expm1 = x + v;
     if (!(fabsf(x) < 1.f)) {
         *expm1 = exp_of(x) - 1.f;
-        v = *expm1 - x;
+        v = *expm1 - fminf(x, 0x1.fffffep+127f);  // infinite at infinity
     }
     return v;
 }

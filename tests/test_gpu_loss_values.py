@@ -87,3 +87,21 @@ def test_no_advantage_and_no_number():
     lp = torch.tensor([0.0, math.nan, -1.0], device="cuda")
     out = m.policy_loss(lp, torch.zeros(3, device="cuda"), torch.zeros(3, device="cuda"))
     assert torch.isnan(out.dlogp).tolist() == [False, True, False] and torch.isnan(out.loss)
+
+
+@pytest.mark.parametrize("tokens", [64, 9000])
+@pytest.mark.parametrize("kl", ["linear", "square", "low"])
+def test_divergence_of_an_impossible_token(tokens, kl):
+    """A token that has no probability now, or none under the reference: the limits of the
+    divergence and of its slope."""
+    import paper_1903_06934_amd as m
+    for now in (True, False):
+        d, i = one_far(tokens, "ref", 0.0, 1.0)
+        d["logp" if now else "ref"][i] = -INF  # x is +inf, or -inf
+        out = call_policy(m, d, False, kl, False, 1.0, kl_weight=1.0)
+        assert out.kl == (INF if kl != "linear" or not now else -INF)
+        assert out.loss == out.kl
+        want = {"linear": 1.0, "square": -INF if now else INF, "low": -INF if now else 1.0}[kl]
+        # Beside it the surrogate's slope: 0 of a ratio of 0, -1 of a ratio of 1.
+        assert float(out.dlogp[i]) == want - (0.0 if now else 1.0)
+        assert int(torch.isfinite(out.dlogp).sum()) >= tokens - 1
