@@ -873,7 +873,7 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
                                          m[h].mask & inside<S>(m[h], from, to), w[h],
                                          (float)(u * a.scale), sum);
     block_totals<S::BLOCK>(sum, red, [&](int i, double v) { total[i] = v * u; }, counted);
-    // The same wave has written them.
+    __syncthreads();
     if (threadIdx.x < 6)
         a.stats[threadIdx.x] = policy_result(a, total, (int)threadIdx.x);
 }

@@ -7,7 +7,7 @@ import torch
 
 import step_ref as ref
 from test_gpu_step import call_policy, gen, make_policy, want_policy
-from train_ref import INF, assert_close
+from train_ref import INF, U, assert_close
 
 pytestmark = pytest.mark.gpu
 
@@ -105,3 +105,15 @@ def test_divergence_of_an_impossible_token(tokens, kl):
         # Beside it the surrogate's slope: 0 of a ratio of 0, -1 of a ratio of 1.
         assert float(out.dlogp[i]) == want - (0.0 if now else 1.0)
         assert int(torch.isfinite(out.dlogp).sum()) >= tokens - 1
+
+
+def test_results_of_one_workgroup_together():
+    """The loss is that of the same call's sums, call after call on changing tokens."""
+    import paper_1903_06934_amd as m
+    sets = [make_policy(gen(n, 14), n, 3) for n in (5, 300, 4096, 8192)]
+    for _ in range(20):
+        for d in sets:
+            s = call_policy(m, d, True, "low", True, "sequences").stats.double().tolist()
+            size = abs(s[1]) + 0.07 * abs(s[2]) + 0.02 * abs(s[3])
+            # Each statistic and the two weights are rounded once, the loss too.
+            assert abs(s[0] - (s[1] + 0.07 * s[2] - 0.02 * s[3])) <= 3 * U * size
