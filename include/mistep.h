@@ -98,10 +98,8 @@ int residual_norm_bwd(int xtype, int wtype, long long rows, long long cols, cons
  * token counts where it is not 0 and the token is in a sequence.  What the other
  * tensors hold of a token that does not count is not used (it may be NaN), and
  * its gradients are 0.  0 <= tokens, seqs < 2^31 (else MICONV_ERR_SHAPE).
- * Sums are held in 64 bits, but for those of at most eight tokens side by side in
- * the policy loss: these are held in 32 bits, and infinite beyond them.  The
- * gradients are those of the loss, times scale (finite, else MICONV_ERR_VALUE);
- * they are NULL where they are not wanted.
+ * Weights and sums are held in 64 bits.  The gradients are those of the loss, times
+ * scale (finite, else MICONV_ERR_VALUE); they are NULL where they are not wanted.
  */
 
 /*
@@ -117,9 +115,9 @@ int residual_norm_bwd(int xtype, int wtype, long long rows, long long cols, cons
  *   loss = surrogate + kl_weight kl - entropy_weight h   (h = 0 without entropy).
  * The token is clipped where a > 0 and d > ln(1 + clip_high), a < 0 and d <
  * ln(1 - clip_low), or a < 0 and d > ln(dual_clip); d is compared in 64 bits.  The
- * surrogate's slope in lp is -ratio a, and 0 where it is clipped.  Exponentials are of 32
- * bits: infinite from 2^128 on, 0 below 2^-126.  Where a is 0, so are the surrogate and
- * its slope, for an infinite ratio too.
+ * surrogate's slope in lp is -ratio a, and 0 where it is clipped.  Where a is 0, both are
+ * 0, for an infinite ratio too.  A token's terms and slopes are of 32 bits: exponentials
+ * are infinite from 2^128 on, and 0 below 2^-126.
  * Each token's weight u is, by mean:
  *   MISTEP_MEAN_TOKENS     1 / (tokens that count),
  *   MISTEP_MEAN_SEQUENCES  1 / (those of its sequence) / (sequences that have any),

@@ -37,8 +37,15 @@ template <int B, int P, int E>
 struct Tile {
     static constexpr int BLOCK = B, PACKS = P, EACH = E, ALL = B * P, SIZE = ALL * E;
 
-    // Of the thread's h-th pack among all.
-    static __device__ __forceinline__ int rank(int h) { return h * B + (int)threadIdx.x; }
+    // Of the thread's h-th pack among all.  Computed where it is used: what follows from it,
+    // held from chunk to chunk, would take the registers of the tokens (policy_main: up to
+    // ten spilled, 2 000 003 tokens 26.0 us for 24.9).
+    static __device__ __forceinline__ int rank(int h)
+    {
+        int t = (int)threadIdx.x;
+        asm volatile("" : "+v"(t));
+        return h * B + t;
+    }
 };
 
 // Calls of many tokens.  The scans over a chunk cost as much for eight tokens a thread as
@@ -635,17 +642,30 @@ __device__ __forceinline__ float low_kl(float x, float *expm1)
     return v;
 }
 
+// The same in all lanes: held once for the wave, in no lane's register.
+__device__ __forceinline__ float uniform(float v)
+{
+    return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
+}
+
+__device__ __forceinline__ double uniform(double v)
+{
+    const uint2 u = __builtin_bit_cast(uint2, v);
+    return __builtin_bit_cast(double, uint2{(unsigned)__builtin_amdgcn_readfirstlane((int)u.x),
+                                            (unsigned)__builtin_amdgcn_readfirstlane((int)u.y)});
+}
+
 // The borders of the clip in 32 bits, and the ratio at them.
 struct Borders {
     float low, high, dual, at_low, at_high, at_dual;
     float near;  // how near to a border 32 bits do not tell on which side a log ratio is
 
     __device__ __forceinline__ explicit Borders(const PolicyArgs &a)
-        : low((float)a.log_low), high((float)a.log_high), dual((float)a.log_dual), at_low(a.low),
-          at_high(a.high), at_dual(a.dual)
+        : low(uniform((float)a.log_low)), high(uniform((float)a.log_high)),
+          dual(uniform((float)a.log_dual)), at_low(a.low), at_high(a.high), at_dual(a.dual)
     {
         const auto size = [](float v) { return __builtin_isfinite(v) ? fabsf(v) : 0.f; };
-        near = fmaxf(fmaxf(size(low), size(high)), size(dual)) * 0x1p-22f;
+        near = uniform(fmaxf(fmaxf(size(low), size(high)), size(dual)) * 0x1p-22f);
     }
 };
 
@@ -726,43 +746,84 @@ __device__ __forceinline__ void load_tokens(const PolicyArgs &a, const Mine &m, 
         load_floats(a.advantages, m, k.adv);
 }
 
-// The tokens' surrogates, divergences, entropies, ratios and clips (times their
-// weights within their sequences, if WEIGHTS) to sum, their gradients to memory.
-// counted: the tokens that count; w: their weights; factor: what those of the gradients
-// are multiplied by.
-template <bool WEIGHTS, Ref REF, int E>
-__device__ __forceinline__ void token_losses(const PolicyArgs &a, const Borders &borders,
-                                             const Mine &m, const Tokens<E> &k, unsigned counted,
-                                             const float (&w)[E], float factor,
-                                             double (&sum)[5])
+// A pack's weights within their sequences: 1 unless WEIGHTS, 0 of tokens that do not count.
+// counted: those that do; weights, place: theirs, and where they lie.
+template <bool WEIGHTS, int E>
+__device__ __forceinline__ void token_weights(unsigned counted, const double *weights,
+                                              const int (&place)[E], double (&w)[E])
 {
-    float g[E], gh[E], part[5] = {0, 0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < E; j++) {
-        // A token that does not count is one of nothing but zeros, with no weight.  The
-        // few tokens are added in 32 bits: their terms' own roundings are as large.
+        w[j] = WEIGHTS ? weights[place[j]] : 1.0;
+        w[j] = counted >> j & 1 ? w[j] : 0.0;
+    }
+}
+
+// The tokens' entropies, times their weights, to sum, and their gradients to memory; before
+// the rest, so that their registers are free for it.  factor: what a gradient's weight is
+// multiplied by.
+template <int E>
+__device__ __forceinline__ void token_entropies(const PolicyArgs &a, const Mine &m,
+                                                const Tokens<E> &k, const double (&w)[E],
+                                                unsigned counted, double factor, double (&sum)[5])
+{
+    float g[E];
+#pragma unroll
+    for (int j = 0; j < E; j++) {
+        sum[2] = fma((double)(counted >> j & 1 ? k.h[j] : 0.f), w[j], sum[2]);
+        g[j] = (float)(-(double)a.entropy_weight * factor * w[j]);
+    }
+    if (a.dentropy)
+        store_floats(a.dentropy, m, g);
+}
+
+// The tokens' surrogates, divergences, ratios and clips, times their weights, to sum, and
+// their gradients to memory.  A token's terms are of 32 bits, as its log probabilities are;
+// weights, products and sums of 64 (2 000 003 tokens 24.9 us, with all of them in 32 bits up
+// to a thread's sum 24.4), and a gradient is rounded once.
+template <Ref REF, int E>
+__device__ __forceinline__ void token_losses(const PolicyArgs &a, const Borders &borders,
+                                             const Mine &m, const Tokens<E> &k, const double (&w)[E],
+                                             unsigned counted, double factor, double (&sum)[5])
+{
+    float g[E];
+#pragma unroll
+    for (int j = 0; j < E; j++) {
+        // A token that does not count is one of nothing but zeros, with no weight.
         const bool in = counted >> j & 1;
         const auto only = [in](float v) { return in ? v : 0.f; };
         const Token r = token_loss<REF>(a, borders, only(k.lp[j]), only(k.lo[j]),
                                         REF == Ref::none ? 0.f : only(k.lr[j]), only(k.adv[j]));
-        const float d = only(WEIGHTS ? w[j] : 1.f), f = d * factor;
-        part[0] = fmaf(r.surrogate, d, part[0]);
+        sum[0] = fma((double)r.surrogate, w[j], sum[0]);
         if (REF != Ref::none)
-            part[1] = fmaf(r.kl, d, part[1]);
-        part[2] = fmaf(only(k.h[j]), d, part[2]);
-        part[3] = fmaf(r.ratio, d, part[3]);
-        part[4] += r.clipped ? d : 0.f;
-        g[j] = r.slope * f;
-        gh[j] = -a.entropy_weight * f;
+            sum[1] = fma((double)r.kl, w[j], sum[1]);
+        sum[3] = fma((double)r.ratio, w[j], sum[3]);
+        sum[4] += r.clipped ? w[j] : 0.0;
+        g[j] = (float)((double)r.slope * (w[j] * factor));
         __builtin_amdgcn_sched_barrier(0);  // a token at a time: fewer registers, more waves
     }
-#pragma unroll
-    for (int i = 0; i < 5; i++)
-        sum[i] += (double)part[i];
     if (a.dlogp)
         store_floats(a.dlogp, m, g);
-    if (a.dentropy)
-        store_floats(a.dentropy, m, gh);
+}
+
+// A thread's packs.
+template <class S, bool WEIGHTS, Ref REF>
+__device__ __forceinline__ void all_losses(const PolicyArgs &a, const Borders &borders,
+                                           const Mine (&m)[S::PACKS],
+                                           const Tokens<S::EACH> (&k)[S::PACKS], int from, int to,
+                                           const double *weights,
+                                           const int (&place)[S::PACKS][S::EACH], double factor,
+                                           double (&sum)[5])
+{
+    double w[S::EACH];
+#pragma unroll
+    for (int h = 0; h < S::PACKS; h++) {
+        const unsigned counted = m[h].mask & inside<S>(m[h], from, to);
+        token_weights<WEIGHTS>(counted, weights, place[h], w);
+        if (a.entropy)
+            token_entropies(a, m[h], k[h], w, counted, factor, sum);
+        token_losses<REF>(a, borders, m[h], k[h], w, counted, factor, sum);
+    }
 }
 
 // The results from the sums over all tokens (times their weights): the loss is
@@ -779,34 +840,36 @@ __device__ __forceinline__ float policy_result(const PolicyArgs &a, const double
     return (float)v;
 }
 
-// What a sequence gives its tokens.
-struct OfSequence {
-    float weight, adv;
+// What sequences give their tokens, where these begin in the chunk.
+template <int SIZE>
+struct OfSequences {
+    double weight[SIZE];
+    float adv[SIZE];
+
+    // Of sequence s with n tokens that count.
+    __device__ __forceinline__ void set(const PolicyArgs &a, int at, long long s, int n)
+    {
+        const float v = a.by_sequence ? a.advantages[s] : 0.f;  // awaited with n
+        weight[at] = a.mean == 1 ? 1.0 / max(n, 1) : 1.0;
+        adv[at] = v;
+    }
 };
 
-__device__ __forceinline__ OfSequence of_sequence(const PolicyArgs &a, long long s, int n)
-{
-    return OfSequence{a.mean == 1 ? 1.f / (float)max(n, 1) : 1.f,
-                      a.by_sequence ? a.advantages[s] : 0.f};
-}
-
-// The tokens' weights and advantages from what lies where their sequences begin.
+// Where the tokens' weights lie, and their advantages from there.
 template <class S>
 __device__ __forceinline__ void from_sequences(const PolicyArgs &a, Marks<S> &marks,
-                                               const OfSequence *seq,
+                                               const OfSequences<S::SIZE> &seq,
                                                Tokens<S::EACH> (&k)[S::PACKS],
-                                               float (&w)[S::PACKS][S::EACH])
+                                               int (&place)[S::PACKS][S::EACH])
 {
-    int place[S::PACKS][S::EACH];
     marks.places(place);
 #pragma unroll
     for (int h = 0; h < S::PACKS; h++)
 #pragma unroll
         for (int j = 0; j < S::EACH; j++) {
-            const OfSequence q = seq[max(place[h][j], 0)];
-            w[h][j] = q.weight;
+            place[h][j] = max(place[h][j], 0);
             if (a.by_sequence)
-                k[h].adv[j] = q.adv;
+                k[h].adv[j] = seq.adv[place[h][j]];
         }
 }
 
@@ -818,7 +881,7 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
     constexpr int WAVES = S::BLOCK / 64;
     __shared__ Marks<std::conditional_t<SEQS, S, Tile<64, 1, 4>>> marks;
     __shared__ CountTable<std::conditional_t<SEQS, S, Tile<64, 1, 4>>> table;
-    __shared__ OfSequence seq[SEQS ? S::SIZE : 1];
+    __shared__ OfSequences<SEQS ? S::SIZE : 1> seq;
     __shared__ double red[WAVES][5], total[5];
     __shared__ int counts[WAVES][1];
     const Starts starts{a.starts, a.tokens};
@@ -826,14 +889,14 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
     Sequences<S::BLOCK, kPolicyLook> q(starts, SEQS ? a.seqs : 0, 0, a.tokens);
     Mine m[S::PACKS];
     Tokens<S::EACH> k[S::PACKS];
-    float w[S::PACKS][S::EACH];
+    int place[S::PACKS][S::EACH];
 #pragma unroll
     for (int h = 0; h < S::PACKS; h++) {
         m[h] = my_tokens<S>(a.mask, 0, a.tokens, S::rank(h));
         load_tokens<REF>(a, m[h], k[h]);
 #pragma unroll
         for (int j = 0; j < S::EACH; j++)
-            w[h][j] = 1.f;
+            place[h][j] = 0;
     }
     int n[1] = {0};  // tokens that count, or sequences that have any
 #pragma unroll
@@ -854,7 +917,7 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
             if (a.mean == 1)
                 n[0] += c > 0;
             marks.at[s0] = 1;
-            seq[s0] = of_sequence(a, s, c);
+            seq.set(a, s0, s, c);
         });
     }
     if (a.mean != 2) {
@@ -863,15 +926,12 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
     }
     if constexpr (SEQS) {
         __syncthreads();
-        from_sequences(a, marks, seq, k, w);
+        from_sequences(a, marks, seq, k, place);
     }
     const Borders borders(a);
     double sum[5] = {0, 0, 0, 0, 0};
-#pragma unroll
-    for (int h = 0; h < S::PACKS; h++)
-        token_losses<SEQS, REF, S::EACH>(a, borders, m[h], k[h],
-                                         m[h].mask & inside<S>(m[h], from, to), w[h],
-                                         (float)(u * a.scale), sum);
+    all_losses<S, SEQS, REF>(a, borders, m, k, from, to, seq.weight, place, uniform(u * a.scale),
+                             sum);
     block_totals<S::BLOCK>(sum, red, [&](int i, double v) { total[i] = v * u; }, counted);
     __syncthreads();
     if (threadIdx.x < 6)
@@ -882,7 +942,7 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
 // us for 34 MB read and 16 written, 3.7 TB/s).  Some 150 vector instructions a token, of it
 // two exponentials; by 128 registers four workgroups a CU hide their loads behind each
 // other's arithmetic (by 219, two packs' loads and losses at once, two of them: 33 us in
-// all; two to eight spilled registers in some of the forms are in these figures).
+// all).
 // OWN: all sequences are joined here, by `lanes` lanes each.
 template <bool SEQS, bool OWN, Ref REF>
 __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Counts c, int chunks,
@@ -891,7 +951,7 @@ __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Co
     typedef Narrow S;
     __shared__ int n_of[OWN ? S::BLOCK : 1], some[S::BLOCK / 64][1];
     __shared__ Marks<std::conditional_t<SEQS, S, Tile<64, 1, 4>>> marks;
-    __shared__ OfSequence seq[SEQS ? S::SIZE : 1];
+    __shared__ OfSequences<SEQS ? S::SIZE : 1> seq;
     __shared__ double red[S::BLOCK / 64][5], of_all;
     const Starts starts{a.starts, a.tokens};
     const Borders borders(a);
@@ -921,14 +981,14 @@ __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Co
         Sequences<S::BLOCK, kPolicyLook> q(starts, SEQS ? a.seqs : 0, begin, end);
         Mine m[S::PACKS];
         Tokens<S::EACH> tokens[S::PACKS];
-        float w[S::PACKS][S::EACH];
+        int place[S::PACKS][S::EACH];
 #pragma unroll
         for (int h = 0; h < S::PACKS; h++) {
             m[h] = my_tokens<S>(a.mask, begin, end, S::rank(h));
             load_tokens<REF>(a, m[h], tokens[h]);
 #pragma unroll
             for (int j = 0; j < S::EACH; j++)
-                w[h][j] = 1.f;
+                place[h][j] = 0;
         }
         if constexpr (SEQS) {
             marks.clear();
@@ -941,19 +1001,16 @@ __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Co
                 else if (a.mean == 1 && a.mask)
                     n = c.n.seq[s];
                 marks.at[at] = 1;
-                seq[at] = of_sequence(a, s, n);
+                seq.set(a, at, s, n);
             });
         }
         if (SEQS || k == (int)blockIdx.x)
             __syncthreads();
-        u = of_all;
+        u = uniform(of_all);
         if constexpr (SEQS)
-            from_sequences(a, marks, seq, tokens, w);
-#pragma unroll
-        for (int h = 0; h < S::PACKS; h++)
-            token_losses<SEQS, REF, S::EACH>(a, borders, m[h], tokens[h],
-                                             m[h].mask & inside<S>(m[h], from, to), w[h],
-                                             (float)(u * a.scale), sum);
+            from_sequences(a, marks, seq, tokens, place);
+        all_losses<S, SEQS, REF>(a, borders, m, tokens, from, to, seq.weight, place,
+                                 uniform(u * a.scale), sum);
         if (SEQS)
             __syncthreads();
     }

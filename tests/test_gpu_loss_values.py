@@ -7,7 +7,7 @@ import torch
 
 import step_ref as ref
 from test_gpu_step import call_policy, gen, make_policy, want_policy
-from train_ref import INF, U, assert_close
+from train_ref import INF, U, assert_close, half_ulp
 
 pytestmark = pytest.mark.gpu
 
@@ -117,3 +117,52 @@ def test_results_of_one_workgroup_together():
             size = abs(s[1]) + 0.07 * abs(s[2]) + 0.02 * abs(s[3])
             # Each statistic and the two weights are rounded once, the loss too.
             assert abs(s[0] - (s[1] + 0.07 * s[2] - 0.02 * s[3])) <= 3 * U * size
+
+
+def policy_of(adv, **kw):
+    """The call on tokens whose ratio is 1: their surrogates are -adv."""
+    import paper_1903_06934_amd as m
+    lp = torch.zeros(len(adv), device="cuda")
+    return m.policy_loss(lp, lp, adv.cuda(), **kw)
+
+
+@pytest.mark.parametrize("tokens", [8, 4000, 8000, 9000])
+def test_sums_hold_what_32_bits_lose(tokens):
+    """Neighbours that cancel each other leave what lies between them; sums past 32 bits
+    whose mean is within them."""
+    adv = torch.zeros(tokens)
+    adv[:3] = torch.tensor([1.0, 2.0 ** -30, -1.0])
+    adv[4:7] = torch.tensor([-1.0, 2.0 ** -31, 1.0])
+    out = policy_of(adv, mean=1.0)
+    assert float(out.loss) == float(out.surrogate) == -(2.0 ** -30 + 2.0 ** -31)
+    big = torch.full((tokens,), 3e38)
+    for kw in ({}, {"starts": torch.tensor([0, tokens // 3, tokens]).cuda(), "mean": "sequences"}):
+        out = policy_of(big, **kw)
+        # The sum's mean in 64 bits, rounded.
+        want = -big[:1].double()
+        assert_close(out.stats[:2], want.expand(2), U * want.abs(), "stats")
+    e = torch.tensor([1.0, 2.0 ** -30, -1.0, 0.0]).repeat(tokens // 4).cuda()
+    out = policy_of(torch.zeros(tokens), entropy=e, mean=float(tokens // 4))
+    assert float(out.entropy) == 2.0 ** -30
+
+
+@pytest.mark.parametrize("tokens,seqs", [(4000, 40), (8000, 33), (50000, 300), (200000, 7)])
+def test_gradients_are_rounded_once(tokens, seqs):
+    """Of slopes that 32 bits hold: at the nearest number of 32 bits, but for what the
+    weights' 64 bits decide."""
+    import paper_1903_06934_amd as m
+    d = make_policy(gen(tokens, 15), tokens, seqs)
+    lp, ent, starts = torch.zeros(tokens), d["entropy"], d["starts"]
+    length = (starts[1:] - starts[:-1]).double()
+    seq = torch.searchsorted(starts[1:].contiguous(), torch.arange(tokens), right=True)
+    each = {"sequences": 1 / length[seq] / (length > 0).sum(), "tokens": 1 / lp.new_full((1,), tokens,
+            dtype=torch.float64).expand(tokens)}
+    for mean, by in (("sequences", False), ("sequences", True), ("tokens", True)):
+        adv = d["seq_adv" if by else "adv"]
+        out = m.policy_loss(lp.cuda(), lp.cuda(), adv.cuda(), by_sequence=by, entropy=ent.cuda(),
+                            starts=starts.cuda(), entropy_weight=0.25, mean=mean, scale=3.0)
+        g = -3 * (adv[seq] if by else adv).double() * each[mean]
+        for got, want in ((out.dlogp, g), (out.dentropy, -0.75 * each[mean])):
+            # Some five roundings of 64 bits.
+            bound = half_ulp(want, torch.float32) + 2.0 ** -50 * want.abs()
+            assert_close(got, want, bound, f"{mean} {by}")
