@@ -98,8 +98,9 @@ int residual_norm_bwd(int xtype, int wtype, long long rows, long long cols, cons
  * token counts where it is not 0 and the token is in a sequence.  What the other
  * tensors hold of a token that does not count is not used (it may be NaN), and
  * its gradients are 0.  0 <= tokens, seqs < 2^31 (else MICONV_ERR_SHAPE).
- * Weights and sums are held in 64 bits.  The gradients are those of the loss, times
- * scale (finite, else MICONV_ERR_VALUE); they are NULL where they are not wanted.
+ * Weights, sums and the log ratios that pairs add are held in 64 bits.  The gradients
+ * are those of the loss, times scale (finite, else MICONV_ERR_VALUE); they are NULL
+ * where they are not wanted.
  */
 
 /*

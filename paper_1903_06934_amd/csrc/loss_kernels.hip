@@ -1112,18 +1112,19 @@ __device__ __forceinline__ double pair_gradient(const PreferenceArgs &a, double 
     return second ? -v : v;
 }
 
-// The tokens' log ratios, 0 where they do not count.
+// The tokens' log ratios in 64 bits (2 000 003 tokens of 1024 pairs 20.9 us, rounded to 32
+// before they are added 20.7), 0 where they do not count.
 template <int E>
-__device__ __forceinline__ void load_ratios(const PreferenceArgs &a, const Mine &m, float (&v)[E])
+__device__ __forceinline__ void load_ratios(const PreferenceArgs &a, const Mine &m, double (&v)[E])
 {
-    float lr[E];
-    load_floats(a.logp, m, v);
+    float lp[E], lr[E];
+    load_floats(a.logp, m, lp);
     if (a.ref_logp)
         load_floats(a.ref_logp, m, lr);
 #pragma unroll
     for (int j = 0; j < E; j++) {
-        v[j] = a.ref_logp ? v[j] - lr[j] : v[j];
-        v[j] = m.mask >> j & 1 ? v[j] : 0.f;
+        v[j] = a.ref_logp ? (double)lp[j] - (double)lr[j] : (double)lp[j];
+        v[j] = m.mask >> j & 1 ? v[j] : 0.0;
     }
 }
 
@@ -1138,7 +1139,7 @@ struct Sums {
 
     // One barrier; the caller's follows.
     __device__ __forceinline__ void scan(const Marks<S> &marks,
-                                         const float (&v)[S::PACKS][S::EACH])
+                                         const double (&v)[S::PACKS][S::EACH])
     {
         const int lane = threadIdx.x & 63;
         double run[S::PACKS][S::EACH], before[S::PACKS];
@@ -1151,7 +1152,7 @@ struct Sums {
             double s = 0;
 #pragma unroll
             for (int j = 0; j < S::EACH; j++) {
-                s = mine[h] >> j & 1 ? (double)v[h][j] : s + (double)v[h][j];
+                s = mine[h] >> j & 1 ? v[h][j] : s + v[h][j];
                 run[h][j] = s;
             }
             // A lane takes those before it up to the last that has a mark.
@@ -1220,7 +1221,7 @@ __global__ __launch_bounds__(Wide::BLOCK) void preference_sums(PreferenceArgs a,
     for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
         const int begin = k * S::SIZE, end = end_of_chunk(begin, a.tokens);
         Sequences<S::BLOCK, kPairsLook> q(starts, 2 * a.pairs, begin, end);
-        float v[S::PACKS][S::EACH];
+        double v[S::PACKS][S::EACH];
 #pragma unroll
         for (int h = 0; h < S::PACKS; h++) {
             const Mine m = my_tokens<S>(a.mask, begin, end, S::rank(h));
@@ -1434,7 +1435,7 @@ __global__ __launch_bounds__(S::BLOCK) void preference_one(PreferenceArgs a)
     __shared__ int counts[S::BLOCK / 64];
     const Starts starts{a.starts, a.tokens};
     Mine m[S::PACKS];
-    float v[S::PACKS][S::EACH];
+    double v[S::PACKS][S::EACH];
 #pragma unroll
     for (int h = 0; h < S::PACKS; h++) {
         m[h] = my_tokens<S>(a.mask, 0, a.tokens, S::rank(h));

@@ -166,3 +166,17 @@ def test_gradients_are_rounded_once(tokens, seqs):
             # Some five roundings of 64 bits.
             bound = half_ulp(want, torch.float32) + 2.0 ** -50 * want.abs()
             assert_close(got, want, bound, f"{mean} {by}")
+
+
+@pytest.mark.parametrize("tokens", [8, 4000, 8000, 9000, 300000])
+def test_log_ratios_hold_what_32_bits_lose(tokens):
+    """Differences of log probabilities that 32 bits cannot hold, which cancel in the sum."""
+    import paper_1903_06934_amd as m
+    lp, lr = torch.zeros(tokens), torch.zeros(tokens)
+    half = tokens // 2
+    lp[:2], lr[0] = torch.tensor([1.0, -1.0]), 2.0 ** -30
+    lp[half:half + 2], lr[half + 1] = torch.tensor([-1.0, 1.0]), -2.0 ** -28
+    starts = torch.tensor([0, half, tokens])
+    out = m.preference_loss(lp.cuda(), lr.cuda(), starts.cuda(), 1.0)
+    assert out.rewards.tolist() == [-2.0 ** -30, 2.0 ** -28]
+    assert float(out.gap) == -2.0 ** -30 - 2.0 ** -28
