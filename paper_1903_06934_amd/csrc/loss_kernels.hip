@@ -15,8 +15,8 @@
 // pair's loss the sums of both its sequences, before the first gradient: that is what
 // the launches are for.  Over the tokens there are two, which read the mask twice and
 // everything else once; the others are over sequences (unless these are few), or join
-// partial sums.  2 000 003 tokens move 50 MB for a policy, in 24.1 us, and 26 MB for
-// pairs, in 20.4: the launches over the tokens run at 2 to 4 TB/s (a thread has one pack
+// partial sums.  2 000 003 tokens move 50 MB for a policy, in 25.3 us, and 26 MB for
+// pairs, in 20.5: the launches over the tokens run at 2 to 4 TB/s (a thread has one pack
 // or two, and waits for them once), launches and their gaps take the rest.  Up to some
 // 100 000 tokens there is nothing but latency: 3 to 4 us a launch (20 000 to 100 000
 // tokens in 10 to 16 us), 5 to 11 for one workgroup's chain of loads, scans, exponentials
@@ -50,15 +50,15 @@ struct Tile {
 
 // Calls of many tokens.  The scans over a chunk cost as much for eight tokens a thread as
 // for four, but eight tokens of a policy at once take too many registers (2 000 003
-// tokens: pairs 20.1 us, by packs of four 21.1; policy 33.0 by packs of eight, 24.7 by two
+// tokens: pairs 20.6 us, by packs of four 21.7; policy 26.0 by packs of eight, 24.8 by two
 // of four).
 constexpr int kChunk = 2048;
 typedef Tile<256, 1, 8> Wide;
 typedef Tile<256, 2, 4> Narrow;
 static_assert(Wide::SIZE == kChunk && Narrow::SIZE == kChunk, "one chunk for all launches");
 // Calls of few, in one workgroup: up to 4096 tokens, and up to 8192 (4000 tokens: policy
-// 5.7 us, pairs 7.8, by the larger 7.7 and 9.0; 8000 tokens 11.1 and 9.3, by chunks 15.2 and
-// 13.4).
+// 5.2 us, pairs 7.7, by the larger 6.3 and 9.2; 8000 tokens 10.9 and 9.5, by chunks 13.8 and
+// 11.2).
 typedef Tile<1024, 1, 4> SmallPolicy;
 typedef Tile<512, 1, 8> SmallPairs;
 typedef Tile<1024, 1, 8> Small;
@@ -224,7 +224,7 @@ struct Search {
 // workgroup to go through.  Each thread looks at LOOK of them, loaded at once and before
 // the chunk's tokens, so that these latencies overlap; if there are more, they are
 // searched for the chunk's first and last before (2 000 003 tokens: 1024 pairs with LOOK 8
-// 21.3 us, with 4 and a search 23.0; 1024 sequences of a policy 26.2 and 24.6, as 8 take
+// 20.6 us, with 4 and a search 22.0; 1024 sequences of a policy 29.6 and 24.8, as 8 take
 // the registers of a fourth workgroup a CU).
 constexpr int kPolicyLook = 4, kPairsLook = 8;
 
@@ -532,7 +532,7 @@ struct Counts {
 };
 
 // Which tokens count: of each sequence (mean 1) as its pieces, or of the workgroup's
-// chunks.  Reads the mask alone (2 000 003 tokens: 4.4 us, 1024 sequences); not launched
+// chunks.  Reads the mask alone (2 000 003 tokens: 4.6 us, 1024 sequences); not launched
 // where there is none, or where the caller gives the number.
 __global__ __launch_bounds__(Narrow::BLOCK) void policy_count(PolicyArgs a, Counts c, int chunks)
 {
@@ -582,7 +582,7 @@ __device__ __forceinline__ int sequence_tokens(const PolicyArgs &a, const Counts
     return a.mask ? join(has, c.n, s, s0, s1, lanes) : max(s1 - s0, 0);
 }
 
-// Each sequence's tokens that count, and how many sequences have any (2.3 us for 1024:
+// Each sequence's tokens that count, and how many sequences have any (2.4 us for 1024:
 // the latency of starts, then of their pieces).
 constexpr int kJoinBlock = 256;
 
@@ -938,11 +938,10 @@ __global__ __launch_bounds__(S::BLOCK) void policy_one(PolicyArgs a)
         a.stats[threadIdx.x] = policy_result(a, total, (int)threadIdx.x);
 }
 
-// The losses and gradients of a workgroup's chunks (2 000 003 tokens, 1024 sequences: 13.8
-// us for 34 MB read and 16 written, 3.7 TB/s).  Some 150 vector instructions a token, of it
-// two exponentials; by 128 registers four workgroups a CU hide their loads behind each
-// other's arithmetic (by 219, two packs' loads and losses at once, two of them: 33 us in
-// all).
+// The losses and gradients of a workgroup's chunks (2 000 003 tokens, 1024 sequences: 15.6
+// us for 34 MB read and 16 written, 3.2 TB/s).  Some 160 vector instructions a token, of it
+// two exponentials; by 128 registers, none spilled, four workgroups a CU hide their loads
+// behind each other's arithmetic.
 // OWN: all sequences are joined here, by `lanes` lanes each.
 template <bool SEQS, bool OWN, Ref REF>
 __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Counts c, int chunks,
@@ -1019,7 +1018,7 @@ __global__ __launch_bounds__(Narrow::BLOCK, 4) void policy_main(PolicyArgs a, Co
     });
 }
 
-// A wave a sum of the workgroups' (2.0 us).
+// A wave a sum of the workgroups' (2.0 to 3.7 us).
 __global__ __launch_bounds__(5 * 64) void policy_stats(PolicyArgs a, const double *part, int groups)
 {
     __shared__ double sum[5];
@@ -1112,8 +1111,8 @@ __device__ __forceinline__ double pair_gradient(const PreferenceArgs &a, double 
     return second ? -v : v;
 }
 
-// The tokens' log ratios in 64 bits (2 000 003 tokens of 1024 pairs 20.9 us, rounded to 32
-// before they are added 20.7), 0 where they do not count.
+// The tokens' log ratios in 64 bits (2 000 003 tokens of 1024 pairs 20.7 us, rounded to 32
+// before they are added 20.5), 0 where they do not count.
 template <int E>
 __device__ __forceinline__ void load_ratios(const PreferenceArgs &a, const Mine &m, double (&v)[E])
 {
@@ -1209,7 +1208,7 @@ __device__ __forceinline__ void mark_sequence(M &marks, int first, int end)
 
 // The sums of log ratios and the counts of each sequence, or its pieces: a segmented scan
 // over the chunk in 64 bits, at whose places the sequences' threads look (2 000 003
-// tokens: 9.2 us for 18 MB, 74 vector instructions a token).
+// tokens: 9.4 us for 18 MB, 76 vector instructions a token).
 __global__ __launch_bounds__(Wide::BLOCK) void preference_sums(PreferenceArgs a, Pairs p,
                                                                 int chunks)
 {
@@ -1336,7 +1335,7 @@ __device__ __forceinline__ void store_gradients(const PreferenceArgs &a, const M
 }
 
 // The gradients; the workgroup behind those of the chunks adds the results (2 000 003
-// tokens: 6.3 us for 2 MB of mask and 8 MB written).
+// tokens: 6.4 us for 2 MB of mask and 8 MB written).
 // OWN: all pairs are joined here, by `lanes` lanes each.
 template <bool OWN>
 __global__ __launch_bounds__(Wide::BLOCK) void preference_fill(PreferenceArgs a, Pairs p,
@@ -1512,7 +1511,7 @@ __global__ __launch_bounds__(S::BLOCK) void preference_one(PreferenceArgs a)
 int chunks_of(long long tokens) { return (int)std::max(1LL, (tokens + kChunk - 1) / kChunk); }
 
 // Lanes for a sequence: some two for each of its chunks, on an average, up to a wave (2 199
-// 573 tokens of 58 pairs: 22.6 us, with one lane 56.0; 1 015 210 of 174 15.9 and 20.1).
+// 573 tokens of 58 pairs: 24.1 us, with one lane 60.4; 1 015 210 of 174 16.2 and 20.7).
 int join_lanes(int chunks, long long seqs)
 {
     int lanes = 1;
@@ -1530,9 +1529,9 @@ int join_groups(long long n, int lanes)
 
 // So few sequences or pairs that every workgroup of the launch over the tokens joins all of
 // them itself, which saves a launch: lanes for each, else 0; at least half of what a launch
-// of their own would give them (158 508 tokens of 199 pairs 11.6 us, with that launch 13.9; 42
-// 011 of a policy's 45 sequences 14.4 and 16.2; 2 468 375 of 79 pairs, by two lanes instead
-// of 16, 41.3 and 24.0).
+// of their own would give them (158 508 tokens of 199 pairs 11.4 us, with that launch 13.7; 42
+// 011 of a policy's 45 sequences 14.0 and 15.9; 2 468 375 of 79 pairs, by two lanes instead
+// of 16, 34.6 and 24.2).
 int own_lanes(long long n, int lanes)
 {
     int own = 64;

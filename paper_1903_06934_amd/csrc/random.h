@@ -52,7 +52,7 @@ struct Dropper {
         philox(key0, key1, step, layer, g, w);
     }
 
-    // The bits of element i of 2 * (words) elements.
+    // Whether the element is kept whose bits are word's high half (odd), or its low one.
     __device__ __forceinline__ bool kept(uint32_t word, int odd) const
     {
         return (odd ? word >> 16 : word & 0xffff) >= below;

@@ -7,7 +7,7 @@
 // stream's gradient are read, that of the branch and of the residual written, which are
 // one tensor where nothing is dropped.  Bound by memory (16384 x 4096 bf16: forward 94.1
 // us for 537 MB, 5.7 TB/s, the sum and the norm by launches of their own 64.7 and 47;
-// backward 132 for 671 MB and 34 MB of partial sums, 5.3 TB/s), rows of few elements a
+// backward 138 for 671 MB, 4.9 TB/s, and 34 MB of partial sums), rows of few elements a
 // thread by the loads they wait for (12544 x 513 fp32 backward 25.7 us, a copy of as many
 // bytes 21), few rows by latencies (4 x 2048 bf16 forward 4.0).
 // total is rounded to its type before its statistics are taken, so that the backward
